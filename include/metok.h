@@ -25,7 +25,8 @@
  *     legacy default stream) and the call returns without synchronising.
  *     Outputs, including device-resident counts, are valid once the caller has
  *     synchronised with the stream.
- *   - Inputs are never written, except the K/V buffers of metok_kv_compact.
+ *   - Inputs are never written, except the K/V buffers of metok_kv_compact and what
+ *     (6) to (8) say of a paged cache.
  *   - dtype: METOK_F32 (float) or METOK_BF16 (bfloat16).  bf16 paths accumulate
  *     in fp32; selections compare fp32 scores; ties always go to the lower index.
  *   - Ratios are doubles; every count derived from a ratio is
@@ -407,6 +408,112 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
                      int vis_start, int n_vis, const float* scores, int scores_per_layer,
                      int32_t* keep_idx, int32_t* keep_len, int32_t* new_len,
                      void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * (6) A paged K/V cache: the append that fills it.
+ *
+ *   One layer's cache is two pools of pages, [n_pages][Hkv][page_size][dh] of
+ *   `dtype`.  Row r of sequence b lies in page block_table[b][r / page_size] at row
+ *   r % page_size of every K/V head; a sequence holds kv_len[b] rows and has room for
+ *   S_cap = max_pages * page_size.  Entries of block_table behind a sequence's rows are
+ *   not read.  page_size is a power of two from 16 to 256.
+ *   Beside the pools a cache may have, per sequence, arrays [n_seqs][S_cap]:
+ *     positions  int32, the row's original position in the prompt, in [0, 2^24);
+ *     mass       float, the attention weight that the row has got so far.
+ *
+ *   metok_paged_append writes new rows i = new_offsets[b] .. new_offsets[b+1]-1 of
+ *   k_new / v_new ([Hkv][n_new][dh], strides in ELEMENTS between heads and between rows,
+ *   multiples of 16 bytes, row strides >= dh) behind sequence b's kv_len[b] rows, with
+ *   positions pos_new[i] (NULL: counted on from the position of the last row, from 0 in an
+ *   empty sequence) and mass mass_new[i] (NULL: 0), and new_len[b] = kv_len[b] + the number
+ *   of its rows.  new_offsets NULL: one row for every sequence (n_new = n_seqs).  kv_len is
+ *   not written: the layers of a decoder append with the same kv_len; new_len must not
+ *   overlap it.
+ *   No two rows of a call may go to the same place (pages that sequences share hold only rows
+ *   that are there already), and the new rows are not in the pools.
+ *   A sequence without room for its rows, with a length outside [0, S_cap], new_offsets that descend or
+ *   leave [0, n_new], or a page outside [0, n_pages) among those to be written, is reported
+ *   by status = METOK_ERR_INVALID_ARG and new_len[b] = kv_len[b]; its rows behind kv_len are
+ *   then unspecified, the other sequences are served as usual.
+ *   DEVICE int32 / float arrays are 4-byte aligned; pools and new rows 16-byte aligned.
+ *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1 (n_new may be 0), strides,
+ *   pos_new without positions, mass_new without mass, n_new != n_seqs without new_offsets,
+ *   new_len overlapping kv_len); UNSUPPORTED (dh other than 64 or 128, page_size, more than
+ *   2^31 - 1 rows of all heads in a pool, S_cap > 2^24).
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    void* k_pool;
+    void* v_pool;
+    const int32_t* block_table;
+    const int32_t* kv_len;
+    int n_pages, Hkv, page_size, dh, n_seqs, max_pages;
+} metok_paged_cache;
+
+METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const void* k_new, const void* v_new,
+                        int64_t k_head, int64_t k_row, int64_t v_head, int64_t v_row, int n_new,
+                        const int32_t* new_offsets, int32_t* positions, const int32_t* pos_new,
+                        float* mass, const float* mass_new, int32_t* new_len, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * (7) Attention of one new token per sequence over its paged cache.
+ *
+ *   The token's own K and V are the cache's last row (metok_paged_append).  Query head h
+ *   reads K/V head h / (Hq / Hkv) and sees every row j of its sequence:
+ *     x_j = softmax_scale * <q, k_j>
+ *     x_j = softcap * tanh(x_j / softcap)                 if softcap > 0
+ *     x_j = x_j - slopes[h] * |pos[kv_len[b]-1] - pos[j]| if slopes
+ *     out = sum_j softmax(x)_j v_j,   lse = ln sum_j exp(x_j)
+ *   with pos = `positions` ([n_seqs][S_cap]; NULL: the row's index).  If `mass` is
+ *   given, mass[b][j] += (1/Hq) sum_h softmax(x)_j for every row j of b: the weight that
+ *   metok_attention_scores takes the mean of, added up token by token.
+ *   A sequence of no rows gets out = 0, lse = -infinity.
+ *
+ *   q, out  DEVICE [n_seqs][Hq][dh], strides in elements (multiples of 16 bytes, elements of
+ *           a head contiguous); lse DEVICE float [n_seqs][Hq] or NULL; slopes DEVICE float [Hq] or NULL
+ *   Rows of a page behind the sequence's last row are not used, whatever they hold.
+ *   A sequence whose length or pages are out of range is reported by status =
+ *   METOK_ERR_INVALID_ARG and its out, lse and mass are left as they were.
+ *   The work is cut along the caches' lengths into equal pieces for all SMs and joined
+ *   by a second kernel; a call's results depend on nothing but its inputs.
+ *   Errors: INVALID_ARG (null or misaligned pointers, Hq % Hkv, strides, softmax_scale not
+ *   finite or <= 0, softcap < 0 or not finite, and as in (6)); UNSUPPORTED (as in (6), Hq > 8192,
+ *   more than 2^31 - 1 pieces of work); WORKSPACE.
+ * ------------------------------------------------------------------------- */
+METOK_API size_t metok_paged_attention_workspace_bytes(int dtype, const metok_paged_cache* c, int Hq, int with_mass);
+METOK_API int metok_paged_attention(int dtype, const metok_paged_cache* c, const void* q, int64_t q_seq, int64_t q_head,
+                        int Hq, float softmax_scale, float softcap, const float* slopes, const int32_t* positions,
+                        float* mass, void* out, int64_t out_seq, int64_t out_head, float* lse, int32_t* status,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * (8) Eviction from the paged cache by accumulated attention weight, in place.
+ *
+ *   For every layer l and sequence b with more than `budget` rows, the `budget` rows that
+ *   rank highest stay: first the protected ones, whose position is < n_sink or
+ *   > (position of the last row) - n_recent, then by mass (a NaN ranks highest), equal
+ *   ones by lower row.  new_len[b] = min(kv_len[b], budget).  Kept rows below new_len stay
+ *   where they are; the kept rows behind it, in ascending order, go to the places of the
+ *   rows that leave, in ascending order: no row moves that need not.  So the rows are no
+ *   longer in the order of their positions, which is why positions are wanted here and
+ *   go with their rows; attention over the cache does not depend on the order.
+ *     keep_idx[l][b][i] = the row that row i now holds (i < new_len[b]), -1 behind;
+ *     K and V of every layer, positions and mass [L][n_seqs][S_cap] are moved;
+ *     mass of the rows from new_len[b] to kv_len[b]-1 is set to 0.
+ *
+ *   k_layers, v_layers HOST arrays of L DEVICE pools, no two of them overlapping (c->k_pool
+ *   and v_pool are not read); all layers have the same table and lengths.  new_len must not
+ *   overlap kv_len.
+ *   A sequence whose length or pages are out of range, or that shares a page in use with
+ *   another sequence or has one twice, is left as it is in every layer and reports new_len = kv_len,
+ *   keep_idx = -1 and status = METOK_ERR_INVALID_ARG.
+ *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1, L < 1, budget < 1 or > S_cap,
+ *   n_sink < 0, n_recent < 1, new_len overlapping kv_len, a pool given twice); UNSUPPORTED (as in (6);
+ *   L > 1024, L * n_seqs > 65535); WORKSPACE.
+ * ------------------------------------------------------------------------- */
+METOK_API size_t metok_paged_evict_workspace_bytes(const metok_paged_cache* c, int L, int budget);
+METOK_API int metok_paged_evict(int dtype, const metok_paged_cache* c, void* const* k_layers, void* const* v_layers, int L,
+                        int budget, int n_sink, int n_recent, int32_t* positions, float* mass,
+                        int32_t* keep_idx, int32_t* new_len, int32_t* status, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------- *
  * helpers (host only, no CUDA work)

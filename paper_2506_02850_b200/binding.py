@@ -32,6 +32,7 @@ KV_PAPER, KV_TOPK, KV_GIVEN = 0, 1, 2
 
 _c = ctypes
 _vp, _i, _sz, _f, _d = _c.c_void_p, _c.c_int, _c.c_size_t, _c.c_float, _c.c_double
+_i64 = _c.c_int64
 
 
 class VisionParams(_c.Structure):
@@ -51,6 +52,11 @@ class MetokError(RuntimeError):
         self.cuda_error = cuda_error
         extra = f" (cudaError {cuda_error})" if cuda_error else ""
         super().__init__(f"{fn} failed: {status} {text}{extra}")
+
+
+class PagedCache(_c.Structure):
+    _fields_ = [("k_pool", _vp), ("v_pool", _vp), ("block_table", _vp), ("kv_len", _vp), ("n_pages", _i), ("Hkv", _i), ("page_size", _i),
+                ("dh", _i), ("n_seqs", _i), ("max_pages", _i)]
 
 
 _SIGNATURES = {
@@ -80,6 +86,13 @@ _SIGNATURES = {
     "metok_kv_compact_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "metok_kv_compact": (_i, [_c.POINTER(_vp), _c.POINTER(_vp), _i, _i, _i, _i, _i, _i, _i, _i, _d, _i, _i,
                               _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "metok_paged_append": (_i, [_i, _c.POINTER(PagedCache), _vp, _vp, _i64, _i64, _i64, _i64, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "metok_paged_attention_workspace_bytes": (_sz, [_i, _c.POINTER(PagedCache), _i, _i]),
+    "metok_paged_attention": (_i, [_i, _c.POINTER(PagedCache), _vp, _i64, _i64, _i, _f, _f, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp,
+                                   _vp, _sz, _vp]),
+    "metok_paged_evict_workspace_bytes": (_sz, [_c.POINTER(PagedCache), _i, _i]),
+    "metok_paged_evict": (_i, [_i, _c.POINTER(PagedCache), _c.POINTER(_vp), _c.POINTER(_vp), _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp,
+                               _vp, _sz, _vp]),
     "metok_profile_begin": (_i, []),
     "metok_profile_read": (_i, [_c.c_char_p, _sz]),
     "metok_profile_end": (_i, [_c.c_char_p, _sz]),
@@ -386,6 +399,47 @@ def metok_kv_compact(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch.
                               new_len)
     if type(res) is int:
         _check("metok_kv_compact", res)
+    return res
+
+
+def metok_paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, block_table: torch.Tensor,
+                       kv_len: torch.Tensor, new_offsets: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                       pos_new: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None,
+                       mass_new: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """New rows `k_new`, `v_new` ([Hkv, n_new, dh], any strides between heads and rows) behind the `kv_len` rows of the sequences of one
+    layer's paged cache.  `new_offsets` (int32 [n_seqs + 1]) deals them out; without it every sequence gets one.  `positions` and `mass`
+    ([n_seqs, max_pages * page_size]) get `pos_new` (default: counted on from the last row's) and `mass_new` (default: 0).
+    Returns "new_len" (given, or new) and "status" (0, or -1 where a sequence had no room or a bad page)."""
+    res = _calls().paged_append(k_new, v_new, k_pool, v_pool, block_table, kv_len, new_offsets, positions, pos_new, mass, mass_new,
+                                new_len)
+    if type(res) is int:
+        _check("metok_paged_append", res)
+    return res
+
+
+def metok_paged_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                          softmax_scale: float, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                          positions: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None, with_lse: bool = False,
+                          out: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Attention of one token per sequence (`q` [n_seqs, Hq, dh]) over its cache, whose last row is the token's own.  `mass` gets the
+    rows' attention weight added, as the mean over the heads.  Returns "out", "lse" (`with_lse`) and "status" (0, or -1 where a
+    sequence's length or pages are out of range: it is left out)."""
+    res = _calls().paged_attention(q, k_pool, v_pool, block_table, kv_len, softmax_scale, softcap, slopes, positions, mass, with_lse, out)
+    if type(res) is int:
+        _check("metok_paged_attention", res)
+    return res
+
+
+def metok_paged_evict(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch.Tensor], block_table: torch.Tensor, kv_len: torch.Tensor,
+                      mass: torch.Tensor, positions: torch.Tensor, budget: int, n_sink: int, n_recent: int,
+                      new_len: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Sequences of more than `budget` rows keep, in every layer, those whose position is among the first `n_sink` or the newest
+    `n_recent`, and of the others those with the most `mass`; K, V, `mass` and `positions` ([L, n_seqs, max_pages * page_size]) are moved
+    in place, kept rows behind the new length into the places of rows that leave.  Returns "keep_idx" (int32 [L, n_seqs, budget]: the
+    row that each row now holds, -1 behind the new length), "new_len" and "status" (0, or -1 where a sequence was left as it is)."""
+    res = _calls().paged_evict(k_layers, v_layers, block_table, kv_len, mass, positions, budget, n_sink, n_recent, new_len)
+    if type(res) is int:
+        _check("metok_paged_evict", res)
     return res
 
 

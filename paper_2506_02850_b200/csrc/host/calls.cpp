@@ -15,6 +15,7 @@
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -33,7 +34,9 @@ namespace {
     X(metok_compress_vision_bound) X(metok_compress_vision_workspace_bytes) X(metok_compress_vision)     \
     X(metok_prefill_prune_workspace_bytes) X(metok_prefill_prune)                                        \
     X(metok_retention_budgets) X(metok_prune_schedule_sizes) X(metok_prefill_prune_schedule_workspace_bytes)                        \
-    X(metok_prefill_prune_schedule) X(metok_kv_compact_workspace_bytes) X(metok_kv_compact)
+    X(metok_prefill_prune_schedule) X(metok_kv_compact_workspace_bytes) X(metok_kv_compact)               \
+    X(metok_paged_append) X(metok_paged_attention_workspace_bytes) X(metok_paged_attention)              \
+    X(metok_paged_evict_workspace_bytes) X(metok_paged_evict)
 struct Api {
 #define X(name) decltype(&::name) name;
     METOK_HOST_CALLS(X)
@@ -67,7 +70,7 @@ struct Py {                                                   // owned reference
     X(sims) X(boundaries) X(event_offsets) X(frame_event) X(_sims) X(_boundaries) X(_offsets)            \
     X(token_score) X(token_inv_norm) X(out_feats) X(out_src) X(out_event) X(out_members) X(assign)       \
     X(frame_score) X(event_score) X(event_is_key) X(n_out) X(status) X(scores) X(keep_idx) X(S_out)      \
-    X(hidden_out) X(token_group) X(origin) X(n_vis) X(S) X(_inputs) X(keep_len) X(new_len)
+    X(hidden_out) X(token_group) X(origin) X(n_vis) X(S) X(_inputs) X(keep_len) X(new_len) X(out) X(lse)
 struct Names {
 #define X(name) PyObject* name;
     METOK_HOST_NAMES(X)
@@ -593,6 +596,179 @@ PyObject* kv_compact(PyObject* const* a, Py_ssize_t n) {
     return res.p;
 }
 
+// ---- the paged cache and the attention over it -------------------------------------------------------
+// These calls run on the device of their tensors, whatever the current one is, on that device's current stream; all
+// their tensors lie on it.  Their workspaces come from the caching allocator for the one call: no two calls share one,
+// so that captured graphs may be replayed side by side.
+const at::Tensor& on(PyObject* o, const char* name, const at::Device& dev) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.device() != dev) fail(PyExc_ValueError, "%s is on another device than the call's first tensor", name);
+    return t;
+}
+// A contiguous array of n elements (n < 0: any number) of the type, or an undefined tensor for None.
+at::Tensor array(PyObject* o, const char* name, const at::Device& dev, at::ScalarType dt, int64_t n) {
+    if (o == Py_None) return at::Tensor();
+    const at::Tensor& t = on(o, name, dev);
+    if (!t.is_contiguous()) fail(PyExc_ValueError, "%s must be contiguous", name);
+    if (t.scalar_type() != dt) fail(PyExc_TypeError, dt == at::kInt ? "%s must be int32" : "%s must be float32", name);
+    if (n >= 0 && t.numel() != n) fail(PyExc_ValueError, "%s has the wrong number of elements", name);
+    return t;
+}
+template <typename T>
+T* ptr_or_null(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr; }
+// Rows [heads][rows][dh] whose elements are contiguous; other strides are free.
+const at::Tensor& rows3(PyObject* o, const char* name, const at::Device& dev, at::ScalarType dt) {
+    const at::Tensor& t = on(o, name, dev);
+    if (t.dim() != 3) fail(PyExc_ValueError, "%s has the wrong number of dimensions", name);
+    if (t.scalar_type() != dt) fail(PyExc_TypeError, "%s has another dtype than the call's first tensor", name);
+    if (t.size(2) != 1 && t.stride(2) != 1) fail(PyExc_ValueError, "the elements of a row of %s must be contiguous", name);
+    return t;
+}
+// A dimension's stride; one that is never stepped along counts as `dense` (torch leaves it arbitrary).
+int64_t step(const at::Tensor& t, int dim, int64_t dense) { return t.size(dim) > 1 ? t.stride(dim) : dense; }
+
+const at::Tensor& first_tensor(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (!t.is_cuda()) fail(PyExc_ValueError, "%s must be a CUDA tensor", name);
+    return t;
+}
+int size_of(const at::Tensor& t, int dim, const char* name) {
+    if (t.size(dim) > 0x7FFFFFFF) fail(PyExc_ValueError, "%s is too large", name);
+    return (int)t.size(dim);
+}
+
+// The pools of one layer, the table and the lengths; `hold` keeps the last two.
+metok_paged_cache paged_cache(const at::Tensor& k, PyObject* v_obj, PyObject* table_obj, PyObject* len_obj, at::Tensor* hold) {
+    const at::Device dev = k.device();
+    if (k.dim() != 4 || !k.is_contiguous()) fail(PyExc_ValueError, "%s must be a contiguous [n_pages, Hkv, page_size, dh]", "a pool");
+    const at::Tensor& v = on(v_obj, "a pool", dev);
+    if (v.sizes() != k.sizes() || !v.is_contiguous() || v.scalar_type() != k.scalar_type())
+        fail(PyExc_ValueError, "%s must be contiguous, of one shape and type", "the pools");
+    const at::Tensor& table = on(table_obj, "block_table", dev);
+    if (table.dim() != 2) fail(PyExc_ValueError, "%s must be [n_seqs, max_pages]", "block_table");
+    hold[0] = array(table_obj, "block_table", dev, at::kInt, -1);
+    hold[1] = array(len_obj, "kv_len", dev, at::kInt, table.size(0));
+    if (!hold[1].defined()) fail(PyExc_TypeError, "%s must be a tensor", "kv_len");
+    return {k.data_ptr(), v.data_ptr(), (const int32_t*)hold[0].data_ptr(), (const int32_t*)hold[1].data_ptr(), size_of(k, 0, "a pool"),
+            size_of(k, 1, "a pool"), size_of(k, 2, "a pool"), size_of(k, 3, "a pool"), size_of(table, 0, "block_table"),
+            size_of(table, 1, "block_table")};
+}
+
+// k_new, v_new, k_pool, v_pool, block_table, kv_len, new_offsets, positions, pos_new, mass, mass_new, new_len
+PyObject* paged_append(PyObject* const* a, Py_ssize_t n) {
+    want(n, 12);
+    const at::Tensor& kp = first_tensor(a[2], "k_pool");
+    const at::Device dev = kp.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor hold[2];
+    const metok_paged_cache c = paged_cache(kp, a[3], a[4], a[5], hold);
+    const at::ScalarType dt = kp.scalar_type();
+    const at::Tensor &kn = rows3(a[0], "k_new", dev, dt), &vn = rows3(a[1], "v_new", dev, dt);
+    if (kn.sizes() != vn.sizes() || kn.size(0) != c.Hkv || kn.size(2) != c.dh) fail(PyExc_ValueError, "%s must be [Hkv, n_new, dh]", "k_new, v_new");
+    const int n_new = size_of(kn, 1, "k_new");
+    const int64_t S_cap = (int64_t)c.max_pages * c.page_size;
+    const at::Tensor off = array(a[6], "new_offsets", dev, at::kInt, (int64_t)c.n_seqs + 1), pos = array(a[7], "positions", dev, at::kInt, c.n_seqs * S_cap),
+                     pos_new = array(a[8], "pos_new", dev, at::kInt, n_new), mass = array(a[9], "mass", dev, at::kFloat, c.n_seqs * S_cap),
+                     mass_new = array(a[10], "mass_new", dev, at::kFloat, n_new);
+    at::Tensor new_len = array(a[11], "new_len", dev, at::kInt, c.n_seqs);
+    if (!new_len.defined()) new_len = empty_i32(c.n_seqs, dev);
+    const at::Tensor status = empty_i32(1, dev);
+    const int st = api.metok_paged_append(dtype_code(kp), &c, kn.data_ptr(), vn.data_ptr(), step(kn, 0, 0), step(kn, 1, c.dh), step(vn, 0, 0),
+                                          step(vn, 1, c.dh), n_new, ptr_or_null<const int32_t>(off), ptr_or_null<int32_t>(pos),
+                                          ptr_or_null<const int32_t>(pos_new), ptr_or_null<float>(mass), ptr_or_null<const float>(mass_new),
+                                          (int32_t*)new_len.data_ptr(), (int32_t*)status.data_ptr(), current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.new_len, new_len);
+    put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
+// q, k_pool, v_pool, block_table, kv_len, softmax_scale, softcap, slopes, positions, mass, with_lse, out
+PyObject* paged_attention(PyObject* const* a, Py_ssize_t n) {
+    want(n, 12);
+    const at::Tensor& kp = first_tensor(a[1], "k_pool");
+    const at::Device dev = kp.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor hold[2];
+    const metok_paged_cache c = paged_cache(kp, a[2], a[3], a[4], hold);
+    const at::Tensor& q = rows3(a[0], "q", dev, kp.scalar_type());
+    if (q.size(0) != c.n_seqs || q.size(2) != c.dh) fail(PyExc_ValueError, "%s must be [n_seqs, Hq, dh]", "q");
+    const int Hq = size_of(q, 1, "q"), dt = dtype_code(kp);
+    const int64_t S_cap = (int64_t)c.max_pages * c.page_size;
+    const at::Tensor slopes = array(a[7], "slopes", dev, at::kFloat, Hq), pos = array(a[8], "positions", dev, at::kInt, c.n_seqs * S_cap),
+                     mass = array(a[9], "mass", dev, at::kFloat, c.n_seqs * S_cap);
+    const at::Tensor out = a[11] == Py_None ? empty(q.sizes(), q.scalar_type(), dev) : rows3(a[11], "out", dev, q.scalar_type());
+    if (out.sizes() != q.sizes()) fail(PyExc_ValueError, "%s must have the shape of q", "out");
+    const int with_lse = PyObject_IsTrue(a[10]);
+    if (with_lse < 0) throw PyError();
+    at::Tensor lse;
+    if (with_lse) lse = empty({c.n_seqs, Hq}, at::kFloat, dev);
+    const at::Tensor status = empty_i32(1, dev);
+    const size_t need = api.metok_paged_attention_workspace_bytes(dt, &c, Hq, mass.defined());
+    const at::Tensor ws = empty({(int64_t)need}, at::kByte, dev);
+    const int st = api.metok_paged_attention(
+        dt, &c, q.data_ptr(), step(q, 0, 0), step(q, 1, c.dh), Hq, (float)number(a[5]), (float)number(a[6]), ptr_or_null<const float>(slopes),
+        ptr_or_null<const int32_t>(pos), ptr_or_null<float>(mass), out.data_ptr(), step(out, 0, 0), step(out, 1, c.dh), ptr_or_null<float>(lse),
+        (int32_t*)status.data_ptr(), ws.data_ptr(), need, current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.out, out);
+    if (with_lse) put(res.p, names.lse, lse);
+    put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
+// k_layers, v_layers, block_table, kv_len, mass, positions, budget, n_sink, n_recent, new_len
+PyObject* paged_evict(PyObject* const* a, Py_ssize_t n) {
+    want(n, 10);
+    Seq ks(a[0]), vs(a[1]);
+    if (ks.n < 1) fail(PyExc_ValueError, "%s is empty", "k_layers");
+    if (vs.n != ks.n) fail(PyExc_ValueError, "%s must hold one pool per layer", "v_layers");
+    const at::Tensor& k0 = first_tensor(ks.items[0], "a pool");
+    const at::Device dev = k0.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor hold[2];
+    const metok_paged_cache c = paged_cache(k0, vs.items[0], a[2], a[3], hold);
+    if (ks.n > 1024) return PyLong_FromLong(METOK_ERR_UNSUPPORTED);
+    const int L = (int)ks.n;
+    std::vector<void*> kp(L), vp(L);
+    for (int l = 0; l < L; ++l) {
+        const at::Tensor &k = on(ks.items[l], "a pool", dev), &v = on(vs.items[l], "a pool", dev);
+        if (k.sizes() != k0.sizes() || v.sizes() != k0.sizes() || !k.is_contiguous() || !v.is_contiguous() || k.scalar_type() != k0.scalar_type() ||
+            v.scalar_type() != k0.scalar_type())
+            fail(PyExc_ValueError, "%s must be contiguous, of one shape and type", "the pools");
+        kp[l] = k.data_ptr();
+        vp[l] = v.data_ptr();
+    }
+    const int64_t S_cap = (int64_t)c.max_pages * c.page_size;
+    const at::Tensor mass = array(a[4], "mass", dev, at::kFloat, L * c.n_seqs * S_cap), pos = array(a[5], "positions", dev, at::kInt, L * c.n_seqs * S_cap);
+    const long budget = integer(a[6]), sink = integer(a[7]), recent = integer(a[8]);
+    if (budget < 1 || budget > S_cap || sink < 0 || recent < 1) return PyLong_FromLong(METOK_ERR_INVALID_ARG);
+    // (beyond the largest position nothing changes)
+    const int n_sink = (int)(sink > (1 << 30) ? 1 << 30 : sink), n_recent = (int)(recent > (1 << 30) ? 1 << 30 : recent);
+    at::Tensor new_len = array(a[9], "new_len", dev, at::kInt, c.n_seqs);
+    if (!new_len.defined()) new_len = empty_i32(c.n_seqs, dev);
+    const at::Tensor keep = empty({L, c.n_seqs, budget}, at::kInt, dev), status = empty_i32(1, dev);
+    const size_t need = api.metok_paged_evict_workspace_bytes(&c, L, (int)budget);
+    const at::Tensor ws = empty({(int64_t)need}, at::kByte, dev);
+    const int st = api.metok_paged_evict(dtype_code(k0), &c, kp.data(), vp.data(), L, (int)budget, n_sink, n_recent, ptr_or_null<int32_t>(pos),
+                                         ptr_or_null<float>(mass), (int32_t*)keep.data_ptr(), (int32_t*)new_len.data_ptr(),
+                                         (int32_t*)status.data_ptr(), ws.data_ptr(), need, current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.keep_idx, keep);
+    put(res.p, names.new_len, new_len);
+    put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
 // Runs a call and turns its failures into Python exceptions.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -616,6 +792,9 @@ PyMethodDef methods[] = {
     FAST("prefill_prune", prefill_prune),
     FAST("prefill_prune_schedule", prefill_prune_schedule),
     FAST("kv_compact", kv_compact),
+    FAST("paged_append", paged_append),
+    FAST("paged_attention", paged_attention),
+    FAST("paged_evict", paged_evict),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_metok_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

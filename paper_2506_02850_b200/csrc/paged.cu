@@ -1,0 +1,426 @@
+// metok_paged_append and metok_paged_evict: rows into a paged K/V cache, and out of it by accumulated attention weight.
+#include "launchers.h"
+#include "paged.cuh"
+
+namespace metok {
+
+namespace {
+
+// ---- append -------------------------------------------------------------------------
+// A warp copies kAppendChunks 16-byte chunks per lane of one new row (all heads, K then V): a row of 4 heads of 128 bf16 is
+// one warp's work, one of 40 fp32 heads that of twenty, so that a step of few rows still fills the SMs.  Reads and writes are
+// contiguous pieces of dh elements; what bounds a long call is HBM, a step's call its launch and three round trips (the
+// row's sequence, its length and page, the copy).
+constexpr int kAppendWarps = 8, kAppendChunks = 4;
+
+struct AppendArgs {
+    PagedDims d;
+    const uint4 *k_new, *v_new;
+    uint4 *k_pool, *v_pool;
+    long long k_head, k_row, v_head, v_row;            // in 16-byte chunks
+    int n_new, parts;
+    const int32_t *block_table, *kv_len, *offsets, *pos_new;
+    int32_t* positions;
+    float* mass;
+    const float* mass_new;
+    int32_t *new_len, *status;
+};
+
+// The sequence of new row i: the number of offsets[1 .. n) that are <= i.  Whole warp, 32-ary search; with offsets that
+// descend the answer is some sequence, which the caller finds not to hold the row.
+__device__ __forceinline__ int sequence_of(const int32_t* __restrict__ offsets, int n, int i, int lane) {
+    int lo = 0, left = n - 1;                          // it lies in [lo, lo + left]
+    while (left > 0) {
+        const int step = (left + 31) >> 5, at = lane * step + step - 1;
+        const uint32_t beyond = __ballot_sync(0xFFFFFFFFu, at >= left ? true : offsets[1 + lo + at] > i);
+        if (!beyond) return lo + left;
+        const int skip = (__ffs(beyond) - 1) * step;
+        lo += skip;
+        left = min(step - 1, left - skip);
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(kAppendWarps * 32)
+paged_append_kernel(const AppendArgs a) {
+    grid_dep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, S_cap = a.d.S_cap();
+    if (blockIdx.x == 0) {                             // the first CTA checks the sequences and writes their lengths
+        int bad = 0;
+        for (int b = warp; b < a.d.n_seqs; b += kAppendWarps) {
+            const int len = a.kv_len[b], lo = a.offsets ? a.offsets[b] : b, hi = a.offsets ? a.offsets[b + 1] : b + 1;
+            bool ok = lo >= 0 && hi >= lo && hi <= a.n_new && len >= 0 && len <= S_cap && hi - lo <= S_cap - len;
+            if (ok && hi > lo) {
+                const int p1 = (len + hi - lo - 1) >> a.d.page_shift;
+                bool there = true;
+                for (int p = (len >> a.d.page_shift) + lane; p <= p1; p += 32) {
+                    const int page = a.block_table[(size_t)b * a.d.max_pages + p];
+                    there &= page >= 0 && page < a.d.n_pages;
+                }
+                ok = __all_sync(0xFFFFFFFFu, there);
+            }
+            if (lane == 0) a.new_len[b] = ok ? len + hi - lo : len;
+            bad |= !ok;
+        }
+        bad = __syncthreads_or(bad);
+        if (threadIdx.x == 0) *a.status = bad ? METOK_ERR_INVALID_ARG : METOK_OK;
+        return;
+    }
+    const long long item = (long long)(blockIdx.x - 1) * kAppendWarps + warp;
+    const int i = (int)(item / a.parts), part = (int)(item - (long long)i * a.parts);
+    if (i >= a.n_new) return;
+    const int b = a.offsets ? sequence_of(a.offsets, a.d.n_seqs, i, lane) : i;
+    const int lo = a.offsets ? a.offsets[b] : b, hi = a.offsets ? a.offsets[b + 1] : b + 1, len = a.kv_len[b];
+    // the row is the sequence's, and the sequence has room
+    if (i < lo || i >= hi || lo < 0 || hi > a.n_new || len < 0 || len > S_cap || hi - lo > S_cap - len) return;
+    const int row = len + (i - lo);
+    const int page = a.block_table[(size_t)b * a.d.max_pages + (row >> a.d.page_shift)];
+    if (page < 0 || page >= a.d.n_pages) return;
+    const int cpr = a.d.row_chunks, half = a.d.Hkv * cpr;
+    uint4* to[kAppendChunks];
+    uint4 v[kAppendChunks];
+#pragma unroll
+    for (int u = 0; u < kAppendChunks; ++u) {
+        int e = part * (32 * kAppendChunks) + u * 32 + lane;
+        to[u] = nullptr;
+        if (e >= 2 * half) continue;
+        const bool is_v = e >= half;
+        if (is_v) e -= half;
+        const int h = e / cpr, c = e - h * cpr;
+        to[u] = (is_v ? a.v_pool : a.k_pool) + paged_chunk(a.d, page, h, row) + c;
+        v[u] = __ldg(is_v ? a.v_new + h * a.v_head + i * a.v_row + c : a.k_new + h * a.k_head + i * a.k_row + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendChunks; ++u)
+        if (to[u]) *to[u] = v[u];
+    if (part == 0 && lane == 0) {
+        if (a.positions) {
+            int32_t* pos = a.positions + (size_t)b * S_cap;
+            pos[row] = a.pos_new ? a.pos_new[i] : (len > 0 ? pos[len - 1] + 1 : 0) + (i - lo);
+        }
+        if (a.mass) a.mass[(size_t)b * S_cap + row] = a.mass_new ? a.mass_new[i] : 0.f;
+    }
+}
+
+// ---- evict --------------------------------------------------------------------------
+// Three kernels.  claim: every page in use is claimed by one sequence; who meets a page claimed already, or out of range,
+// marks both sequences, which are then left alone.  select: a CTA per (layer, sequence) finds the rows that stay, pairs
+// the holes below the new length with the kept rows behind it, and moves their positions and mass.  move: K and V rows of
+// the pairs.  Sources lie at or beyond the new length and places below it, so no order is needed between them.
+struct EvictArgs {
+    PagedDims d;
+    int L, budget, n_sink, n_recent;
+    const int32_t *block_table, *kv_len;
+    int32_t* positions;
+    float* mass;
+    int32_t *keep_idx, *new_len, *status;
+    int32_t *claim, *bad;                              // [n_pages] and [n_seqs], zeroed before the first kernel
+    int32_t *from, *to, *n_moved;                      // [L][n_seqs][budget] twice, [L][n_seqs]
+};
+
+__global__ void __launch_bounds__(256)
+evict_claim_kernel(const EvictArgs a) {
+    const int b = blockIdx.x, len = a.kv_len[b];
+    if (len < 0 || len > a.d.S_cap()) {
+        if (threadIdx.x == 0) a.bad[b] = 1;
+        return;
+    }
+    const int used = (len + (1 << a.d.page_shift) - 1) >> a.d.page_shift;
+    for (int p = threadIdx.x; p < used; p += 256) {
+        const int page = a.block_table[(size_t)b * a.d.max_pages + p];
+        if (page < 0 || page >= a.d.n_pages) {
+            a.bad[b] = 1;
+            continue;
+        }
+        const int before = atomicExch(&a.claim[page], b + 1);   // every meeting is seen by whoever comes second
+        if (before) a.bad[b] = a.bad[before - 1] = 1;
+    }
+}
+
+// Sum over the threads before this one, and over all: `total`.
+__device__ __forceinline__ int block_scan(int v, int* s_warp, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+    int incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    int w = lane < nwarps ? s_warp[lane] : 0;
+    const int mine = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xFFFFFFFFu, w, o);
+        if (lane >= o) w += x;
+    }
+    *total = __shfl_sync(0xFFFFFFFFu, w, 31);
+    const int before = __shfl_sync(0xFFFFFFFFu, w - mine, warp);
+    __syncthreads();                                   // s_warp may be written again
+    return before + incl - v;
+}
+
+// Rank key of a row: larger ranks higher.  Protected rows above everything, a NaN above every number.
+__device__ __forceinline__ uint32_t evict_key(float mass, int pos, int n_sink, long long recent_from) {
+    if (pos < n_sink || (long long)pos > recent_from) return 0xFFFFFFFFu;
+    return mass != mass ? 0xFFFFFFFEu : float_key(mass);
+}
+
+constexpr int kEvictBuckets = 2048;
+
+__global__ void __launch_bounds__(1024)
+evict_select_kernel(const EvictArgs a) {
+    grid_dep_wait();
+    __shared__ uint32_t s_hist[kEvictBuckets];
+    __shared__ int s_warp[32];
+    __shared__ uint32_t s_prefix;
+    __shared__ int s_need;
+    const int b = blockIdx.x, layer = blockIdx.y, S_cap = a.d.S_cap(), tid = threadIdx.x, nthr = blockDim.x;
+    const size_t prob = (size_t)layer * a.d.n_seqs + b;
+    const int len = a.kv_len[b], n = min(len, a.budget);
+    const bool bad = a.bad[b] != 0;
+    int32_t* keep = a.keep_idx + prob * a.budget;
+    if (layer == 0 && b == 0) {                        // the call's status
+        int any = 0;
+        for (int s = tid; s < a.d.n_seqs; s += nthr) any |= a.bad[s];
+        any = __syncthreads_or(any);
+        if (tid == 0) *a.status = any ? METOK_ERR_INVALID_ARG : METOK_OK;
+    }
+    if (layer == 0 && tid == 0) a.new_len[b] = bad ? len : n;
+    if (bad || len <= a.budget) {
+        for (int i = tid; i < a.budget; i += nthr) keep[i] = !bad && i < n ? i : -1;
+        if (tid == 0) a.n_moved[prob] = 0;
+        return;
+    }
+    int32_t* pos = a.positions + prob * S_cap;
+    float* mass = a.mass + prob * S_cap;
+    const long long recent_from = (long long)pos[len - 1] - a.n_recent;
+    auto key_of = [&](int i) { return evict_key(mass[i], pos[i], a.n_sink, recent_from); };
+
+    // the n-th highest key, digit by digit from the top
+    uint32_t prefix = 0u;                              // its digits so far
+    int need = n, done = 0;                            // rows still to take among those with these digits; bits decided
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int bits = pass < 2 ? 11 : 10, shift = 32 - done - bits;
+        for (int i = tid; i < kEvictBuckets; i += nthr) s_hist[i] = 0u;
+        __syncthreads();
+        for (int i = tid; i < len; i += nthr) {
+            const uint32_t k = key_of(i);
+            if (done == 0 || (k >> (32 - done)) == prefix) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1u)], 1u);
+        }
+        __syncthreads();
+        // buckets from the top, a run of them per thread
+        const int per = (kEvictBuckets + nthr - 1) / nthr, first = kEvictBuckets - 1 - tid * per;
+        int sum = 0, total;
+        for (int j = 0; j < per; ++j)
+            if (first - j >= 0) sum += (int)s_hist[first - j];
+        const int before = block_scan(sum, s_warp, &total);
+        if (before < need && need <= before + sum) {   // exactly one thread
+            int left = need - before;
+            for (int j = 0; j < per; ++j) {
+                const int c = (int)s_hist[first - j];
+                if (left <= c) {
+                    s_prefix = (prefix << bits) | (uint32_t)(first - j);
+                    s_need = left;
+                    break;
+                }
+                left -= c;
+            }
+        }
+        __syncthreads();
+        prefix = s_prefix;
+        need = s_need;
+        done += bits;
+        __syncthreads();
+    }
+
+    // rows in order: above the threshold, or among the first `need` equal to it, they stay
+    int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget;
+    int equal = 0, holes = 0, movers = 0;              // so far
+#pragma unroll 1
+    for (int base = 0; base < len; base += nthr) {
+        const int i = base + tid;
+        const uint32_t k = i < len ? key_of(i) : 0u;
+        const bool eq = i < len && k == prefix;
+        int total;
+        const int eq_before = equal + block_scan(eq, s_warp, &total);
+        equal += total;
+        const bool stay = i < len && (k > prefix || (eq && eq_before < need));
+        const bool hole = i < n && !stay, mover = i >= n && stay;
+        const int x = block_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), s_warp, &total);   // at most 1024 of each
+        if (hole) to[holes + (x & 0xFFFF)] = i;
+        if (mover) from[movers + (x >> 16)] = i;
+        if (stay && i < n) keep[i] = i;
+        holes += total & 0xFFFF;
+        movers += total >> 16;
+    }
+    __syncthreads();
+    for (int i = n + tid; i < a.budget; i += nthr) keep[i] = -1;
+    for (int r = tid; r < movers; r += nthr) {
+        const int src = from[r], dst = to[r];
+        keep[dst] = src;
+        pos[dst] = pos[src];
+        mass[dst] = mass[src];
+    }
+    __syncthreads();
+    for (int i = n + tid; i < len; i += nthr) mass[i] = 0.f;
+    if (tid == 0) a.n_moved[prob] = movers;
+}
+
+constexpr int kEvictPtrLayers = 64;                    // layers per launch of the move
+struct EvictPools {
+    uint4 *k[kEvictPtrLayers], *v[kEvictPtrLayers];
+};
+constexpr int kMoveThreads = 256, kMoveUnroll = 4;
+
+__global__ void __launch_bounds__(kMoveThreads)
+evict_move_kernel(const EvictArgs a, const EvictPools pools, int layer0) {
+    grid_dep_wait();
+    const int ll = blockIdx.y / a.d.n_seqs, b = blockIdx.y - ll * a.d.n_seqs;
+    const size_t prob = (size_t)(layer0 + ll) * a.d.n_seqs + b;
+    const int n = a.n_moved[prob], cpr = a.d.row_chunks, per_row = 2 * a.d.Hkv * cpr;
+    const int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget, *table = a.block_table + (size_t)b * a.d.max_pages;
+    const long long total = (long long)n * per_row;
+    for (long long g0 = (long long)blockIdx.x * (kMoveThreads * kMoveUnroll) + threadIdx.x; g0 < total;
+         g0 += (long long)gridDim.x * (kMoveThreads * kMoveUnroll)) {
+        uint4 v[kMoveUnroll];
+        uint4* dst[kMoveUnroll];
+#pragma unroll
+        for (int u = 0; u < kMoveUnroll; ++u) {
+            const long long g = g0 + u * kMoveThreads;
+            dst[u] = nullptr;
+            if (g >= total) continue;
+            const int r = (int)(g / per_row), e = (int)(g - (long long)r * per_row), hh = e / cpr, c = e - hh * cpr;
+            const int h = hh >= a.d.Hkv ? hh - a.d.Hkv : hh, s = from[r], t = to[r];
+            uint4* pool = hh >= a.d.Hkv ? pools.v[ll] : pools.k[ll];
+            dst[u] = pool + paged_chunk(a.d, table[t >> a.d.page_shift], h, t) + c;
+            v[u] = pool[paged_chunk(a.d, table[s >> a.d.page_shift], h, s) + c];
+        }
+#pragma unroll
+        for (int u = 0; u < kMoveUnroll; ++u)
+            if (dst[u]) *dst[u] = v[u];
+    }
+}
+
+}  // namespace
+}  // namespace metok
+
+using namespace metok;
+
+extern "C" int metok_paged_append(int dtype, const metok_paged_cache* c, const void* k_new, const void* v_new, int64_t k_head,
+                                  int64_t k_row, int64_t v_head, int64_t v_row, int n_new, const int32_t* new_offsets,
+                                  int32_t* positions, const int32_t* pos_new, float* mass, const float* mass_new, int32_t* new_len,
+                                  int32_t* status, void* stream) {
+    PagedDims d;
+    const int rc = paged_dims(dtype, c, &d);
+    if (rc != METOK_OK) return rc;
+    if (!c->k_pool || !c->v_pool || !c->block_table || !c->kv_len || !new_len || !status || n_new < 0) return METOK_ERR_INVALID_ARG;
+    if (n_new > 0 && (!k_new || !v_new)) return METOK_ERR_INVALID_ARG;
+    if (!aligned16(c->k_pool) || !aligned16(c->v_pool) || !aligned16(k_new) || !aligned16(v_new)) return METOK_ERR_INVALID_ARG;
+    if (!aligned4(c->block_table) || !aligned4(c->kv_len) || !aligned4(new_offsets) || !aligned4(positions) || !aligned4(pos_new) ||
+        !aligned4(mass) || !aligned4(mass_new) || !aligned4(new_len) || !aligned4(status))
+        return METOK_ERR_INVALID_ARG;
+    if ((pos_new && !positions) || (mass_new && !mass) || (!new_offsets && n_new != c->n_seqs)) return METOK_ERR_INVALID_ARG;
+    if (overlap(new_len, (size_t)c->n_seqs * 4, c->kv_len, (size_t)c->n_seqs * 4)) return METOK_ERR_INVALID_ARG;
+    const int per = 16 / (dtype == METOK_F32 ? 4 : 2);                  // elements of a chunk
+    if (k_head < 0 || v_head < 0 || k_row < c->dh || v_row < c->dh || (k_head | k_row | v_head | v_row) % per) return METOK_ERR_INVALID_ARG;
+    AppendArgs a;
+    a.d = d;
+    a.k_new = (const uint4*)k_new; a.v_new = (const uint4*)v_new;
+    a.k_pool = (uint4*)c->k_pool; a.v_pool = (uint4*)c->v_pool;
+    a.k_head = k_head / per; a.k_row = k_row / per; a.v_head = v_head / per; a.v_row = v_row / per;
+    a.n_new = n_new;
+    a.parts = ceil_div(2 * d.Hkv * d.row_chunks, 32 * kAppendChunks);
+    a.block_table = c->block_table; a.kv_len = c->kv_len; a.offsets = new_offsets; a.pos_new = pos_new;
+    a.positions = positions; a.mass = mass; a.mass_new = mass_new; a.new_len = new_len; a.status = status;
+    const long long blocks = 1 + ((long long)n_new * a.parts + kAppendWarps - 1) / kAppendWarps;
+    if (blocks > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    cudaStream_t st = (cudaStream_t)stream;
+    {
+        METOK_TIMED("paged_append", st);
+        launch_chained(paged_append_kernel, dim3((unsigned)blocks), dim3(kAppendWarps * 32), 0, st, a);
+    }
+    METOK_LAUNCH_CHECK();
+    return METOK_OK;
+}
+
+namespace {
+void evict_carve(Carver& cv, const PagedDims& d, int L, int budget, EvictArgs* a) {
+    a->claim = cv.take<int32_t>((size_t)d.n_pages + d.n_seqs);          // one piece: cleared together
+    a->bad = a->claim ? a->claim + d.n_pages : nullptr;
+    const size_t lists = (size_t)L * d.n_seqs * budget;
+    a->from = cv.take<int32_t>(lists);
+    a->to = cv.take<int32_t>(lists);
+    a->n_moved = cv.take<int32_t>((size_t)L * d.n_seqs);
+}
+}  // namespace
+
+extern "C" size_t metok_paged_evict_workspace_bytes(const metok_paged_cache* c, int L, int budget) {
+    PagedDims d;
+    if (paged_dims(METOK_F32, c, &d) != METOK_OK || L < 1 || budget < 1) return 0;
+    EvictArgs a;
+    Carver cv(nullptr);
+    evict_carve(cv, d, L, budget, &a);
+    return cv.total();
+}
+
+extern "C" int metok_paged_evict(int dtype, const metok_paged_cache* c, void* const* k_layers, void* const* v_layers, int L, int budget,
+                                 int n_sink, int n_recent, int32_t* positions, float* mass, int32_t* keep_idx, int32_t* new_len,
+                                 int32_t* status, void* ws, size_t ws_bytes, void* stream) {
+    PagedDims d;
+    const int rc = paged_dims(dtype, c, &d);
+    if (rc != METOK_OK) return rc;
+    if (!c->block_table || !c->kv_len || !k_layers || !v_layers || !positions || !mass || !keep_idx || !new_len || !status)
+        return METOK_ERR_INVALID_ARG;
+    if (L < 1 || budget < 1 || budget > d.S_cap() || n_sink < 0 || n_recent < 1) return METOK_ERR_INVALID_ARG;
+    if (!aligned4(c->block_table) || !aligned4(c->kv_len) || !aligned4(positions) || !aligned4(mass) || !aligned4(keep_idx) ||
+        !aligned4(new_len) || !aligned4(status))
+        return METOK_ERR_INVALID_ARG;
+    if (L > 1024 || (long long)L * c->n_seqs > 65535) return METOK_ERR_UNSUPPORTED;
+    for (int l = 0; l < L; ++l) {
+        if (!k_layers[l] || !v_layers[l] || !aligned16(k_layers[l]) || !aligned16(v_layers[l]) || k_layers[l] == v_layers[l]) return METOK_ERR_INVALID_ARG;
+        for (int m = 0; m < l; ++m)                                     // moved twice, a row would be lost
+            if (k_layers[l] == k_layers[m] || v_layers[l] == v_layers[m] || k_layers[l] == v_layers[m] || v_layers[l] == k_layers[m])
+                return METOK_ERR_INVALID_ARG;
+    }
+    if (overlap(new_len, (size_t)c->n_seqs * 4, c->kv_len, (size_t)c->n_seqs * 4)) return METOK_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < metok_paged_evict_workspace_bytes(c, L, budget)) return METOK_ERR_WORKSPACE;
+    EvictArgs a;
+    a.d = d;
+    a.L = L; a.budget = budget; a.n_sink = n_sink; a.n_recent = n_recent;
+    a.block_table = c->block_table; a.kv_len = c->kv_len; a.positions = positions; a.mass = mass;
+    a.keep_idx = keep_idx; a.new_len = new_len; a.status = status;
+    Carver cv(ws);
+    evict_carve(cv, d, L, budget, &a);
+    cudaStream_t st = (cudaStream_t)stream;
+    METOK_CUDA_TRY(cudaMemsetAsync(a.claim, 0, ((size_t)d.n_pages + d.n_seqs) * sizeof(int32_t), st));
+    {
+        METOK_TIMED("evict_claim", st);
+        evict_claim_kernel<<<d.n_seqs, 256, 0, st>>>(a);
+    }
+    METOK_LAUNCH_CHECK();
+    {
+        METOK_TIMED("evict_select", st);
+        const int threads = std::min(1024, std::max(128, ceil_div(d.S_cap(), 32) * 32));
+        launch_chained(evict_select_kernel, dim3(d.n_seqs, L), dim3(threads), 0, st, a);
+    }
+    METOK_LAUNCH_CHECK();
+    // pairs of a problem: at most the rows behind the new length, and the places below it
+    const long long most = (long long)std::min(budget, d.S_cap() - budget) * 2 * d.Hkv * d.row_chunks;
+    const long long blocks = std::max(1LL, std::min((most + kMoveThreads * kMoveUnroll - 1) / (kMoveThreads * kMoveUnroll),
+                                                    (long long)ceil_div(kNumSMs * 8, L * d.n_seqs)));
+    for (int l0 = 0; l0 < L; l0 += kEvictPtrLayers) {
+        const int nl = std::min(kEvictPtrLayers, L - l0);
+        EvictPools pools = {};
+        for (int l = 0; l < nl; ++l) {
+            pools.k[l] = (uint4*)k_layers[l0 + l];
+            pools.v[l] = (uint4*)v_layers[l0 + l];
+        }
+        METOK_TIMED("evict_move", st);
+        launch_chained(evict_move_kernel, dim3((unsigned)blocks, nl * d.n_seqs), dim3(kMoveThreads), 0, st, a, pools, l0);
+        METOK_LAUNCH_CHECK();
+    }
+    return METOK_OK;
+}
