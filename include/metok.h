@@ -410,6 +410,72 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
                      void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------- *
+ * (5) Attention of a prompt's rows -- the attention of Eq. 2 and 3 over what the
+ *     compression has left (the rows of metok_prefill_prune's hidden_out, the
+ *     caches of metok_kv_compact), for the layers between the pruning levels.
+ *
+ *   Documents s = 0 .. n_seq-1 are packed: queries seq_q[s] .. seq_q[s+1]-1 and
+ *   keys seq_k[s] .. seq_k[s+1]-1 (Lq and Lk of them) belong to document s and see
+ *   nothing of the others.  The queries are the document's LAST rows: query i
+ *   (0-based in its document) sits at key c = Lk - Lq + i.  It sees key j if
+ *     causal == 0,  or  j <= c,  or  j < prefix_len[s]   (the video as a prefix).
+ *   For the keys that it sees
+ *     x_j = softmax_scale * <q, k_j>
+ *     x_j = softcap * tanh(x_j / softcap)                 if softcap > 0
+ *     x_j = x_j - slopes[h] * |pos[c] - pos[j]|           if slopes
+ *     out = sum_j softmax(x)_j v_j,   lse = ln sum_j exp(x_j).
+ *   pos is `positions` (the rows' original positions: pruning leaves gaps), or the
+ *   row's index in its document if NULL.  A query that sees no key (Lk < Lq, or
+ *   Lk = 0) gets out = 0 and lse = -infinity; one that sits before the first key
+ *   (Lk < Lq) but sees keys (prefix, or not causal) has the first key's position.
+ *   Query head h reads K/V head h / (Hq / Hkv).
+ *
+ *   Rows: q [Hq][n_q][dh], k and v [Hkv][n_k][dh], out [Hq][n_q][dh] with the
+ *   given strides in ELEMENTS between heads and between rows (so token-major
+ *   projections and caches with room behind their rows need no copy); elements of
+ *   a row are contiguous.  DEVICE, 16-byte aligned; strides are multiples of 16
+ *   bytes, row strides >= dh; rows of `out` do not overlap, and out overlaps no input.
+ *   seq_q, seq_k DEVICE int32 [n_seq+1], prefix_len DEVICE int32 [n_seq], positions
+ *   DEVICE int32 [n_k], slopes DEVICE float [Hq], lse DEVICE float [Hq][n_q]: 4-byte
+ *   aligned; all but q, k, v, out may be NULL.  seq_q and seq_k are both NULL for one
+ *   document of all rows (n_seq = 1).  Positions lie in [0, 2^24).
+ *   Rows of q, k, v, out and lse outside every document are neither used nor written,
+ *   whatever they hold.  Inside a document v has to be finite: a row that a query does
+ *   not see counts with weight 0.
+ *   status DEVICE int32: written METOK_OK; METOK_ERR_INVALID_ARG if seq_q or seq_k
+ *   descends or leaves [0, n_q] / [0, n_k] (then no row is written); METOK_ERR_TIMEOUT.
+ *
+ *   bf16: products on the tensor cores; logits, softmax statistics and sums in
+ *   fp32; the unnormalised weights are rounded to bf16 for the product with V.
+ *   fp32: fp32 throughout.
+ *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1 (n_q, n_k may be 0),
+ *   Hq % Hkv, strides, softmax_scale not finite or <= 0, softcap < 0 or not finite, one of
+ *   seq_q / seq_k without the other, n_seq != 1 without them); UNSUPPORTED (dh other
+ *   than 64 or 128, more than 2^24 rows, n_seq > 65536, Hq > 65535, more than 2^31 - 1 pieces of work);
+ *   WORKSPACE.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    void* out;
+    float* lse;
+    int64_t q_head, q_row, k_head, k_row, v_head, v_row, out_head, out_row;
+    int Hq, Hkv, dh, n_q, n_k, n_seq;
+    const int32_t* seq_q;
+    const int32_t* seq_k;
+    const int32_t* prefix_len;
+    const int32_t* positions;
+    const float* slopes;
+    float softmax_scale, softcap;
+    int causal;
+} metok_attention_params;
+
+METOK_API size_t metok_prefill_attention_workspace_bytes(int dtype, const metok_attention_params* p);
+METOK_API int metok_prefill_attention(int dtype, const metok_attention_params* p, int32_t* status,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- *
  * (6) A paged K/V cache: the append that fills it.
  *
  *   One layer's cache is two pools of pages, [n_pages][Hkv][page_size][dh] of

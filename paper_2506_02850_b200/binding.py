@@ -54,6 +54,14 @@ class MetokError(RuntimeError):
         super().__init__(f"{fn} failed: {status} {text}{extra}")
 
 
+class AttentionParams(_c.Structure):
+    _fields_ = ([(n, _vp) for n in ("q", "k", "v", "out", "lse")] +
+                [(n, _i64) for n in ("q_head", "q_row", "k_head", "k_row", "v_head", "v_row", "out_head", "out_row")] +
+                [(n, _i) for n in ("Hq", "Hkv", "dh", "n_q", "n_k", "n_seq")] +
+                [(n, _vp) for n in ("seq_q", "seq_k", "prefix_len", "positions", "slopes")] +
+                [("softmax_scale", _f), ("softcap", _f), ("causal", _i)])
+
+
 class PagedCache(_c.Structure):
     _fields_ = [("k_pool", _vp), ("v_pool", _vp), ("block_table", _vp), ("kv_len", _vp), ("n_pages", _i), ("Hkv", _i), ("page_size", _i),
                 ("dh", _i), ("n_seqs", _i), ("max_pages", _i)]
@@ -86,6 +94,8 @@ _SIGNATURES = {
     "metok_kv_compact_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "metok_kv_compact": (_i, [_c.POINTER(_vp), _c.POINTER(_vp), _i, _i, _i, _i, _i, _i, _i, _i, _d, _i, _i,
                               _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "metok_prefill_attention_workspace_bytes": (_sz, [_i, _c.POINTER(AttentionParams)]),
+    "metok_prefill_attention": (_i, [_i, _c.POINTER(AttentionParams), _vp, _vp, _sz, _vp]),
     "metok_paged_append": (_i, [_i, _c.POINTER(PagedCache), _vp, _vp, _i64, _i64, _i64, _i64, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "metok_paged_attention_workspace_bytes": (_sz, [_i, _c.POINTER(PagedCache), _i, _i]),
     "metok_paged_attention": (_i, [_i, _c.POINTER(PagedCache), _vp, _i64, _i64, _i, _f, _f, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp,
@@ -399,6 +409,21 @@ def metok_kv_compact(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch.
                               new_len)
     if type(res) is int:
         _check("metok_kv_compact", res)
+    return res
+
+
+def metok_prefill_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scale: float, seq_q: Optional[torch.Tensor] = None,
+                            seq_k: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None, causal: bool = True,
+                            softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                            with_lse: bool = False, out: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Attention of a prompt's rows: `q` [Hq, n_q, dh] over `k`, `v` [Hkv, n_k, dh] (any strides between heads and rows).  `seq_q` and
+    `seq_k` (int32 [documents + 1]) pack several documents, whose queries are their last rows; `prefix_len` (int32 [documents]) keys of
+    each are seen by all of its queries; `slopes` (float [Hq]) take slope * distance off the logits, distances going by `positions`
+    (int32 [n_k], default: the row's index).  Returns "out", "lse" (`with_lse`) and "status" (0, -1 if the offsets descend or
+    leave the rows, or -5 after a device-side timeout)."""
+    res = _calls().prefill_attention(q, k, v, softmax_scale, seq_q, seq_k, prefix_len, causal, softcap, slopes, positions, with_lse, out)
+    if type(res) is int:
+        _check("metok_prefill_attention", res)
     return res
 
 

@@ -35,6 +35,7 @@ namespace {
     X(metok_prefill_prune_workspace_bytes) X(metok_prefill_prune)                                        \
     X(metok_retention_budgets) X(metok_prune_schedule_sizes) X(metok_prefill_prune_schedule_workspace_bytes)                        \
     X(metok_prefill_prune_schedule) X(metok_kv_compact_workspace_bytes) X(metok_kv_compact)               \
+    X(metok_prefill_attention_workspace_bytes) X(metok_prefill_attention)                                \
     X(metok_paged_append) X(metok_paged_attention_workspace_bytes) X(metok_paged_attention)              \
     X(metok_paged_evict_workspace_bytes) X(metok_paged_evict)
 struct Api {
@@ -637,6 +638,58 @@ int size_of(const at::Tensor& t, int dim, const char* name) {
     return (int)t.size(dim);
 }
 
+// q, k, v, softmax_scale, seq_q, seq_k, prefix_len, causal, softcap, slopes, positions, with_lse, out
+PyObject* prefill_attention(PyObject* const* a, Py_ssize_t n) {
+    want(n, 13);
+    const at::Tensor& q = first_tensor(a[0], "q");
+    const at::Device dev = q.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    const at::ScalarType dt = q.scalar_type();
+    rows3(a[0], "q", dev, dt);
+    const at::Tensor &k = rows3(a[1], "k", dev, dt), &v = rows3(a[2], "v", dev, dt);
+    if (k.sizes() != v.sizes() || k.size(2) != q.size(2)) fail(PyExc_ValueError, "%s must be [Hkv, n_k, dh], q [Hq, n_q, dh]", "k, v");
+    metok_attention_params p = {};
+    p.Hq = size_of(q, 0, "q"); p.n_q = size_of(q, 1, "q"); p.dh = size_of(q, 2, "q");
+    p.Hkv = size_of(k, 0, "k"); p.n_k = size_of(k, 1, "k");
+    const at::Tensor seq_q = array(a[4], "seq_q", dev, at::kInt, -1), seq_k = array(a[5], "seq_k", dev, at::kInt, -1);
+    if (seq_q.defined() != seq_k.defined()) fail(PyExc_ValueError, "%s: both or neither", "seq_q, seq_k");
+    p.n_seq = 1;
+    if (seq_q.defined()) {
+        if (seq_q.numel() < 2 || seq_q.numel() != seq_k.numel()) fail(PyExc_ValueError, "%s must be int32 [documents + 1]", "seq_q, seq_k");
+        if (seq_q.numel() > 0x7FFFFFFF) fail(PyExc_ValueError, "%s is too large", "seq_q");
+        p.n_seq = (int)seq_q.numel() - 1;
+    }
+    const at::Tensor prefix = array(a[6], "prefix_len", dev, at::kInt, p.n_seq), slopes = array(a[9], "slopes", dev, at::kFloat, p.Hq),
+                     pos = array(a[10], "positions", dev, at::kInt, p.n_k);
+    const int causal = PyObject_IsTrue(a[7]), with_lse = PyObject_IsTrue(a[11]);
+    if (causal < 0 || with_lse < 0) throw PyError();
+    const at::Tensor out = a[12] == Py_None ? empty(q.sizes(), dt, dev) : rows3(a[12], "out", dev, dt);
+    if (out.sizes() != q.sizes()) fail(PyExc_ValueError, "%s must have the shape of q", "out");
+    at::Tensor lse;
+    if (with_lse) lse = empty({p.Hq, p.n_q}, at::kFloat, dev);
+    const at::Tensor status = empty_i32(1, dev);
+    p.q = q.data_ptr(); p.k = k.data_ptr(); p.v = v.data_ptr(); p.out = out.data_ptr(); p.lse = ptr_or_null<float>(lse);
+    p.q_head = step(q, 0, 0); p.q_row = step(q, 1, p.dh); p.k_head = step(k, 0, 0); p.k_row = step(k, 1, p.dh);
+    p.v_head = step(v, 0, 0); p.v_row = step(v, 1, p.dh); p.out_head = step(out, 0, 0); p.out_row = step(out, 1, p.dh);
+    p.seq_q = ptr_or_null<const int32_t>(seq_q); p.seq_k = ptr_or_null<const int32_t>(seq_k);
+    p.prefix_len = ptr_or_null<const int32_t>(prefix); p.positions = ptr_or_null<const int32_t>(pos);
+    p.slopes = ptr_or_null<const float>(slopes);
+    p.softmax_scale = (float)number(a[3]); p.softcap = (float)number(a[8]); p.causal = causal;
+    const int code = dtype_code(q);
+    const size_t need = api.metok_prefill_attention_workspace_bytes(code, &p);
+    at::Tensor ws;
+    if (need > 0) ws = empty({(int64_t)need}, at::kByte, dev);
+    const int st = api.metok_prefill_attention(code, &p, (int32_t*)status.data_ptr(), ptr_or_null<void>(ws), need, current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.out, out);
+    if (with_lse) put(res.p, names.lse, lse);
+    put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
 // The pools of one layer, the table and the lengths; `hold` keeps the last two.
 metok_paged_cache paged_cache(const at::Tensor& k, PyObject* v_obj, PyObject* table_obj, PyObject* len_obj, at::Tensor* hold) {
     const at::Device dev = k.device();
@@ -792,6 +845,7 @@ PyMethodDef methods[] = {
     FAST("prefill_prune", prefill_prune),
     FAST("prefill_prune_schedule", prefill_prune_schedule),
     FAST("kv_compact", kv_compact),
+    FAST("prefill_attention", prefill_attention),
     FAST("paged_append", paged_append),
     FAST("paged_attention", paged_attention),
     FAST("paged_evict", paged_evict),

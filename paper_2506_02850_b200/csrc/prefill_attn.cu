@@ -1,0 +1,309 @@
+// metok_prefill_attention: the C entry, the kernel on the CUDA cores, and the join of split keys.
+//
+// CUDA cores: a CTA of 256 threads takes 64 query rows of a head and walks their keys in tiles of 64.  Thread (ty, tx)
+// holds the logits of rows 4 ty + i and keys tx + 16 j, and the outputs of the same rows; a row's running maximum and
+// sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling from row to
+// row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
+#include <algorithm>
+
+#include "launchers.h"
+#include "prefill_attn.cuh"
+#include "sm100.cuh"
+
+namespace metok {
+
+namespace {
+
+constexpr int kSM = 64, kSN = 64, kSThreads = 256;
+
+template <typename T, int DH>
+struct SimtAttnSmem {
+    float q[kSM][DH + 4], k[kSN][DH + 4], v[kSN][DH], p[kSM][kSN + 4];
+    float pos[kSN];
+};
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(kSThreads)
+prompt_attn_simt_kernel(const PromptArgs a) {
+    grid_dep_wait();
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    SimtAttnSmem<T, DH>& sm = *reinterpret_cast<SimtAttnSmem<T, DH>*>(smem_raw);
+    const int h = blockIdx.x % a.Hq, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hq, [](int Lq) { return (Lq + kSM - 1) / kSM; });
+    if (d.tile < 0) return;
+    const int i0 = d.tile * kSM, rows = min(kSM, d.Lq - i0), g = h / a.G;
+    const int first_keys = prompt_keys(a, d, i0), all_keys = prompt_keys(a, d, i0 + rows - 1);
+    const int nt = (all_keys + kSN - 1) / kSN, t_lo = (int)((long long)nt * blockIdx.y / a.splits), t_hi = (int)((long long)nt * (blockIdx.y + 1) / a.splits);
+    const T* q = reinterpret_cast<const T*>(a.q) + h * a.q_head + (long long)(d.q0 + i0) * a.q_row;
+    const T* k = reinterpret_cast<const T*>(a.k) + g * a.k_head + (long long)d.k0 * a.k_row;
+    const T* v = reinterpret_cast<const T*>(a.v) + g * a.v_head + (long long)d.k0 * a.v_row;
+    constexpr int VE = Vec16<T>::N, CPR = DH / VE;     // elements of a 16-byte piece, pieces of a row
+    for (int c = tid; c < kSM * CPR; c += kSThreads) {
+        const int r = c / CPR, e = (c - r * CPR) * VE;
+        float x[VE];
+        if (r < rows) Vec16<T>::load(q + (long long)r * a.q_row + e, x);
+        else Vec16<T>::zero(x);
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) *reinterpret_cast<float4*>(&sm.q[r][e + i]) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    }
+    int keys[4];
+    float my_pos[4], m[4], l[4], o[4][DH / 16];
+    const float slope = a.slopes ? a.slopes[h] * kAttnLog2e : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i0 + ty * 4 + i;
+        keys[i] = ty * 4 + i < rows ? prompt_keys(a, d, r) : 0;
+        my_pos[i] = a.slopes ? prompt_position(a, d, d.Lk - d.Lq + r) : 0.f;
+        m[i] = __int_as_float(0xFF800000);
+        l[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DH / 16; ++c) o[i][c] = 0.f;
+    }
+    for (int t = t_lo; t < t_hi; ++t) {
+        const int j0 = t * kSN;
+        __syncthreads();
+        for (int c = tid; c < kSN * CPR; c += kSThreads) {
+            const int r = c / CPR, e = (c - r * CPR) * VE;
+            float x[VE], y[VE];
+            if (j0 + r < d.Lk) {
+                Vec16<T>::load(k + (long long)(j0 + r) * a.k_row + e, x);
+                Vec16<T>::load(v + (long long)(j0 + r) * a.v_row + e, y);
+            } else {
+                Vec16<T>::zero(x);
+                Vec16<T>::zero(y);
+            }
+#pragma unroll
+            for (int i = 0; i < VE; i += 4) {
+                *reinterpret_cast<float4*>(&sm.k[r][e + i]) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                *reinterpret_cast<float4*>(&sm.v[r][e + i]) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+            }
+        }
+        if (a.slopes && tid < kSN) sm.pos[tid] = prompt_position(a, d, j0 + tid);
+        __syncthreads();
+        float s[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+        for (int e = 0; e < DH; e += 4) {
+            float4 x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(&sm.q[ty * 4 + i][e]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][e]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
+        }
+        const bool masked = j0 + kSN > first_keys || rows < kSM;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float top = m[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(s[i][j] * a.cap_scale) : s[i][j] * a.scale_log2;
+                if (a.slopes) x = fmaf(-slope, fabsf(my_pos[i] - sm.pos[tx + 16 * j]), x);
+                if (masked && j0 + tx + 16 * j >= keys[i]) x = __int_as_float(0xFF800000);
+                s[i][j] = x;
+                top = fmaxf(top, x);
+            }
+#pragma unroll
+            for (int w = 8; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
+            const float base = top == __int_as_float(0xFF800000) ? 0.f : top;    // no key so far: weights of 0, not of inf - inf
+            const float f = exp2f(m[i] - base);
+            m[i] = top;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[i][j] = exp2f(s[i][j] - base);
+                sum += s[i][j];
+                sm.p[ty * 4 + i][tx + 16 * j] = s[i][j];
+            }
+            l[i] = l[i] * f + sum;
+#pragma unroll
+            for (int c = 0; c < DH / 16; ++c) o[i][c] *= f;
+        }
+        __syncwarp();                                  // a row's weights are written and read by one half of a warp
+#pragma unroll 2
+        for (int j = 0; j < kSN; j += 4) {
+            float4 p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.p[ty * 4 + i][j]);
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+                for (int c = 0; c < DH / 64; ++c) {
+                    const float4 x = *reinterpret_cast<const float4*>(&sm.v[j + jj][tx * 4 + 64 * c]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float w = jj == 0 ? p[i].x : jj == 1 ? p[i].y : jj == 2 ? p[i].z : p[i].w;
+                        o[i][4 * c] = fmaf(w, x.x, o[i][4 * c]);
+                        o[i][4 * c + 1] = fmaf(w, x.y, o[i][4 * c + 1]);
+                        o[i][4 * c + 2] = fmaf(w, x.z, o[i][4 * c + 2]);
+                        o[i][4 * c + 3] = fmaf(w, x.w, o[i][4 * c + 3]);
+                    }
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int w = 8; w >= 1; w >>= 1) l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], w);
+        const int r = ty * 4 + i;
+        if (r >= rows) continue;
+        const long long row = d.q0 + i0 + r;
+        if (a.splits > 1) {
+            const long long at = ((long long)blockIdx.y * a.Hq + h) * a.n_q + row;
+#pragma unroll
+            for (int c = 0; c < DH / 64; ++c)
+                *reinterpret_cast<float4*>(a.part_o + at * DH + tx * 4 + 64 * c) = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+            if (tx == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m[i], l[i]);
+            continue;
+        }
+        const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
+        T* out = reinterpret_cast<T*>(a.out) + h * a.out_head + row * a.out_row;
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) from_float(out[tx * 4 + 64 * c + e], o[i][4 * c + e] * inv);
+        if (tx == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (m[i] + log2f(l[i]));
+    }
+}
+
+// Joins the parts of split keys: a warp per row of a head.
+constexpr int kJoinWarps = 8;
+template <typename T, int DH>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+prompt_join_kernel(const PromptArgs a) {
+    grid_dep_wait();
+    if (*a.status != METOK_OK) return;                 // offsets out of order: no row is anybody's
+    const int lane = threadIdx.x & 31, h = blockIdx.y;
+    const long long row = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+    const int lo = a.seq_q ? a.seq_q[0] : 0, hi = a.seq_q ? a.seq_q[a.n_seq] : a.n_q;
+    if (row < lo || row >= hi) return;
+    float M = __int_as_float(0xFF800000);
+    for (int s = lane; s < a.splits; s += 32) M = fmaxf(M, a.part_ml[(((long long)s * a.Hq + h) * a.n_q + row) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+    constexpr int E = DH / 32;
+    float acc[E], L = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const long long at = ((long long)s * a.Hq + h) * a.n_q + row;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+        if (!(ml.y > 0.f)) continue;                   // a part of no keys has written no output
+        const float f = exp2f(ml.x - M);
+        L += f * ml.y;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += f * a.part_o[at * DH + lane * E + e];
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    T* out = reinterpret_cast<T*>(a.out) + h * a.out_head + row * a.out_row;
+#pragma unroll
+    for (int e = 0; e < E; ++e) from_float(out[lane * E + e], acc[e] * inv);
+    if (lane == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (M + log2f(L));
+}
+
+struct PromptPlan {
+    long long ctas;                                    // without splits
+    int splits;
+};
+// Tiles of all documents: at most a started one more per document than whole ones fit into n_q.
+PromptPlan prompt_plan(const metok_attention_params* p) {
+    PromptPlan pl;
+    const long long tiles = (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q);
+    pl.ctas = std::max(1LL, tiles) * p->Hq;
+    // few rows: the keys are cut until the SMs have two CTAs each, but no part shorter than four tiles
+    const long long most = std::max(1, p->n_k / (4 * kSN)), want = 2 * kNumSMs / pl.ctas;
+    pl.splits = (int)std::max(1LL, std::min({most, want, 64LL}));
+    return pl;
+}
+void prompt_carve(Carver& cv, const metok_attention_params* p, int splits, PromptArgs* a) {
+    if (splits == 1) return;
+    const size_t rows = (size_t)splits * p->Hq * p->n_q;
+    a->part_o = cv.take<float>(rows * p->dh);
+    a->part_ml = cv.take<float>(rows * 2);
+}
+
+template <typename T, int DH>
+int launch_prompt(const PromptArgs& a, const PromptPlan& pl, cudaStream_t st) {
+    auto kern = prompt_attn_simt_kernel<T, DH>;
+    METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<T, DH>));
+    {
+        METOK_TIMED("prompt_attn_simt", st);
+        launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<T, DH>), st, a);
+    }
+    METOK_LAUNCH_CHECK();
+    if (pl.splits > 1) {
+        METOK_TIMED("prompt_join", st);
+        launch_chained(prompt_join_kernel<T, DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
+        METOK_LAUNCH_CHECK();
+    }
+    return METOK_OK;
+}
+
+int prompt_check(int dtype, const metok_attention_params* p) {
+    if (!p || (dtype != METOK_F32 && dtype != METOK_BF16)) return METOK_ERR_INVALID_ARG;
+    if (p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv || p->dh < 1 || p->n_q < 0 || p->n_k < 0 || p->n_seq < 1) return METOK_ERR_INVALID_ARG;
+    if (!p->seq_q != !p->seq_k || (!p->seq_q && p->n_seq != 1)) return METOK_ERR_INVALID_ARG;
+    if (p->dh != 64 && p->dh != 128) return METOK_ERR_UNSUPPORTED;
+    if (p->n_q > (1 << 24) || p->n_k > (1 << 24) || p->n_seq > 65536 || p->Hq > 65535) return METOK_ERR_UNSUPPORTED;
+    if (prompt_plan(p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    return METOK_OK;
+}
+
+}  // namespace
+}  // namespace metok
+
+using namespace metok;
+
+extern "C" size_t metok_prefill_attention_workspace_bytes(int dtype, const metok_attention_params* p) {
+    if (prompt_check(dtype, p) != METOK_OK) return 0;
+    PromptArgs a;
+    Carver cv(nullptr);
+    prompt_carve(cv, p, prompt_plan(p).splits, &a);
+    return cv.total();
+}
+
+extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* p, int32_t* status, void* ws, size_t ws_bytes, void* stream) {
+    int rc = prompt_check(dtype, p);
+    if (rc != METOK_OK) return rc;
+    if ((p->n_q > 0 && (!p->q || !p->out)) || (p->n_k > 0 && (!p->k || !p->v)) || !status) return METOK_ERR_INVALID_ARG;
+    auto aligned4 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; };
+    if (!aligned16(p->q) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->out)) return METOK_ERR_INVALID_ARG;
+    if (!aligned4(p->lse) || !aligned4(p->seq_q) || !aligned4(p->seq_k) || !aligned4(p->prefix_len) || !aligned4(p->positions) ||
+        !aligned4(p->slopes) || !aligned4(status))
+        return METOK_ERR_INVALID_ARG;
+    const int per = 16 / (dtype == METOK_F32 ? 4 : 2);
+    if (p->q_head < 0 || p->k_head < 0 || p->v_head < 0 || p->out_head < 0) return METOK_ERR_INVALID_ARG;
+    if (p->q_row < p->dh || p->k_row < p->dh || p->v_row < p->dh || p->out_row < p->dh) return METOK_ERR_INVALID_ARG;
+    if (p->Hq > 1 && p->out_head < p->dh) return METOK_ERR_INVALID_ARG;
+    if ((p->q_head | p->k_head | p->v_head | p->out_head | p->q_row | p->k_row | p->v_row | p->out_row) % per) return METOK_ERR_INVALID_ARG;
+    if (!(p->softmax_scale > 0.f) || !(p->softmax_scale < 3.0e38f) || !(p->softcap >= 0.f) || !(p->softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
+    const size_t need = metok_prefill_attention_workspace_bytes(dtype, p);
+    if (need > 0 && (!ws || !aligned16(ws) || ws_bytes < need)) return METOK_ERR_WORKSPACE;
+    const PromptPlan pl = prompt_plan(p);
+    PromptArgs a = {};
+    a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out; a.lse = p->lse;
+    a.q_head = p->q_head; a.q_row = p->q_row; a.k_head = p->k_head; a.k_row = p->k_row;
+    a.v_head = p->v_head; a.v_row = p->v_row; a.out_head = p->out_head; a.out_row = p->out_row;
+    a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.n_q = p->n_q; a.n_k = p->n_k; a.n_seq = p->n_seq;
+    a.seq_q = p->seq_q; a.seq_k = p->seq_k; a.prefix_len = p->prefix_len; a.positions = p->positions; a.slopes = p->slopes;
+    a.scale_log2 = p->softmax_scale * kAttnLog2e;
+    a.cap_scale = p->softcap > 0.f ? p->softmax_scale / p->softcap : 0.f;
+    a.cap_log2 = p->softcap * kAttnLog2e;
+    a.causal = p->causal != 0;
+    a.splits = pl.splits;
+    a.status = status;
+    Carver cv(ws);
+    prompt_carve(cv, p, pl.splits, &a);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == METOK_BF16)
+        return p->dh == 64 ? launch_prompt<__nv_bfloat16, 64>(a, pl, st) : launch_prompt<__nv_bfloat16, 128>(a, pl, st);
+    return p->dh == 64 ? launch_prompt<float, 64>(a, pl, st) : launch_prompt<float, 128>(a, pl, st);
+}
