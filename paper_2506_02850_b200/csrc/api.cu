@@ -85,7 +85,8 @@ KernelTimer::~KernelTimer() {
 }  // namespace metok
 
 namespace metok {
-int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+namespace {
+int encode_tmap(CUtensorMap* out, int dtype, const void* base, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -97,12 +98,8 @@ int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows,
         if (!fn || q != cudaDriverEntryPointSuccess) return METOK_ERR_UNSUPPORTED;
         encode = reinterpret_cast<EncodeFn>(fn);
     }
-    const cuuint32_t esize = dtype == METOK_F32 ? 4 : 2;
-    const cuuint64_t dims[2] = {cols, rows};
-    const cuuint64_t strides[1] = {cols * esize};             // bytes between rows
-    const cuuint32_t box[2] = {128 / esize, box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = encode(out, dtype == METOK_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = encode(out, dtype == METOK_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank,
                               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -110,6 +107,21 @@ int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows,
         return METOK_ERR_CUDA;
     }
     return METOK_OK;
+}
+}  // namespace
+int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+    const cuuint32_t esize = dtype == METOK_F32 ? 4 : 2;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {cols * esize};             // bytes between rows
+    const cuuint32_t box[2] = {128 / esize, box_rows};
+    return encode_tmap(out, dtype, base, 2, dims, strides, box);
+}
+int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t row_stride, uint64_t head_stride,
+                    uint32_t box_rows) {
+    const cuuint64_t dims[3] = {cols, rows, heads};
+    const cuuint64_t strides[2] = {row_stride * 2, (heads > 1 ? head_stride : row_stride) * 2};
+    const cuuint32_t box[3] = {64, box_rows, 1};
+    return encode_tmap(out, METOK_BF16, base, 3, dims, strides, box);
 }
 int make_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
     return make_tmap_rows(out, METOK_BF16, base, rows, cols, box_rows);

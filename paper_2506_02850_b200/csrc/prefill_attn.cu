@@ -1,6 +1,6 @@
-// metok_prefill_attention: the C entry, the kernel on the CUDA cores, and the join of split keys.
+// metok_prefill_attention: the C entry, the fp32 kernel, and the join of split keys.  (bf16: prefill_attn_mma.cu.)
 //
-// CUDA cores: a CTA of 256 threads takes 64 query rows of a head and walks their keys in tiles of 64.  Thread (ty, tx)
+// fp32, on the CUDA cores: a CTA of 256 threads takes 64 query rows of a head and walks their keys in tiles of 64.  Thread (ty, tx)
 // holds the logits of rows 4 ty + i and keys tx + 16 j, and the outputs of the same rows; a row's running maximum and
 // sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling from row to
 // row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
@@ -16,18 +16,19 @@ namespace {
 
 constexpr int kSM = 64, kSN = 64, kSThreads = 256;
 
-template <typename T, int DH>
+template <int DH>
 struct SimtAttnSmem {
     float q[kSM][DH + 4], k[kSN][DH + 4], v[kSN][DH], p[kSM][kSN + 4];
     float pos[kSN];
 };
 
-template <typename T, int DH>
+template <int DH>
 __global__ void __launch_bounds__(kSThreads)
 prompt_attn_simt_kernel(const PromptArgs a) {
+    using T = float;
     grid_dep_wait();
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    SimtAttnSmem<T, DH>& sm = *reinterpret_cast<SimtAttnSmem<T, DH>*>(smem_raw);
+    SimtAttnSmem<DH>& sm = *reinterpret_cast<SimtAttnSmem<DH>*>(smem_raw);
     const int h = blockIdx.x % a.Hq, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hq, [](int Lq) { return (Lq + kSM - 1) / kSM; });
     if (d.tile < 0) return;
@@ -213,14 +214,21 @@ struct PromptPlan {
     long long ctas;                                    // without splits
     int splits;
 };
-// Tiles of all documents: at most a started one more per document than whole ones fit into n_q.
-PromptPlan prompt_plan(const metok_attention_params* p) {
+// CUDA cores: tiles of all documents, at most a started one more per document than whole ones fit into n_q.
+PromptPlan prompt_plan(int dtype, const metok_attention_params* p) {
     PromptPlan pl;
-    const long long tiles = (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q);
-    pl.ctas = std::max(1LL, tiles) * p->Hq;
-    // few rows: the keys are cut until the SMs have two CTAs each, but no part shorter than four tiles
-    const long long most = std::max(1, p->n_k / (4 * kSN)), want = 2 * kNumSMs / pl.ctas;
-    pl.splits = (int)std::max(1LL, std::min({most, want, 64LL}));
+    long long room, part;                              // CTAs that run at once; fewest keys of a part
+    if (dtype == METOK_BF16) {
+        pl.ctas = prompt_mma_ctas(p->Hkv, p->Hq / p->Hkv, p->n_q, p->n_seq);
+        room = kNumSMs;
+        part = 256;
+    } else {
+        pl.ctas = std::max(1LL, (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q)) * p->Hq;
+        room = 2 * kNumSMs;
+        part = 4 * kSN;
+    }
+    // few rows: the keys are cut until every SM has work
+    pl.splits = (int)std::max(1LL, std::min({p->n_k / part, room / pl.ctas, 64LL}));
     return pl;
 }
 void prompt_carve(Carver& cv, const metok_attention_params* p, int splits, PromptArgs* a) {
@@ -232,13 +240,16 @@ void prompt_carve(Carver& cv, const metok_attention_params* p, int splits, Promp
 
 template <typename T, int DH>
 int launch_prompt(const PromptArgs& a, const PromptPlan& pl, cudaStream_t st) {
-    auto kern = prompt_attn_simt_kernel<T, DH>;
-    METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<T, DH>));
-    {
+    if constexpr (sizeof(T) == 2) {
+        const int rc = launch_prompt_attn_mma(a, DH, pl.ctas, st);
+        if (rc != METOK_OK) return rc;
+    } else {
+        auto kern = prompt_attn_simt_kernel<DH>;
+        METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<DH>));
         METOK_TIMED("prompt_attn_simt", st);
-        launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<T, DH>), st, a);
+        launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<DH>), st, a);
+        METOK_LAUNCH_CHECK();
     }
-    METOK_LAUNCH_CHECK();
     if (pl.splits > 1) {
         METOK_TIMED("prompt_join", st);
         launch_chained(prompt_join_kernel<T, DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
@@ -253,7 +264,7 @@ int prompt_check(int dtype, const metok_attention_params* p) {
     if (!p->seq_q != !p->seq_k || (!p->seq_q && p->n_seq != 1)) return METOK_ERR_INVALID_ARG;
     if (p->dh != 64 && p->dh != 128) return METOK_ERR_UNSUPPORTED;
     if (p->n_q > (1 << 24) || p->n_k > (1 << 24) || p->n_seq > 65536 || p->Hq > 65535) return METOK_ERR_UNSUPPORTED;
-    if (prompt_plan(p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    if (prompt_plan(dtype, p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     return METOK_OK;
 }
 
@@ -266,7 +277,7 @@ extern "C" size_t metok_prefill_attention_workspace_bytes(int dtype, const metok
     if (prompt_check(dtype, p) != METOK_OK) return 0;
     PromptArgs a;
     Carver cv(nullptr);
-    prompt_carve(cv, p, prompt_plan(p).splits, &a);
+    prompt_carve(cv, p, prompt_plan(dtype, p).splits, &a);
     return cv.total();
 }
 
@@ -287,7 +298,7 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     if (!(p->softmax_scale > 0.f) || !(p->softmax_scale < 3.0e38f) || !(p->softcap >= 0.f) || !(p->softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
     const size_t need = metok_prefill_attention_workspace_bytes(dtype, p);
     if (need > 0 && (!ws || !aligned16(ws) || ws_bytes < need)) return METOK_ERR_WORKSPACE;
-    const PromptPlan pl = prompt_plan(p);
+    const PromptPlan pl = prompt_plan(dtype, p);
     PromptArgs a = {};
     a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out; a.lse = p->lse;
     a.q_head = p->q_head; a.q_row = p->q_row; a.k_head = p->k_head; a.k_row = p->k_row;

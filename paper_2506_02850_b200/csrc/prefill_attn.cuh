@@ -22,6 +22,10 @@ struct PromptArgs {
     int32_t* status;
 };
 
+// The tensor-core kernel (bf16): CTAs without splits, and the launch.
+long long prompt_mma_ctas(int Hkv, int G, int n_q, int n_seq);
+int launch_prompt_attn_mma(const PromptArgs& a, int dh, long long ctas, cudaStream_t st);
+
 struct PromptDoc {
     int q0, k0, Lq, Lk, prefix;
     int tile;                                  // of the document's tiles, longest keys first; -1: there is none
