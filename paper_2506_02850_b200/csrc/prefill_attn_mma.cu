@@ -12,7 +12,8 @@
 // within the range of the exponent gives the same result, and a change costs a pass over O_x.  The row's own thread makes
 // it: when S_x of a tile has arrived, the product before it on O_x is complete (one thread issues all of them, in order).
 //
-// Warps 0-3 and 4-7: the rows of tiles 0 and 1; warp 8: TMA; warp 9: products.  Every wait is bounded.
+// Warps 0-3 and 4-7: the rows of tiles 0 and 1; warp 8: TMA; warp 9: products.  Every wait is bounded.  A row's 128 logits are read
+// from tensor memory twice, 32 at a time (for the maximum, then for the weights): held in registers they spill.
 #include <algorithm>
 
 #include "launchers.h"
@@ -94,7 +95,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     using S = MmaShape<DH>;
     grid_dep_wait();
     extern __shared__ uint8_t smem_dyn[];
-    __shared__ __align__(8) uint64_t q_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2], o_bar[2], drain_bar;
+    __shared__ __align__(8) uint64_t q_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], o_bar[2], drain_bar;
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort;
     __shared__ __align__(16) float s_pos[2][2][kN];    // [tile][buffer]: positions of the keys
@@ -135,7 +136,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         mbar_init(smem_u32(&q_bar), 1);
         mbar_init(smem_u32(&drain_bar), 1);
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&p_bar[x]), 4); mbar_init(smem_u32(&o_bar[x]), 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
         s_abort = 0;
         mbar_fence_init();
     }
@@ -231,16 +232,20 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 if (j >= n[x]) continue;
-                if (!(ok = mbar_wait_warp(smem_u32(&p_bar[x]), (uint32_t)j & 1u, abort_flag))) break;
-                tc_fence_after();
-                if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < kN / 16; ++kk)
-                        umma_bf16_ts(tmem + 2 * kN + (uint32_t)x * DH, tmem + (uint32_t)x * kN + kk * 8, desc_v(kv_addr(vs) + kk * 2048, S::kBlk), idesc_o,
-                                     j > 0 || kk > 0 ? 1u : 0u);
-                    if (j + 1 == n[x]) umma_commit(smem_u32(&o_bar[x]));
+                for (int half = 0; half < 2; ++half) { // the first 64 keys' weights are there while the others are made
+                    if (!(ok = mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)j & 1u, abort_flag))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                            umma_bf16_ts(tmem + 2 * kN + (uint32_t)x * DH, tmem + (uint32_t)x * kN + kk * 8, desc_v(kv_addr(vs) + kk * 2048, S::kBlk), idesc_o,
+                                         j > 0 || kk > 0 ? 1u : 0u);
+                        if (half && j + 1 == n[x]) umma_commit(smem_u32(&o_bar[x]));
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (!ok) break;
                 if (j + 1 < n[x]) logits(x, j + 1);
             }
             if (!ok) break;
@@ -286,62 +291,62 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 break;
             }
             tc_fence_after();
-            uint32_t raw[4][32];
+            const bool masked = k0 + kN > sure;
+            uint32_t buf[2][32];
+            // the maximum; logits that are more than a scaled product are written back
+            float mx = ninf;
+            tmem_ld32_issue(t_s, buf[0]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + c * 32, raw[c]);
+            for (int c = 0; c < 4; ++c) {
+                uint32_t (&raw)[32] = buf[c & 1];
+                tmem_ld32_wait(raw);
+                if (!(kCap || kBias) && c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);
+                float v[32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32_wait(raw[c]);
-            float v[4][32];
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+                if constexpr (kCap) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                    for (int i = 0; i < 32; ++i) v[i] = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(v[i] * (2.f * kAttnLog2e * a.cap_scale), 80.f)));
+                } else if constexpr (kBias) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[c][i] = __uint_as_float(raw[c][i]);
-            if constexpr (kCap) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[c][i] = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(v[c][i] * (2.f * kAttnLog2e * a.cap_scale), 80.f)));
-            } else if constexpr (kBias) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[c][i] *= a.scale_log2;
-            }
-            if constexpr (kBias) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
+                    for (int i = 0; i < 32; ++i) v[i] *= a.scale_log2;
+                }
+                if constexpr (kBias) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
                         const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][j & 1][c * 32 + i]);
-                        v[c][i] = fmaf(-slope, fabsf(my_pos - p.x), v[c][i]);
-                        v[c][i + 1] = fmaf(-slope, fabsf(my_pos - p.y), v[c][i + 1]);
-                        v[c][i + 2] = fmaf(-slope, fabsf(my_pos - p.z), v[c][i + 2]);
-                        v[c][i + 3] = fmaf(-slope, fabsf(my_pos - p.w), v[c][i + 3]);
+                        v[i] = fmaf(-slope, fabsf(my_pos - p.x), v[i]);
+                        v[i + 1] = fmaf(-slope, fabsf(my_pos - p.y), v[i + 1]);
+                        v[i + 2] = fmaf(-slope, fabsf(my_pos - p.z), v[i + 2]);
+                        v[i + 3] = fmaf(-slope, fabsf(my_pos - p.w), v[i + 3]);
                     }
-            }
-            const float sc = kCap || kBias ? 1.f : a.scale_log2;        // still to be multiplied in
-            if (k0 + kN > sure) {
+                }
+                if constexpr (kCap || kBias) {
+                    uint32_t w[32];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                    for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
+                    tmem_st32(t_s + c * 32, w);
+                    if (c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);   // (earlier, its registers would not be there)
+                }
+                if (masked) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[c][i] = k0 + c * 32 + i < keys ? v[c][i] : ninf;
-            }
-            float top[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
+                    for (int i = 0; i < 32; ++i) v[i] = k0 + c * 32 + i < keys ? v[i] : ninf;
+                }
                 float t8[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t8[i] = fmaxf(fmaxf(v[c][i], v[c][i + 8]), fmaxf(v[c][i + 16], v[c][i + 24]));
-                top[c] = fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7])));
+                for (int i = 0; i < 8; ++i) t8[i] = fmaxf(fmaxf(v[i], v[i + 8]), fmaxf(v[i + 16], v[i + 24]));
+                mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7]))));
             }
-            const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+            if constexpr (kCap || kBias) tmem_st_wait();
+            const float sc = kCap || kBias ? 1.f : a.scale_log2;        // still to be multiplied in
+            mx *= sc;
             const bool grow = mx > m + kGrow;          // (also from -infinity)
             if (__any_sync(0xFFFFFFFFu, grow)) {
                 const float f = grow ? fast_exp2(m - mx) : 1.f;
                 if (grow) m = mx;
                 l *= f;
                 if (j > 0) {                           // the product before this one on O_x is complete
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < DH / 32; ++c) {
                         uint32_t o[32];
                         tmem_ld32_issue(t_o + c * 32, o);
@@ -352,34 +357,52 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     }
                 }
             }
+            tmem_ld32_issue(t_s, buf[0]);
             const float base = m == ninf ? 0.f : m;
             const uint64_t sc2 = pair(sc, sc), add2 = pair(-base, -base);
             uint64_t sum0 = 0ull, sum1 = 0ull;
+            uint32_t p[32];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t p[32];
+            for (int c = 0; c < 4; ++c) {
+                uint32_t (&raw)[32] = buf[c & 1];
+                tmem_ld32_wait(raw);
+                if (c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);
+                if (masked) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int c = half * 2 + (i >> 4), e = 2 * (i & 15);
-                    const uint64_t y = fma_pair(pair(v[c][e], v[c][e + 1]), sc2, add2);
-                    const uint64_t w = exp2_pair(y);
-                    if (i & 1) sum1 = add_pair(sum1, w);
-                    else sum0 = add_pair(sum0, w);
-                    float w0, w1;
-                    unpair(w, w0, w1);
-                    p[i] = pack_bf16(w0, w1);
+                    for (int i = 0; i < 16; ++i) {
+                        const int k = k0 + c * 32 + 2 * i;
+                        const uint64_t w = exp2_pair(fma_pair(pair(k < keys ? __uint_as_float(raw[2 * i]) : ninf, k + 1 < keys ? __uint_as_float(raw[2 * i + 1]) : ninf), sc2, add2));
+                        if (i & 1) sum1 = add_pair(sum1, w);
+                        else sum0 = add_pair(sum0, w);
+                        float w0, w1;
+                        unpair(w, w0, w1);
+                        p[(c & 1) * 16 + i] = pack_bf16(w0, w1);
+                    }
+                } else {                               // every fourth pair on the FMA pipe (never 0 there: not where keys are hidden)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint64_t y = fma_pair(pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), sc2, add2);
+                        const uint64_t w = (i & 3) == 3 ? exp2_fma_pair<false>(y) : exp2_pair(y);
+                        if (i & 1) sum1 = add_pair(sum1, w);
+                        else sum0 = add_pair(sum0, w);
+                        float w0, w1;
+                        unpair(w, w0, w1);
+                        p[(c & 1) * 16 + i] = pack_bf16(w0, w1);
+                    }
                 }
-                tmem_st32(t_s + half * 32, p);
+                if (c & 1) {                           // 64 keys' weights: their product may begin
+                    tmem_st32(t_s + (c >> 1) * 32, p);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][c >> 1]));
+                }
             }
             {
                 float s0, s1;
                 unpair(add_pair(sum0, sum1), s0, s1);
                 l += s0 + s1;
             }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&p_bar[x]));
         }
         if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), 0u, abort_flag)) ok = false;
         ok = __all_sync(0xFFFFFFFFu, ok);
