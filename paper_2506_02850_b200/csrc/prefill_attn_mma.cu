@@ -8,12 +8,13 @@
 //   O_x += P_x V         tcgen05.mma, P_x from tensor memory, V as it lies (keys x dh: the second operand's other order)
 // S_0, S_1, O_0 and O_1 fill the 512 columns.  While one tile's rows are in their exponentials the other's products run.
 //
-// A row's reference m is the maximum of its first tile and grows only where a later logit is more than 2^8 above it: any m
-// within the range of the exponent gives the same result, and a change costs a pass over O_x.  The row's own thread makes
-// it: when S_x of a tile has arrived, the product before it on O_x is complete (one thread issues all of them, in order).
+// Key tiles are taken from the last one down.  A row's reference m is the maximum of the first tile that it sees; later tiles' weights are taken against it with no maximum of their own,
+// since any m within the range of the exponent gives the same result.  Where the sum of 64 weights leaves that range they are
+// made again against their own maximum, and O_x and the sum are scaled: by the row's own thread, when the products
+// before on O_x are complete (one thread issues all of them, in order).
 //
 // Warps 0-3 and 4-7: the rows of tiles 0 and 1; warp 8: TMA; warp 9: products.  Every wait is bounded.  A row's 128 logits are read
-// from tensor memory twice, 32 at a time (for the maximum, then for the weights): held in registers they spill.
+// from tensor memory 32 at a time: held in registers they spill.
 #include <algorithm>
 
 #include "launchers.h"
@@ -25,7 +26,7 @@ namespace metok {
 namespace {
 
 constexpr int kM = 128, kN = 128, kThreads = 320;
-constexpr float kGrow = 8.f;                           // octaves that a logit may pass the row's reference by
+constexpr float kMost = 1.0e18f, kRoom = 32.f;         // sum of 64 weights beyond which a row's reference grows, and by how many octaves above their maximum
 
 template <int DH>
 struct MmaShape {
@@ -95,7 +96,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     using S = MmaShape<DH>;
     grid_dep_wait();
     extern __shared__ uint8_t smem_dyn[];
-    __shared__ __align__(8) uint64_t q_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], o_bar[2], drain_bar;
+    __shared__ __align__(8) uint64_t q_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], h_bar[2], o_bar[2], drain_bar;
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort;
     __shared__ __align__(16) float s_pos[2][2][kN];    // [tile][buffer]: positions of the keys
@@ -127,7 +128,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) n[x] = max(0, min(n[x], hi) - lo);
-    const int nt = max(n[0], n[1]);                    // key tiles lo .. lo + nt - 1
+    // key tiles lo + nt - 1 down to lo: the nearest ones first, which a bias makes the largest; item x joins in at step st[x]
+    const int nt = max(n[0], n[1]), st[2] = {nt - n[0], nt - n[1]};
+    auto tile_key = [&](int j) { return (lo + nt - 1 - j) * kN; };
 
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     auto q_addr = [&](int x) { return smem_base + (uint32_t)x * S::kTile; };
@@ -136,7 +139,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         mbar_init(smem_u32(&q_bar), 1);
         mbar_init(smem_u32(&drain_bar), 1);
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
+        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); mbar_init(smem_u32(&h_bar[x]), 1); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
         s_abort = 0;
         mbar_fence_init();
     }
@@ -169,7 +172,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
             __syncwarp();
             for (; it < 2 * nt; ++it) {
-                const int s = it % S::kStages, row = d.k0 + (lo + (it >> 1)) * kN;
+                const int s = it % S::kStages, row = d.k0 + tile_key(it >> 1);
                 if (!mbar_wait_warp(smem_u32(&empty_bar[s]), ((uint32_t)(it / S::kStages) & 1u) ^ 1u, abort_flag)) break;
                 if (elect_one()) {
                     const uint32_t fb = smem_u32(&full_bar[s]);
@@ -205,21 +208,36 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
             __syncwarp();
         };
-        if (ok && nt > 0) {
-            ok = wait_full(0);
-            if (ok) {
-                tc_fence_after();
+        auto values = [&](int x, int j, int half) {    // O_x += P_x V of 64 keys of tile j
+            const int vs = (2 * j + 1) % S::kStages, jx = j - st[x];
+            if (!mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)jx & 1u, abort_flag)) return false;
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (n[x] > 0) logits(x, 0);
-                if (elect_one()) umma_commit(smem_u32(&empty_bar[0]));
-                __syncwarp();
+                for (int kk = 0; kk < 4; ++kk)
+                    umma_bf16_ts(tmem + 2 * kN + (uint32_t)x * DH, tmem + (uint32_t)x * kN + half * 32 + kk * 8, desc_v(kv_addr(vs) + (half * 4 + kk) * 2048, S::kBlk), idesc_o,
+                                 jx > 0 || half || kk > 0 ? 1u : 0u);
+                if (!half) umma_commit(smem_u32(&h_bar[x]));
+                else if (j + 1 == nt) umma_commit(smem_u32(&o_bar[x]));
             }
+            __syncwarp();
+            return true;
+        };
+        auto release = [&](int it) {
+            if (elect_one()) umma_commit(smem_u32(&empty_bar[it % S::kStages]));
+            __syncwarp();
+        };
+        // One item's second half and next logits lie between the other's halves, so that the products go on while either's weights
+        // are made: per step  O_0 first half | O_1 second half of the step before, S_1 | O_0 second half, next S_0 | O_1 first half.
+        if (ok && nt > 0 && (ok = wait_full(0))) {
+            tc_fence_after();
+            for (int x = 0; x < 2; ++x)
+                if (st[x] == 0) logits(x, 0);
         }
         for (int j = 0; ok && j < nt; ++j) {
             const int vi = 2 * j + 1, vs = vi % S::kStages;
             if (!(ok = wait_full(vi))) break;
-            const int left = d.Lk - (lo + j) * kN;     // rows of the document in this tile
+            const int left = d.Lk - tile_key(j);       // rows of the document in this tile
             if (left < kN) {                           // those behind count as zeros, whatever they hold
                 for (int c = lane; c < (kN - left) * S::KB * 8; c += 32) {
                     const int r = left + c / (S::KB * 8), e = c % (S::KB * 8);
@@ -228,33 +246,21 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 fence_proxy_async();
                 __syncwarp();
             }
-            if (j + 1 < nt && !(ok = wait_full(2 * j + 2))) break;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (j >= n[x]) continue;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) { // the first 64 keys' weights are there while the others are made
-                    if (!(ok = mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)j & 1u, abort_flag))) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                            umma_bf16_ts(tmem + 2 * kN + (uint32_t)x * DH, tmem + (uint32_t)x * kN + kk * 8, desc_v(kv_addr(vs) + kk * 2048, S::kBlk), idesc_o,
-                                         j > 0 || kk > 0 ? 1u : 0u);
-                        if (half && j + 1 == n[x]) umma_commit(smem_u32(&o_bar[x]));
-                    }
-                    __syncwarp();
-                }
-                if (!ok) break;
-                if (j + 1 < n[x]) logits(x, j + 1);
+            if (j >= st[0] && !(ok = values(0, j, 0))) break;
+            if (j > 0) {
+                if (j > st[1] && !(ok = values(1, j - 1, 1))) break;
+                if (j >= st[1]) logits(1, j);
+                release(vi - 2);
             }
-            if (!ok) break;
-            if (elect_one()) {
-                umma_commit(smem_u32(&empty_bar[vs]));
-                if (j + 1 < nt) umma_commit(smem_u32(&empty_bar[(2 * j + 2) % S::kStages]));
+            release(2 * j);                            // (S_1's, or S_0's in the first step)
+            if (j >= st[0] && !(ok = values(0, j, 1))) break;
+            if (j + 1 < nt) {
+                if (!(ok = wait_full(2 * j + 2))) break;
+                if (j + 1 >= st[0]) logits(0, j + 1);
             }
-            __syncwarp();
+            if (j >= st[1] && !(ok = values(1, j, 0))) break;
         }
+        if (ok && n[1] > 0) ok = values(1, nt - 1, 1);
         if (!ok) {                                     // whatever was issued has retired before the tensor memory goes
             if (elect_one()) umma_commit(smem_u32(&drain_bar));
             __syncwarp();
@@ -275,13 +281,13 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         if (kBias && my_n > 0) {
             slope = a.slopes[my_head] * kAttnLog2e;
             my_pos = prompt_position(a, d, d.Lk - d.Lq + my_i0 + r);
-            next_pos = prompt_position(a, d, lo * kN + r);
+            next_pos = prompt_position(a, d, (lo + my_n - 1) * kN + r);
         }
         for (int j = 0; j < my_n; ++j) {
-            const int k0 = (lo + j) * kN;
+            const int k0 = (lo + my_n - 1 - j) * kN;
             if constexpr (kBias) {                     // (two buffers: who writes one again has met the others since it was read)
                 s_pos[x][j & 1][r] = next_pos;
-                next_pos = prompt_position(a, d, k0 + kN + r);
+                next_pos = prompt_position(a, d, k0 - kN + r);
                 named_bar_sync(1 + x, 128);
             }
             if (ok && !mbar_wait(smem_u32(&s_bar[x]), (uint32_t)j & 1u, abort_flag)) ok = false;
@@ -292,24 +298,16 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
             tc_fence_after();
             const bool masked = k0 + kN > sure;
-            uint32_t buf[2][32];
-            // the maximum; logits that are more than a scaled product are written back
-            float mx = ninf;
-            tmem_ld32_issue(t_s, buf[0]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t (&raw)[32] = buf[c & 1];
-                tmem_ld32_wait(raw);
-                if (!(kCap || kBias) && c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+            // Logits of columns 32 c .. in log2 units less `base`; those of keys that the row does not see are -infinity.
+            auto logit = [&](const uint32_t (&raw)[32], int c, float base, float (&v)[32]) {
                 if constexpr (kCap) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(v[i] * (2.f * kAttnLog2e * a.cap_scale), 80.f)));
-                } else if constexpr (kBias) {
+                    for (int i = 0; i < 32; ++i)
+                        v[i] = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(__uint_as_float(raw[i]) * (2.f * kAttnLog2e * a.cap_scale), 80.f)));
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= a.scale_log2;
+                    for (int i = 0; i < 32; i += 2)
+                        unpair(fma_pair(pair(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), pair(a.scale_log2, a.scale_log2), pair(-base, -base)), v[i], v[i + 1]);
                 }
                 if constexpr (kBias) {
 #pragma unroll
@@ -321,87 +319,98 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                         v[i + 3] = fmaf(-slope, fabsf(my_pos - p.w), v[i + 3]);
                     }
                 }
-                if constexpr (kCap || kBias) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
-                    tmem_st32(t_s + c * 32, w);
-                    if (c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);   // (earlier, its registers would not be there)
-                }
                 if (masked) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = k0 + c * 32 + i < keys ? v[i] : ninf;
                 }
-                float t8[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) t8[i] = fmaxf(fmaxf(v[i], v[i + 8]), fmaxf(v[i + 16], v[i + 24]));
-                mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7]))));
-            }
-            if constexpr (kCap || kBias) tmem_st_wait();
-            const float sc = kCap || kBias ? 1.f : a.scale_log2;        // still to be multiplied in
-            mx *= sc;
-            const bool grow = mx > m + kGrow;          // (also from -infinity)
-            if (__any_sync(0xFFFFFFFFu, grow)) {
-                const float f = grow ? fast_exp2(m - mx) : 1.f;
-                if (grow) m = mx;
-                l *= f;
-                if (j > 0) {                           // the product before this one on O_x is complete
+            };
+            // the largest of columns [32 c0, 32 c1)
+            auto largest = [&](int c0, int c1) {
+                float mx = ninf;
 #pragma unroll 1
-                    for (int c = 0; c < DH / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32_issue(t_o + c * 32, o);
-                        tmem_ld32_wait(o);
+                for (int c = c0; c < c1; ++c) {
+                    uint32_t raw[32];
+                    float v[32];
+                    tmem_ld32_issue(t_s + c * 32, raw);
+                    tmem_ld32_wait(raw);
+                    logit(raw, c, 0.f, v);
+                    float t8[8];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st32(t_o + c * 32, o);
-                    }
+                    for (int i = 0; i < 8; ++i) t8[i] = fmaxf(fmaxf(v[i], v[i + 8]), fmaxf(v[i + 16], v[i + 24]));
+                    mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7]))));
                 }
-            }
-            tmem_ld32_issue(t_s, buf[0]);
-            const float base = m == ninf ? 0.f : m;
-            const uint64_t sc2 = pair(sc, sc), add2 = pair(-base, -base);
-            uint64_t sum0 = 0ull, sum1 = 0ull;
-            uint32_t p[32];
+                return mx;
+            };
+            // 32 weights of the row, and their sum
+            auto weights = [&](const uint32_t (&raw)[32], int c, uint32_t* p) {
+                float v[32];
+                logit(raw, c, m == ninf ? 0.f : m, v);
+                uint64_t sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t (&raw)[32] = buf[c & 1];
-                tmem_ld32_wait(raw);
-                if (c < 3) tmem_ld32_issue(t_s + (c + 1) * 32, buf[(c + 1) & 1]);
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int k = k0 + c * 32 + 2 * i;
-                        const uint64_t w = exp2_pair(fma_pair(pair(k < keys ? __uint_as_float(raw[2 * i]) : ninf, k + 1 < keys ? __uint_as_float(raw[2 * i + 1]) : ninf), sc2, add2));
-                        if (i & 1) sum1 = add_pair(sum1, w);
-                        else sum0 = add_pair(sum0, w);
-                        float w0, w1;
-                        unpair(w, w0, w1);
-                        p[(c & 1) * 16 + i] = pack_bf16(w0, w1);
-                    }
-                } else {                               // every fourth pair on the FMA pipe (never 0 there: not where keys are hidden)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint64_t y = fma_pair(pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1])), sc2, add2);
-                        const uint64_t w = (i & 3) == 3 ? exp2_fma_pair<false>(y) : exp2_pair(y);
-                        if (i & 1) sum1 = add_pair(sum1, w);
-                        else sum0 = add_pair(sum0, w);
-                        float w0, w1;
-                        unpair(w, w0, w1);
-                        p[(c & 1) * 16 + i] = pack_bf16(w0, w1);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const float w0 = fast_exp2(v[2 * i]), w1 = fast_exp2(v[2 * i + 1]);
+                    if (i & 1) sum1 = add_pair(sum1, pair(w0, w1));
+                    else sum0 = add_pair(sum0, pair(w0, w1));
+                    p[i] = pack_bf16(w0, w1);
                 }
-                if (c & 1) {                           // 64 keys' weights: their product may begin
-                    tmem_st32(t_s + (c >> 1) * 32, p);
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][c >> 1]));
-                }
-            }
-            {
                 float s0, s1;
                 unpair(add_pair(sum0, sum1), s0, s1);
-                l += s0 + s1;
+                return s0 + s1;
+            };
+            const bool first = m == ninf && keys > k0; // the first tile of which the row sees something
+            if (__any_sync(0xFFFFFFFFu, first)) {
+                const float mx = largest(0, 4);
+                if (first) m = mx;
+            }
+            uint32_t raw[2][32];
+            tmem_ld32_issue(t_s, raw[0]);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t p[32];
+                tmem_ld32_wait(raw[0]);
+                tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
+                float sum = weights(raw[0], half * 2, p);
+                tmem_ld32_wait(raw[1]);
+                if (!half) tmem_ld32_issue(t_s + 64, raw[0]);
+                sum += weights(raw[1], half * 2 + 1, p + 16);
+                const bool far = !(sum < kMost);
+                if (__any_sync(0xFFFFFFFFu, far)) {    // again, against the maximum of these
+                    if (!half) tmem_ld32_wait(raw[0]); // (in order: nothing is on its way while registers are short)
+                    const float mx = largest(half * 2, half * 2 + 2);
+                    const bool grow = far && mx > m;
+                    const float f = grow ? fast_exp2(m - (mx + kRoom)) : 1.f;
+                    if (grow) m = mx + kRoom;
+                    l *= f;
+                    // the product before this one on O_x is complete: that of the tile before since S_x is there, that of the first half when its barrier says so
+                    if (half && ok && !mbar_wait(smem_u32(&h_bar[x]), (uint32_t)j & 1u, abort_flag)) ok = false;
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    tc_fence_after();
+                    if (j > 0 || half) {
+#pragma unroll 1
+                        for (int c = 0; c < DH / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32_issue(t_o + c * 32, o);
+                            tmem_ld32_wait(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(t_o + c * 32, o);
+                        }
+                    }
+                    sum = 0.f;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t again[32];
+                        tmem_ld32_issue(t_s + half * 64 + c * 32, again);
+                        tmem_ld32_wait(again);
+                        sum += weights(again, half * 2 + c, p + c * 16);
+                    }
+                }
+                l += sum;
+                tmem_st32(t_s + half * 32, p);         // 64 keys' weights: their product may begin
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][half]));
             }
         }
         if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), 0u, abort_flag)) ok = false;
@@ -434,7 +443,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                                                                                  pack_bf16(o[i + 4] * scale, o[i + 5] * scale), pack_bf16(o[i + 6] * scale, o[i + 7] * scale));
                 }
             }
-            if (mine && a.splits > 1) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m, l);
+            if (mine && a.splits > 1) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(l > 0.f ? m : ninf, l);
             else if (mine && a.lse) a.lse[(long long)my_head * a.n_q + row] = kAttnLn2 * (m + log2f(l));
         }
     }
