@@ -768,20 +768,31 @@ paged_join_kernel(const PagedAttnArgs a) {
         return;
     }
 
-    // weights: the heads' normalisers, a warp per head
-    for (int h = warp; h < a.Hq; h += kJoinThreads / 32) {
-        const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads, sub = hk * a.NC + ch;
-        const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
+    // weights: the heads' normalisers, eight threads per head, a running (maximum, sum) each with four loads on their way
+    for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
+        const int h = h0 + (tid >> 3), part = tid & 7;
         float M = kLow, L = 0.f;
-        for (int i = lane; i < sl.n; i += 32) M = fmaxf(M, a.part_ml[((sl.first + i) * a.heads + hl) * 2]);
+        if (h < a.Hq) {
+            const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads, sub = hk * a.NC + ch;
+            const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
+            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + sl.first * a.heads + hl;
+            for (int i0 = part; i0 < sl.n; i0 += 32) {
+                float2 x[4];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-        for (int i = lane; i < sl.n; i += 32) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((sl.first + i) * a.heads + hl) * 2);
-            L += exp2f(ml.x - M) * ml.y;
+                for (int u = 0; u < 4; ++u) x[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
+                const float top = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), M);
+                L = L * exp2f(M - top) + (exp2f(x[0].x - top) * x[0].y + exp2f(x[1].x - top) * x[1].y) +
+                    (exp2f(x[2].x - top) * x[2].y + exp2f(x[3].x - top) * x[3].y);
+                M = top;
+            }
         }
-        L = warp_sum(L);
-        if (lane == 0) s_lse[h] = M + log2f(L);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, o), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, o), top = fmaxf(M, m2);
+            L = L * exp2f(M - top) + l2 * exp2f(m2 - top);
+            M = top;
+        }
+        if (h < a.Hq && part == 0) s_lse[h] = M + log2f(L);
     }
     __syncthreads();
     const int row = row0 + tid;
@@ -791,6 +802,7 @@ paged_join_kernel(const PagedAttnArgs a) {
     for (int sub = 0; sub < subs; ++sub) {
         const int hk = sub / a.NC, ch = sub - hk * a.NC, h0 = hk * a.G + ch * a.heads, nh = min(a.heads, a.G - ch * a.heads);
         const float* x = a.logits + (size_t)(base + (long long)sub * nt + tile) * a.heads * rows_tile + off;
+#pragma unroll 8
         for (int g = 0; g < nh; ++g) sum += exp2f(x[(size_t)g * rows_tile] - s_lse[h0 + g]);
     }
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
