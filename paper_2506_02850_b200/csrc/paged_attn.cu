@@ -50,9 +50,14 @@ __device__ __forceinline__ int unit_tiles(const PagedAttnArgs& a, int b) {
     return len > 0 && len <= a.d.S_cap() ? (len + (1 << a.tile_shift) - 1) >> a.tile_shift : 0;
 }
 
-// Tiles of the sequences before sequence b, per unit of a sequence, and of all; whole CTA.
+// Tiles of the sequences before sequence b, per unit of a sequence, and of all; whole CTA.  Up to 32 sequences every warp finds
+// out by itself: no barrier.
 struct LineSums { long long before, all; };
 __device__ __forceinline__ LineSums line_sums(const PagedAttnArgs& a, int b, long long* s_sum) {
+    if (a.d.n_seqs <= 32) {
+        const int lane = threadIdx.x & 31, t = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
+        return {(long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? t : 0), (long long)__reduce_add_sync(0xFFFFFFFFu, t)};
+    }
     long long before = 0, all = 0;
     for (int i = threadIdx.x; i < a.d.n_seqs; i += blockDim.x) {
         const int t = unit_tiles(a, i);
@@ -514,8 +519,11 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     const long long T_all = sums.all * subs, ctas = busy_ctas(a, T_all);
     if (blockIdx.x >= ctas) return;                    // uniform
     const long long t_lo = T_all * blockIdx.x / ctas, t_hi = T_all * (blockIdx.x + 1) / ctas;
-    // the sequence that holds tile t_lo: 32 at a time
-    if (warp == 0) {
+    // the sequence that holds tile t_lo, 32 at a time: by every warp for itself where there are no more
+    Place p;
+    long long start = 0;
+    p.b = 0;
+    if (warp == 0 || a.d.n_seqs <= 32) {
         long long at = 0;                              // tiles before sequence b0
         for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
             const int b = b0 + lane;
@@ -527,20 +535,25 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
             }
             const uint32_t any = __ballot_sync(0xFFFFFFFFu, at + incl > t_lo);
             if (any) {
-                if (lane == __ffs(any) - 1) {
-                    s_b = b;
-                    s_start = at + incl - mine;
-                }
+                const int l = __ffs(any) - 1;
+                p.b = b0 + l;
+                start = at + __shfl_sync(0xFFFFFFFFu, incl - mine, l);
                 break;
             }
             at += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
     }
+    if (a.d.n_seqs > 32 && threadIdx.x == 0) {
+        s_b = p.b;
+        s_start = start;
+    }
     __syncthreads();
-    Place p;
-    p.b = s_b;
+    if (a.d.n_seqs > 32) {
+        p.b = s_b;
+        start = s_start;
+    }
     p.nt = unit_tiles(a, p.b);
-    const long long in = t_lo - s_start;
+    const long long in = t_lo - start;
     p.sub = (int)(in / p.nt);
     p.t = (int)(in - (long long)p.sub * p.nt);
     p.left = t_hi - t_lo;
@@ -739,14 +752,23 @@ paged_join_kernel(const PagedAttnArgs a) {
         for (int w = 0; w < kJoinThreads / 32; ++w) M = fmaxf(M, s_w[w]);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float L = 0.f;
-#pragma unroll 4
-        for (int i = run; i < sl.n; i += kRuns) {
-            const size_t at = (size_t)(sl.first + i) * a.heads + hl;
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-            const float4 o = reinterpret_cast<const float4*>(a.part_o + at * DH)[col];
-            const float f = exp2f(ml.x - M);
-            L += f * ml.y;
-            acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
+        constexpr int kAhead = 6;                      // slots whose loads are on their way
+        for (int i0 = run; i0 < sl.n; i0 += kRuns * kAhead) {
+            float2 ml[kAhead];
+            float4 o[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const size_t at = (size_t)(sl.first + i0 + u * kRuns) * a.heads + hl;
+                const bool in = i0 + u * kRuns < sl.n;
+                ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + at * 2) : make_float2(kLow, 0.f);
+                o[u] = in ? reinterpret_cast<const float4*>(a.part_o + at * DH)[col] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const float f = exp2f(ml[u].x - M);
+                L += f * ml[u].y;
+                acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
+            }
         }
         *reinterpret_cast<float4*>(s_acc[tid]) = acc;
         s_l[tid] = L;
@@ -802,8 +824,13 @@ paged_join_kernel(const PagedAttnArgs a) {
     for (int sub = 0; sub < subs; ++sub) {
         const int hk = sub / a.NC, ch = sub - hk * a.NC, h0 = hk * a.G + ch * a.heads, nh = min(a.heads, a.G - ch * a.heads);
         const float* x = a.logits + (size_t)(base + (long long)sub * nt + tile) * a.heads * rows_tile + off;
-#pragma unroll 8
-        for (int g = 0; g < nh; ++g) sum += exp2f(x[(size_t)g * rows_tile] - s_lse[h0 + g]);
+        for (int g0 = 0; g0 < nh; g0 += 8) {           // eight loads on their way (a loop of nh of them would wait for each)
+            float v[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) v[g] = g0 + g < nh ? x[(size_t)(g0 + g) * rows_tile] : kLow;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) sum += g0 + g < nh ? exp2f(v[g] - s_lse[h0 + g0 + g]) : 0.f;
+        }
     }
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
 }
