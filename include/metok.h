@@ -542,7 +542,7 @@ METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const vo
  *   The work is cut along the caches' lengths into equal pieces for all SMs and joined
  *   by a second kernel; a call's results depend on nothing but its inputs.
  *   Errors: INVALID_ARG (null or misaligned pointers, Hq % Hkv, strides, softmax_scale not
- *   finite or <= 0, softcap < 0 or not finite, and as in (6)); UNSUPPORTED (as in (6), Hq > 8192,
+ *   finite or <= 0, softcap < 0 or not finite, and as in (6)); UNSUPPORTED (as in (6), Hq > 2048,
  *   more than 2^31 - 1 pieces of work); WORKSPACE.
  * ------------------------------------------------------------------------- */
 METOK_API size_t metok_paged_attention_workspace_bytes(int dtype, const metok_paged_cache* c, int Hq, int with_mass);

@@ -222,7 +222,7 @@ __device__ __forceinline__ void bf16_tile(Bf16Unit<DH, NG>& u, const PagedAttnAr
             top[e] = fmaxf(top[e], u.m[n][e]);
         }
         if (__any_sync(0xFFFFFFFFu, top[0] > u.m[n][0] || top[1] > u.m[n][1])) {
-            const float f0 = exp2f(u.m[n][0] - top[0]), f1 = exp2f(u.m[n][1] - top[1]);
+            const float f0 = sm100::fast_exp2(u.m[n][0] - top[0]), f1 = sm100::fast_exp2(u.m[n][1] - top[1]);
             u.l[n][0] *= f0;
             u.l[n][1] *= f1;
 #pragma unroll
@@ -237,7 +237,7 @@ __device__ __forceinline__ void bf16_tile(Bf16Unit<DH, NG>& u, const PagedAttnAr
         }
         float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = (e < 2 ? in0 : in1) ? exp2f(x[n][e] - u.m[n][e & 1]) : 0.f;
+        for (int e = 0; e < 4; ++e) p[e] = (e < 2 ? in0 : in1) ? sm100::fast_exp2(x[n][e] - u.m[n][e & 1]) : 0.f;
         u.l[n][0] += p[0] + p[2];
         u.l[n][1] += p[1] + p[3];
 #pragma unroll
@@ -297,8 +297,8 @@ __device__ __forceinline__ void unit_merge(Bf16Unit<DH, NG>& u, const float* s_o
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float m = s_ml[2 * (h + e)], M = fmaxf(m, u.m[n][e]);
-            f[e] = exp2f(u.m[n][e] - M);
-            g[e] = exp2f(m - M);
+            f[e] = sm100::fast_exp2(u.m[n][e] - M);
+            g[e] = sm100::fast_exp2(m - M);
             u.l[n][e] = u.l[n][e] * f[e] + s_ml[2 * (h + e) + 1] * g[e];
             u.m[n][e] = M;
         }
@@ -409,7 +409,7 @@ __device__ __forceinline__ void f32_tile(F32Unit<DH, HW>& u, const PagedAttnArgs
     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
     if (__any_sync(0xFFFFFFFFu, top > u.m)) {
-        const float f = exp2f(u.m - top);
+        const float f = sm100::fast_exp2(u.m - top);
         u.m = top;
         u.l *= f;
 #pragma unroll
@@ -423,7 +423,7 @@ __device__ __forceinline__ void f32_tile(F32Unit<DH, HW>& u, const PagedAttnArgs
     for (int p = 0; p < P; ++p) {
         const int r = r_lo + p * 4 + kg;
         const bool in = r < rows;
-        const float w = in ? exp2f(x[p] - u.m) : 0.f;
+        const float w = in ? sm100::fast_exp2(x[p] - u.m) : 0.f;
         u.l += w;
         float wh[HW];
 #pragma unroll
@@ -458,7 +458,7 @@ __device__ __forceinline__ void unit_close(F32Unit<DH, HW>& u) {
 template <int DH, int HW>
 __device__ __forceinline__ void unit_merge(F32Unit<DH, HW>& u, const float* s_o, const float* s_ml) {
     const int sub = threadIdx.x & 7, head = u.hb + sub * HW / 8;
-    const float m = s_ml[2 * head], M = fmaxf(m, u.m), f = exp2f(u.m - M), g = exp2f(m - M);
+    const float m = s_ml[2 * head], M = fmaxf(m, u.m), f = sm100::fast_exp2(u.m - M), g = sm100::fast_exp2(m - M);
     u.l = u.l * f + s_ml[2 * head + 1] * g;
     u.m = M;
 #pragma unroll
@@ -654,7 +654,7 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
                         if constexpr (kHeadWarps == 1) {       // both have the head
                             const float m0 = s_ml[0][2 * h], m1 = s_ml[1][2 * h];
                             M = fmaxf(m0, m1);
-                            const float f = exp2f(m0 - M), g = exp2f(m1 - M);
+                            const float f = sm100::fast_exp2(m0 - M), g = sm100::fast_exp2(m1 - M);
                             L = f * s_ml[0][2 * h + 1] + g * s_ml[1][2 * h + 1];
                             const float4 x = reinterpret_cast<const float4*>(s_o[0])[i], y = reinterpret_cast<const float4*>(s_o[1])[i];
                             o = make_float4(f * x.x + g * y.x, f * x.y + g * y.y, f * x.z + g * y.z, f * x.w + g * y.w);
@@ -701,7 +701,7 @@ paged_join_kernel(const PagedAttnArgs a) {
     __shared__ __align__(16) float s_acc[kJoinThreads][4];
     __shared__ float s_l[kJoinThreads];
     __shared__ float s_w[kJoinThreads / 32];
-    extern __shared__ float s_lse[];                   // weights: log2 of the sum of every head
+    extern __shared__ __align__(16) uint8_t s_dyn[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int outs = a.d.n_seqs * a.Hq;
     const bool weights = (int)blockIdx.x >= outs;
@@ -765,7 +765,7 @@ paged_join_kernel(const PagedAttnArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const float f = exp2f(ml[u].x - M);
+                const float f = sm100::fast_exp2(ml[u].x - M);
                 L += f * ml[u].y;
                 acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
             }
@@ -790,28 +790,38 @@ paged_join_kernel(const PagedAttnArgs a) {
         return;
     }
 
-    // weights: the heads' normalisers, eight threads per head, a running (maximum, sum) each with four loads on their way
+    // weights: where every unit's partials lie, then the heads' normalisers: eight threads per head, a running (maximum, sum) each
+    // with four loads on their way
+    long long* s_first = reinterpret_cast<long long*>(s_dyn);            // [subs]
+    int* s_n = reinterpret_cast<int*>(s_first + subs);                   // [subs]
+    float* s_lse = reinterpret_cast<float*>(s_n + subs);                 // [Hq]: log2 of the sum
+    for (int sub = tid; sub < subs; sub += kJoinThreads) {
+        const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
+        s_first[sub] = sl.first;
+        s_n[sub] = sl.n;
+    }
+    __syncthreads();
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
         const int h = h0 + (tid >> 3), part = tid & 7;
         float M = kLow, L = 0.f;
         if (h < a.Hq) {
             const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads, sub = hk * a.NC + ch;
-            const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
+            const Slots sl = {s_first[sub], s_n[sub]};
             const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + sl.first * a.heads + hl;
             for (int i0 = part; i0 < sl.n; i0 += 32) {
                 float2 x[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) x[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
                 const float top = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), M);
-                L = L * exp2f(M - top) + (exp2f(x[0].x - top) * x[0].y + exp2f(x[1].x - top) * x[1].y) +
-                    (exp2f(x[2].x - top) * x[2].y + exp2f(x[3].x - top) * x[3].y);
+                L = L * sm100::fast_exp2(M - top) + (sm100::fast_exp2(x[0].x - top) * x[0].y + sm100::fast_exp2(x[1].x - top) * x[1].y) +
+                    (sm100::fast_exp2(x[2].x - top) * x[2].y + sm100::fast_exp2(x[3].x - top) * x[3].y);
                 M = top;
             }
         }
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) {
             const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, o), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, o), top = fmaxf(M, m2);
-            L = L * exp2f(M - top) + l2 * exp2f(m2 - top);
+            L = L * sm100::fast_exp2(M - top) + l2 * sm100::fast_exp2(m2 - top);
             M = top;
         }
         if (h < a.Hq && part == 0) s_lse[h] = M + log2f(L);
@@ -820,16 +830,17 @@ paged_join_kernel(const PagedAttnArgs a) {
     const int row = row0 + tid;
     if (row >= len) return;
     const int tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
+    const float* x0 = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
     float sum = 0.f;
     for (int sub = 0; sub < subs; ++sub) {
         const int hk = sub / a.NC, ch = sub - hk * a.NC, h0 = hk * a.G + ch * a.heads, nh = min(a.heads, a.G - ch * a.heads);
-        const float* x = a.logits + (size_t)(base + (long long)sub * nt + tile) * a.heads * rows_tile + off;
+        const float* x = x0 + (size_t)sub * nt * a.heads * rows_tile;
         for (int g0 = 0; g0 < nh; g0 += 8) {           // eight loads on their way (a loop of nh of them would wait for each)
             float v[8];
 #pragma unroll
-            for (int g = 0; g < 8; ++g) v[g] = g0 + g < nh ? x[(size_t)(g0 + g) * rows_tile] : kLow;
+            for (int g = 0; g < 8; ++g) v[g] = g0 + g < nh ? x[(g0 + g) * rows_tile] : kLow;
 #pragma unroll
-            for (int g = 0; g < 8; ++g) sum += g0 + g < nh ? exp2f(v[g] - s_lse[h0 + g0 + g]) : 0.f;
+            for (int g = 0; g < 8; ++g) sum += g0 + g < nh ? sm100::fast_exp2(v[g] - s_lse[h0 + g0 + g]) : 0.f;
         }
     }
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
@@ -874,7 +885,7 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
     {
         METOK_TIMED("paged_join", st);
         const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), (size_t)a.Hq * sizeof(float), st, a);
+        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), a.mass ? (size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 : 0, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;
@@ -925,7 +936,7 @@ extern "C" int metok_paged_attention(int dtype, const metok_paged_cache* c, cons
     if (!(softmax_scale > 0.f) || !(softmax_scale < 3.0e38f) || !(softcap >= 0.f) || !(softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
     const PagedPlan p = paged_plan(dtype, d, Hq);
     const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-    if (join > 0x7FFFFFFFLL || Hq > 8192) return METOK_ERR_UNSUPPORTED;
+    if (join > 0x7FFFFFFFLL || Hq > 2048) return METOK_ERR_UNSUPPORTED;
     if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     PagedAttnArgs a;
     a.d = d;
