@@ -103,21 +103,54 @@ paged_append_kernel(const AppendArgs a) {
 }
 
 // ---- evict --------------------------------------------------------------------------
-// Three kernels.  claim: every page in use is claimed by one sequence; who meets a page claimed already, or out of range,
-// marks both sequences, which are then left alone.  select: a CTA per (layer, sequence) finds the rows that stay, pairs
-// the holes below the new length with the kept rows behind it, and moves their positions and mass.  move: K and V rows of
-// the pairs.  Sources lie at or beyond the new length and places below it, so no order is needed between them.
+// Two kernels.  select: a CTA per (layer, sequence) checks the sequence's pages against those of all others, finds the rows that
+// stay, pairs the holes below the new length with the kept rows behind it, and moves their positions and mass.  move: K and V
+// rows of the pairs, and the call's status.  Sources lie at or beyond the new length and places below it, so no order is needed
+// between them.
 struct EvictArgs {
     PagedDims d;
     int L, budget, n_sink, n_recent;
+    int claimed;                                       // the pages were claimed by a kernel of their own: bad[] is there already
+    int keys_fit;                                      // all keys of a sequence fit into the select kernel's shared memory
     const int32_t *block_table, *kv_len;
     int32_t* positions;
     float* mass;
     int32_t *keep_idx, *new_len, *status;
-    int32_t *claim, *bad;                              // [n_pages] and [n_seqs], zeroed before the first kernel
+    int32_t *claim, *bad;                              // [n_pages] and [n_seqs]
     int32_t *from, *to, *n_moved;                      // [L][n_seqs][budget] twice, [L][n_seqs]
 };
 
+// Whether a sequence may be touched: its length and pages are in range, no page is its own twice or another's.  A bit per page in
+// shared memory marks the sequence's own; then every other sequence's pages are looked up.
+constexpr int kEvictBitPages = 1 << 18;                // pages up to which that is done (32 KB); above, a kernel before it claims the pages
+__device__ __forceinline__ bool evict_sound(const EvictArgs& a, int b, uint32_t* s_bits) {
+    const int tid = threadIdx.x, nthr = blockDim.x, len = a.kv_len[b], page_rows = 1 << a.d.page_shift;
+    if (len < 0 || len > a.d.S_cap()) return false;    // uniform
+    const int used = (len + page_rows - 1) >> a.d.page_shift;
+    for (int w = tid; w < (a.d.n_pages + 31) / 32; w += nthr) s_bits[w] = 0u;
+    __syncthreads();
+    int bad = 0;
+    for (int p = tid; p < used; p += nthr) {
+        const int page = a.block_table[(size_t)b * a.d.max_pages + p];
+        if (page < 0 || page >= a.d.n_pages) bad = 1;
+        else if (atomicOr(&s_bits[page >> 5], 1u << (page & 31)) >> (page & 31) & 1u) bad = 1;
+    }
+    bad = __syncthreads_or(bad);
+    if (bad) return false;
+    // other sequences: a warp each
+    for (int s = tid >> 5; s < a.d.n_seqs; s += nthr >> 5) {
+        const int other = a.kv_len[s];
+        if (s == b || other <= 0 || other > a.d.S_cap()) continue;
+        const int n = (other + page_rows - 1) >> a.d.page_shift;
+        for (int p = tid & 31; p < n; p += 32) {
+            const int page = a.block_table[(size_t)s * a.d.max_pages + p];
+            if (page >= 0 && page < a.d.n_pages && (s_bits[page >> 5] >> (page & 31) & 1u)) bad = 1;
+        }
+    }
+    return !__syncthreads_or(bad);
+}
+
+// The same by claims in global memory: who meets a page claimed already marks both sequences.
 __global__ void __launch_bounds__(256)
 evict_claim_kernel(const EvictArgs a) {
     const int b = blockIdx.x, len = a.kv_len[b];
@@ -168,26 +201,25 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int n_sink, l
 }
 
 constexpr int kEvictBuckets = 2048;
+constexpr int kEvictKeys = 40960;                      // keys of a sequence that are kept in shared memory (160 KB)
 
 __global__ void __launch_bounds__(1024)
 evict_select_kernel(const EvictArgs a) {
     grid_dep_wait();
+    extern __shared__ uint32_t s_dyn[];                // the pages' bits, then the keys
     __shared__ uint32_t s_hist[kEvictBuckets];
     __shared__ int s_warp[32];
     __shared__ uint32_t s_prefix;
-    __shared__ int s_need;
+    __shared__ int s_need, s_all;
     const int b = blockIdx.x, layer = blockIdx.y, S_cap = a.d.S_cap(), tid = threadIdx.x, nthr = blockDim.x;
     const size_t prob = (size_t)layer * a.d.n_seqs + b;
     const int len = a.kv_len[b], n = min(len, a.budget);
-    const bool bad = a.bad[b] != 0;
+    const bool bad = a.claimed ? a.bad[b] != 0 : !evict_sound(a, b, s_dyn);
     int32_t* keep = a.keep_idx + prob * a.budget;
-    if (layer == 0 && b == 0) {                        // the call's status
-        int any = 0;
-        for (int s = tid; s < a.d.n_seqs; s += nthr) any |= a.bad[s];
-        any = __syncthreads_or(any);
-        if (tid == 0) *a.status = any ? METOK_ERR_INVALID_ARG : METOK_OK;
+    if (layer == 0 && tid == 0) {
+        a.new_len[b] = bad ? len : n;
+        a.bad[b] = bad;
     }
-    if (layer == 0 && tid == 0) a.new_len[b] = bad ? len : n;
     if (bad || len <= a.budget) {
         for (int i = tid; i < a.budget; i += nthr) keep[i] = !bad && i < n ? i : -1;
         if (tid == 0) a.n_moved[prob] = 0;
@@ -196,14 +228,17 @@ evict_select_kernel(const EvictArgs a) {
     int32_t* pos = a.positions + prob * S_cap;
     float* mass = a.mass + prob * S_cap;
     const long long recent_from = (long long)pos[len - 1] - a.n_recent;
-    auto key_of = [&](int i) { return evict_key(mass[i], pos[i], a.n_sink, recent_from); };
+    __syncthreads();                                   // the bits are done with
+    if (a.keys_fit)
+        for (int i = tid; i < len; i += nthr) s_dyn[i] = evict_key(mass[i], pos[i], a.n_sink, recent_from);
+    auto key_of = [&](int i) { return a.keys_fit ? s_dyn[i] : evict_key(mass[i], pos[i], a.n_sink, recent_from); };   // by the same thread
 
     // the n-th highest key, digit by digit from the top
     uint32_t prefix = 0u;                              // its digits so far
     int need = n, done = 0;                            // rows still to take among those with these digits; bits decided
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int bits = pass < 2 ? 11 : 10, shift = 32 - done - bits;
+    while (done < 32) {
+        const int bits = done < 22 ? 11 : 10, shift = 32 - done - bits;
         for (int i = tid; i < kEvictBuckets; i += nthr) s_hist[i] = 0u;
         __syncthreads();
         for (int i = tid; i < len; i += nthr) {
@@ -224,6 +259,7 @@ evict_select_kernel(const EvictArgs a) {
                 if (left <= c) {
                     s_prefix = (prefix << bits) | (uint32_t)(first - j);
                     s_need = left;
+                    s_all = left == c;
                     break;
                 }
                 left -= c;
@@ -233,8 +269,15 @@ evict_select_kernel(const EvictArgs a) {
         prefix = s_prefix;
         need = s_need;
         done += bits;
+        if (s_all) break;                              // all rows with these digits stay
         __syncthreads();
     }
+    // keys of at least `prefix` with zeros behind it stay; among equal ones (all digits decided) the first `need`
+    if (done < 32) {
+        prefix <<= 32 - done;
+        need = len;
+    }
+    const bool by_order = done == 32;
 
     // rows in order: above the threshold, or among the first `need` equal to it, they stay
     int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget;
@@ -244,9 +287,11 @@ evict_select_kernel(const EvictArgs a) {
         const int i = base + tid;
         const uint32_t k = i < len ? key_of(i) : 0u;
         const bool eq = i < len && k == prefix;
-        int total;
-        const int eq_before = equal + block_scan(eq, s_warp, &total);
-        equal += total;
+        int total, eq_before = 0;
+        if (by_order) {
+            eq_before = equal + block_scan(eq, s_warp, &total);
+            equal += total;
+        }
         const bool stay = i < len && (k > prefix || (eq && eq_before < need));
         const bool hole = i < n && !stay, mover = i >= n && stay;
         const int x = block_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), s_warp, &total);   // at most 1024 of each
@@ -273,12 +318,18 @@ constexpr int kEvictPtrLayers = 64;                    // layers per launch of t
 struct EvictPools {
     uint4 *k[kEvictPtrLayers], *v[kEvictPtrLayers];
 };
-constexpr int kMoveThreads = 256, kMoveUnroll = 4;
+constexpr int kMoveThreads = 256, kMoveUnroll = 4, kMoveMostCtas = 1 << 15;
 
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(const EvictArgs a, const EvictPools pools, int layer0) {
     grid_dep_wait();
     const int ll = blockIdx.y / a.d.n_seqs, b = blockIdx.y - ll * a.d.n_seqs;
+    if (layer0 == 0 && blockIdx.x == 0 && blockIdx.y == 0) {             // the call's status
+        int any = 0;
+        for (int s = threadIdx.x; s < a.d.n_seqs; s += kMoveThreads) any |= a.bad[s];
+        any = __syncthreads_or(any);
+        if (threadIdx.x == 0) *a.status = any ? METOK_ERR_INVALID_ARG : METOK_OK;
+    }
     const size_t prob = (size_t)(layer0 + ll) * a.d.n_seqs + b;
     const int n = a.n_moved[prob], cpr = a.d.row_chunks, per_row = 2 * a.d.Hkv * cpr;
     const int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget, *table = a.block_table + (size_t)b * a.d.max_pages;
@@ -395,22 +446,28 @@ extern "C" int metok_paged_evict(int dtype, const metok_paged_cache* c, void* co
     Carver cv(ws);
     evict_carve(cv, d, L, budget, &a);
     cudaStream_t st = (cudaStream_t)stream;
-    METOK_CUDA_TRY(cudaMemsetAsync(a.claim, 0, ((size_t)d.n_pages + d.n_seqs) * sizeof(int32_t), st));
-    {
+    a.claimed = d.n_pages > kEvictBitPages;
+    a.keys_fit = d.S_cap() <= kEvictKeys;
+    if (a.claimed) {
+        METOK_CUDA_TRY(cudaMemsetAsync(a.claim, 0, ((size_t)d.n_pages + d.n_seqs) * sizeof(int32_t), st));
         METOK_TIMED("evict_claim", st);
         evict_claim_kernel<<<d.n_seqs, 256, 0, st>>>(a);
+        METOK_LAUNCH_CHECK();
     }
-    METOK_LAUNCH_CHECK();
     {
+        const size_t smem = std::max(a.claimed ? 0 : (size_t)(d.n_pages + 31) / 32 * 4, a.keys_fit ? (size_t)d.S_cap() * 4 : 0);
+        METOK_ALLOW_SMEM(evict_select_kernel, smem);
         METOK_TIMED("evict_select", st);
         const int threads = std::min(1024, std::max(128, ceil_div(d.S_cap(), 32) * 32));
-        launch_chained(evict_select_kernel, dim3(d.n_seqs, L), dim3(threads), 0, st, a);
+        launch_chained(evict_select_kernel, dim3(d.n_seqs, L), dim3(threads), smem, st, a);
     }
     METOK_LAUNCH_CHECK();
-    // pairs of a problem: at most the rows behind the new length, and the places below it
+    // A CTA per 16 KB of the most pairs that a problem can have (the rows behind the new length, or the places below it): how many there
+    // are is known on the device alone, and what has no work ends at once.  (A fixed share of the SMs per problem left them idle beside the
+    // longest: 28 layers of 4 sequences of 1184 to 4736 rows 113 us the call, 1263 kept.)
     const long long most = (long long)std::min(budget, d.S_cap() - budget) * 2 * d.Hkv * d.row_chunks;
     const long long blocks = std::max(1LL, std::min((most + kMoveThreads * kMoveUnroll - 1) / (kMoveThreads * kMoveUnroll),
-                                                    (long long)ceil_div(kNumSMs * 8, L * d.n_seqs)));
+                                                    (long long)kMoveMostCtas / (std::min(L, kEvictPtrLayers) * d.n_seqs)));
     for (int l0 = 0; l0 < L; l0 += kEvictPtrLayers) {
         const int nl = std::min(kEvictPtrLayers, L - l0);
         EvictPools pools = {};

@@ -72,7 +72,7 @@ def test_attention_refuses(lib):
                dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")),
                dict(status=None), dict(slopes=p0 + 1), dict(mass=p0 + 2)]:
         assert call(**kw) == (-1, 0), kw
-    assert call(Hq=8194) == (-2, 0)
+    assert call(Hq=2050) == (-2, 0)
     assert call(ws=None) == (-3, 0) and call(ws_bytes=64) == (-3, 0)
     c = cache()
     size = lambda hq, mass: lib.metok_paged_attention_workspace_bytes(B.BF16, ctypes.byref(c), hq, mass)
