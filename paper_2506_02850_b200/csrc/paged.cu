@@ -333,7 +333,8 @@ evict_move_kernel(const EvictArgs a, const EvictPools pools, int layer0) {
     const size_t prob = (size_t)(layer0 + ll) * a.d.n_seqs + b;
     const int n = a.n_moved[prob], cpr = a.d.row_chunks, per_row = 2 * a.d.Hkv * cpr;
     const int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget, *table = a.block_table + (size_t)b * a.d.max_pages;
-    const long long total = (long long)n * per_row;
+    // pair after pair of one head of K or V: neighbours in a page follow one another
+    const long long total = (long long)n * per_row, slab = (long long)n * cpr;
     for (long long g0 = (long long)blockIdx.x * (kMoveThreads * kMoveUnroll) + threadIdx.x; g0 < total;
          g0 += (long long)gridDim.x * (kMoveThreads * kMoveUnroll)) {
         uint4 v[kMoveUnroll];
@@ -343,7 +344,7 @@ evict_move_kernel(const EvictArgs a, const EvictPools pools, int layer0) {
             const long long g = g0 + u * kMoveThreads;
             dst[u] = nullptr;
             if (g >= total) continue;
-            const int r = (int)(g / per_row), e = (int)(g - (long long)r * per_row), hh = e / cpr, c = e - hh * cpr;
+            const int hh = (int)(g / slab), e = (int)(g - (long long)hh * slab), r = e / cpr, c = e - r * cpr;
             const int h = hh >= a.d.Hkv ? hh - a.d.Hkv : hh, s = from[r], t = to[r];
             uint4* pool = hh >= a.d.Hkv ? pools.v[ll] : pools.k[ll];
             dst[u] = pool + paged_chunk(a.d, table[t >> a.d.page_shift], h, t) + c;
