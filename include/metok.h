@@ -434,7 +434,8 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   given strides in ELEMENTS between heads and between rows (so token-major
  *   projections and caches with room behind their rows need no copy); elements of
  *   a row are contiguous.  DEVICE, 16-byte aligned; strides are multiples of 16
- *   bytes, row strides >= dh; rows of `out` do not overlap, and out overlaps no input.
+ *   bytes, row strides >= dh, as those between the heads of q and out (k and v may have 0
+ *   there: one K/V head for all); rows of `out` do not overlap, and out overlaps no input.
  *   seq_q, seq_k DEVICE int32 [n_seq+1], prefix_len DEVICE int32 [n_seq], positions
  *   DEVICE int32 [n_k], slopes DEVICE float [Hq], lse DEVICE float [Hq][n_q]: 4-byte
  *   aligned; all but q, k, v, out may be NULL.  seq_q and seq_k are both NULL for one
@@ -451,7 +452,7 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1 (n_q, n_k may be 0),
  *   Hq % Hkv, strides, softmax_scale not finite or <= 0, softcap < 0 or not finite, one of
  *   seq_q / seq_k without the other, n_seq != 1 without them); UNSUPPORTED (dh other
- *   than 64 or 128, more than 2^24 rows, n_seq > 65536, Hq > 65535, more than 2^31 - 1 pieces of work);
+ *   than 64 or 128, more than 2^24 rows, n_seq > 8192, Hq > 65535, more than 2^31 - 1 pieces of work);
  *   WORKSPACE.
  * ------------------------------------------------------------------------- */
 typedef struct {

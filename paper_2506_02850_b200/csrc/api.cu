@@ -116,11 +116,11 @@ int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows,
     const cuuint32_t box[2] = {128 / esize, box_rows};
     return encode_tmap(out, dtype, base, 2, dims, strides, box);
 }
-int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t row_stride, uint64_t head_stride,
-                    uint32_t box_rows) {
-    const cuuint64_t dims[3] = {cols, rows, heads};
-    const cuuint64_t strides[2] = {row_stride * 2, (heads > 1 ? head_stride : row_stride) * 2};
-    const cuuint32_t box[3] = {64, box_rows, 1};
+int make_tmap_3d(CUtensorMap* out, const void* base, uint64_t cols, uint64_t n1, uint64_t n2, uint64_t stride1, uint64_t stride2, uint32_t b1,
+                 uint32_t b2) {
+    const cuuint64_t dims[3] = {cols, n1, n2};
+    const cuuint64_t strides[2] = {stride1 * 2, stride2 * 2};
+    const cuuint32_t box[3] = {64, b1, b2};
     return encode_tmap(out, METOK_BF16, base, 3, dims, strides, box);
 }
 int make_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {

@@ -54,7 +54,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
     for (int i = 0; i < 4; ++i) {
         const int r = i0 + ty * 4 + i;
         keys[i] = ty * 4 + i < rows ? prompt_keys(a, d, r) : 0;
-        my_pos[i] = a.slopes ? prompt_position(a, d, d.Lk - d.Lq + r) : 0.f;
+        my_pos[i] = a.slopes ? prompt_position(a, d.k0, d.Lk, d.Lk - d.Lq + r) : 0.f;
         m[i] = __int_as_float(0xFF800000);
         l[i] = 0.f;
 #pragma unroll
@@ -79,7 +79,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
                 *reinterpret_cast<float4*>(&sm.v[r][e + i]) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
             }
         }
-        if (a.slopes && tid < kSN) sm.pos[tid] = prompt_position(a, d, j0 + tid);
+        if (a.slopes && tid < kSN) sm.pos[tid] = prompt_position(a, d.k0, d.Lk, j0 + tid);
         __syncthreads();
         float s[4][4];
 #pragma unroll
@@ -210,49 +210,40 @@ prompt_join_kernel(const PromptArgs a) {
     if (lane == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (M + log2f(L));
 }
 
+// fp32: CTAs without splits, and splits of the keys.
 struct PromptPlan {
-    long long ctas;                                    // without splits
+    long long ctas;
     int splits;
 };
-// CUDA cores: tiles of all documents, at most a started one more per document than whole ones fit into n_q.
-PromptPlan prompt_plan(int dtype, const metok_attention_params* p) {
+// Tiles of all documents: at most a started one more per document than whole ones fit into n_q.
+PromptPlan prompt_plan(const metok_attention_params* p) {
     PromptPlan pl;
-    long long room, part;                              // CTAs that run at once; fewest keys of a part
-    if (dtype == METOK_BF16) {
-        pl.ctas = prompt_mma_ctas(p->Hkv, p->Hq / p->Hkv, p->n_q, p->n_seq);
-        room = kNumSMs;
-        part = 256;
-    } else {
-        pl.ctas = std::max(1LL, (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q)) * p->Hq;
-        room = 2 * kNumSMs;
-        part = 4 * kSN;
-    }
-    // few rows: the keys are cut until every SM has work
-    pl.splits = (int)std::max(1LL, std::min({p->n_k / part, room / pl.ctas, 64LL}));
+    pl.ctas = std::max(1LL, (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q)) * p->Hq;
+    // few rows: the keys are cut until every SM has work, no part shorter than four tiles
+    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (4 * kSN), 2 * kNumSMs / pl.ctas, 64LL}));
     return pl;
 }
-void prompt_carve(Carver& cv, const metok_attention_params* p, int splits, PromptArgs* a) {
+void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, PromptArgs* a) {
+    if (dtype == METOK_BF16) return prompt_mma_carve(cv, p->dh, a);
+    const int splits = prompt_plan(p).splits;
     if (splits == 1) return;
     const size_t rows = (size_t)splits * p->Hq * p->n_q;
     a->part_o = cv.take<float>(rows * p->dh);
     a->part_ml = cv.take<float>(rows * 2);
 }
 
-template <typename T, int DH>
-int launch_prompt(const PromptArgs& a, const PromptPlan& pl, cudaStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        const int rc = launch_prompt_attn_mma(a, DH, pl.ctas, st);
-        if (rc != METOK_OK) return rc;
-    } else {
-        auto kern = prompt_attn_simt_kernel<DH>;
-        METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<DH>));
+template <int DH>
+int launch_prompt_simt(const PromptArgs& a, const PromptPlan& pl, cudaStream_t st) {
+    auto kern = prompt_attn_simt_kernel<DH>;
+    METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<DH>));
+    {
         METOK_TIMED("prompt_attn_simt", st);
         launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<DH>), st, a);
-        METOK_LAUNCH_CHECK();
     }
+    METOK_LAUNCH_CHECK();
     if (pl.splits > 1) {
         METOK_TIMED("prompt_join", st);
-        launch_chained(prompt_join_kernel<T, DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
+        launch_chained(prompt_join_kernel<float, DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
         METOK_LAUNCH_CHECK();
     }
     return METOK_OK;
@@ -263,8 +254,8 @@ int prompt_check(int dtype, const metok_attention_params* p) {
     if (p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv || p->dh < 1 || p->n_q < 0 || p->n_k < 0 || p->n_seq < 1) return METOK_ERR_INVALID_ARG;
     if (!p->seq_q != !p->seq_k || (!p->seq_q && p->n_seq != 1)) return METOK_ERR_INVALID_ARG;
     if (p->dh != 64 && p->dh != 128) return METOK_ERR_UNSUPPORTED;
-    if (p->n_q > (1 << 24) || p->n_k > (1 << 24) || p->n_seq > 65536 || p->Hq > 65535) return METOK_ERR_UNSUPPORTED;
-    if (prompt_plan(dtype, p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    if (p->n_q > (1 << 24) || p->n_k > (1 << 24) || p->n_seq > kPromptDocs || p->Hq > 65535) return METOK_ERR_UNSUPPORTED;
+    if (dtype == METOK_F32 && prompt_plan(p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     return METOK_OK;
 }
 
@@ -277,7 +268,7 @@ extern "C" size_t metok_prefill_attention_workspace_bytes(int dtype, const metok
     if (prompt_check(dtype, p) != METOK_OK) return 0;
     PromptArgs a;
     Carver cv(nullptr);
-    prompt_carve(cv, p, prompt_plan(dtype, p).splits, &a);
+    prompt_carve(cv, dtype, p, &a);
     return cv.total();
 }
 
@@ -293,12 +284,11 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     const int per = 16 / (dtype == METOK_F32 ? 4 : 2);
     if (p->q_head < 0 || p->k_head < 0 || p->v_head < 0 || p->out_head < 0) return METOK_ERR_INVALID_ARG;
     if (p->q_row < p->dh || p->k_row < p->dh || p->v_row < p->dh || p->out_row < p->dh) return METOK_ERR_INVALID_ARG;
-    if (p->Hq > 1 && p->out_head < p->dh) return METOK_ERR_INVALID_ARG;
+    if (p->Hq > 1 && (p->q_head < p->dh || p->out_head < p->dh)) return METOK_ERR_INVALID_ARG;
     if ((p->q_head | p->k_head | p->v_head | p->out_head | p->q_row | p->k_row | p->v_row | p->out_row) % per) return METOK_ERR_INVALID_ARG;
     if (!(p->softmax_scale > 0.f) || !(p->softmax_scale < 3.0e38f) || !(p->softcap >= 0.f) || !(p->softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
     const size_t need = metok_prefill_attention_workspace_bytes(dtype, p);
     if (need > 0 && (!ws || !aligned16(ws) || ws_bytes < need)) return METOK_ERR_WORKSPACE;
-    const PromptPlan pl = prompt_plan(dtype, p);
     PromptArgs a = {};
     a.q = p->q; a.k = p->k; a.v = p->v; a.out = p->out; a.lse = p->lse;
     a.q_head = p->q_head; a.q_row = p->q_row; a.k_head = p->k_head; a.k_row = p->k_row;
@@ -309,12 +299,12 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     a.cap_scale = p->softcap > 0.f ? p->softmax_scale / p->softcap : 0.f;
     a.cap_log2 = p->softcap * kAttnLog2e;
     a.causal = p->causal != 0;
-    a.splits = pl.splits;
     a.status = status;
     Carver cv(ws);
-    prompt_carve(cv, p, pl.splits, &a);
+    prompt_carve(cv, dtype, p, &a);
     cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == METOK_BF16)
-        return p->dh == 64 ? launch_prompt<__nv_bfloat16, 64>(a, pl, st) : launch_prompt<__nv_bfloat16, 128>(a, pl, st);
-    return p->dh == 64 ? launch_prompt<float, 64>(a, pl, st) : launch_prompt<float, 128>(a, pl, st);
+    if (dtype == METOK_BF16) return launch_prompt_attn_mma(a, p->dh, st);
+    const PromptPlan pl = prompt_plan(p);
+    a.splits = pl.splits;
+    return p->dh == 64 ? launch_prompt_simt<64>(a, pl, st) : launch_prompt_simt<128>(a, pl, st);
 }

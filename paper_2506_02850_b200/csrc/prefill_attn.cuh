@@ -17,14 +17,18 @@ struct PromptArgs {
     const float* slopes;
     float scale_log2, cap_scale, cap_log2;     // softcap > 0: x = cap_log2 * tanh(dot * cap_scale); else cap_log2 is 0 (log2 units)
     int causal;
-    int splits;                                // parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
-    float *part_o, *part_ml;                   // [splits][Hq][n_q][dh] unnormalised outputs, [splits][Hq][n_q] (maximum, sum)
+    int splits;                                // fp32: parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
+    int heads_item, head_chunks;               // bf16: query heads of a tile of 128 rows, such tiles for all heads of a K/V head
+    float *part_o, *part_ml;                   // unnormalised outputs and (maximum, sum) of the parts; fp32: [splits][Hq][n_q]
+    void* cuts;                                // bf16: what the second kernel joins
     int32_t* status;
 };
 
-// The tensor-core kernel (bf16): CTAs without splits, and the launch.
-long long prompt_mma_ctas(int Hkv, int G, int n_q, int n_seq);
-int launch_prompt_attn_mma(const PromptArgs& a, int dh, long long ctas, cudaStream_t st);
+constexpr int kPromptDocs = 8192;              // documents at most
+
+// The tensor-core kernels (bf16): their workspace, and the launch.
+void prompt_mma_carve(Carver& cv, int dh, PromptArgs* a);
+int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st);
 
 struct PromptDoc {
     int q0, k0, Lq, Lk, prefix;
@@ -95,10 +99,10 @@ __device__ __forceinline__ PromptDoc prompt_tile(const PromptArgs& a, int at, Ti
     return d;
 }
 
-// Position of a document's key (or of the query that sits there).
-__device__ __forceinline__ float prompt_position(const PromptArgs& a, const PromptDoc& d, int j) {
-    j = max(0, min(j, d.Lk - 1));
-    return (float)(a.positions ? a.positions[d.k0 + j] : j);
+// Position of key j of the document whose Lk keys begin at k0 (or of the query that sits there).
+__device__ __forceinline__ float prompt_position(const PromptArgs& a, int k0, int Lk, int j) {
+    j = max(0, min(j, Lk - 1));
+    return (float)(a.positions ? a.positions[k0 + j] : j);
 }
 
 }  // namespace metok

@@ -1,19 +1,25 @@
 // metok_prefill_attention on the tensor cores (bf16).
 //
-// A CTA works on two tiles of 128 query rows of one K/V head: the tiles of a document's query heads of the group are dealt
-// out in pairs (tile by tile, head by head), so that both use the same K and V tiles, and for few rows the heads of a group
-// share a read of the keys.  Per tile of 128 keys and query tile x:
+// An item is a tile of 128 query rows: 128 / G consecutive rows of a document with all G query heads of one K/V head, so that
+// few rows fill a tile too, and a tile's rows end at nearly the same key.  A CTA works on two items side by side (a pair: neighbours
+// in the document), which use the same K and V tiles.  Per tile of 128 keys and item x:
 //   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, fp32 in tensor memory (128 columns)
 //   P_x = 2^(logit - m)  one thread per row; bf16, written over S_x in tensor memory (64 columns)
 //   O_x += P_x V         tcgen05.mma, P_x from tensor memory, V as it lies (keys x dh: the second operand's other order)
-// S_0, S_1, O_0 and O_1 fill the 512 columns.  While one tile's rows are in their exponentials the other's products run.
+// S_0, S_1, O_0 and O_1 fill the 512 columns.  While one item's rows are in their exponentials the other's products run.
 //
-// Key tiles are taken from the last one down.  A row's reference m is the maximum of the first tile that it sees; later tiles' weights are taken against it with no maximum of their own,
-// since any m within the range of the exponent gives the same result.  Where the sum of 64 weights leaves that range they are
-// made again against their own maximum, and O_x and the sum are scaled: by the row's own thread, when the products
-// before on O_x are complete (one thread issues all of them, in order).
+// The key tiles of all pairs of all documents and K/V heads form one line, and every CTA (one per SM) takes an equal piece of it:
+// a piece may begin and end inside a pair, whose parts are then joined by a second kernel.  So a batch of documents of any lengths,
+// few rows over many keys and a number of pairs that is no multiple of the SMs all keep every SM busy to the end.  Every CTA finds its
+// piece by itself, from the documents' offsets.
 //
-// Warps 0-3 and 4-7: the rows of tiles 0 and 1; warp 8: TMA; warp 9: products.  Every wait is bounded.  A row's 128 logits are read
+// Key tiles of a pair are taken from the last one down.  A row's reference m is the maximum of the first tile that it sees; later tiles'
+// weights are taken against it with no maximum of their own, since any m within the range of the exponent gives the same
+// result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x and the sum are
+// scaled: by the row's own thread, when the products before on O_x are complete (one thread issues all of them, in order).
+//
+// Warps 0-3 and 4-7: the rows of items 0 and 1; warp 8: TMA; warps 9 and 10: the products of items 0 and 1, each with waits of its
+// own (an issuing warp is held up while products run, so one warp's waits for both items lie open).  Every wait is bounded.  A row's 128 logits are read
 // from tensor memory 32 at a time: held in registers they spill.
 #include <algorithm>
 
@@ -25,8 +31,10 @@ namespace metok {
 
 namespace {
 
-constexpr int kM = 128, kN = 128, kThreads = 320;
+constexpr int kM = 128, kN = 128, kThreads = 352;
 constexpr float kMost = 1.0e18f, kRoom = 32.f;         // sum of 64 weights beyond which a row's reference grows, and by how many octaves above their maximum
+
+constexpr int kFewest = 2;                             // steps of the line that a CTA is given at least, on average
 
 template <int DH>
 struct MmaShape {
@@ -52,26 +60,19 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// D[tmem] (+)= A[tmem] * B[smem], issued by ONE thread.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// D[tmem] (+)= A[tmem] * B[smem], issued by ONE thread; the descriptor's upper word is that of umma_bf16_words.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(sm100::desc_k128_hi())
         : "memory");
 }
-// Descriptor of V as the second operand in its other order: a tile lies as rows (keys) of 128 swizzled bytes = 64 columns of
-// the product; the next 64 columns follow kBlk bytes on (leading offset), the next eight keys 1024 bytes on (stride).
-__device__ __forceinline__ uint64_t desc_v(uint32_t smem_addr, uint32_t blk_bytes) {
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(blk_bytes >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
+// Lower word of V's descriptor as the second operand in its other order: a tile lies as rows (keys) of 128 swizzled bytes = 64 columns of
+// the product; the next 64 columns follow blk_bytes on (leading offset), the next eight keys 1024 bytes on (stride, as in K's).
+__device__ __forceinline__ uint32_t desc_v_lo(uint32_t smem_addr, uint32_t blk_bytes) { return ((smem_addr & 0x3FFFFu) >> 4) | ((blk_bytes >> 4) << 16); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -86,7 +87,80 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 struct MmaMaps {
     CUtensorMap q, k, v;
-    int q_step, k_step, v_step;                        // 1, or 0 where all heads are the same rows
+    int k_step, v_step;                                // 1, or 0 where all K/V heads are the same rows
+};
+
+// How rows and heads make items.
+__device__ __forceinline__ int item_rows(const PromptArgs& a) { return a.heads_item < kM ? kM / a.heads_item : 1; }
+
+// A pair's place in its document, and what its items need.
+struct Pair {
+    int i0[2], h0[2], rows[2], n[2];                   // first row, first head (of the K/V head's), rows of the tile in use, key tiles
+    int nt;                                            // key tiles of the pair
+};
+__device__ __forceinline__ int doc_items(const PromptArgs& a, int Lq) {
+    const int r = item_rows(a);
+    return (Lq + r - 1) / r * a.head_chunks;
+}
+__device__ __forceinline__ Pair pair_of(const PromptArgs& a, const PromptDoc& d, int t) {
+    Pair p;
+    const int r = item_rows(a), items = doc_items(a, d.Lq);
+    p.nt = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int item = 2 * t + x;
+        const bool there = item < items;
+        const int blk = there ? item / a.head_chunks : 0, ch = there ? item - blk * a.head_chunks : 0;
+        p.i0[x] = blk * r;
+        p.h0[x] = ch * a.heads_item;
+        const int nr = there ? min(r, d.Lq - p.i0[x]) : 0;
+        p.rows[x] = nr * a.heads_item;
+        p.n[x] = there ? (prompt_keys(a, d, p.i0[x] + nr - 1) + kN - 1) / kN : 0;
+        p.nt = max(p.nt, p.n[x]);
+    }
+    return p;
+}
+// Steps of a pair in the line: its key tiles, and one where it has none.
+__device__ __forceinline__ int pair_steps(const PromptArgs& a, const PromptDoc& d, int t) {
+    const int last = min(2 * t + 1, doc_items(a, d.Lq) - 1) / a.head_chunks, r = item_rows(a);
+    return max(1, (prompt_keys(a, d, min(d.Lq, (last + 1) * r) - 1) + kN - 1) / kN);
+}
+__device__ __forceinline__ int doc_pairs(const PromptArgs& a, int Lq) { return (doc_items(a, Lq) + 1) / 2; }
+
+// A CTA's way along the line, pair by pair; the same in every warp.
+struct Walk {
+    PromptDoc d;
+    int doc, g, t, pairs;                              // document, K/V head, pair, pairs of the document
+    int e0;                                            // first step of the pair that is this CTA's
+    long long left;                                    // steps still to do
+};
+__device__ __forceinline__ PromptDoc doc_of(const PromptArgs& a, int s) {
+    PromptDoc d = {0, 0, a.n_q, a.n_k, a.prefix_len ? a.prefix_len[s] : 0, 0};
+    if (a.seq_q) {
+        d.q0 = a.seq_q[s];
+        d.k0 = a.seq_k[s];
+        d.Lq = a.seq_q[s + 1] - d.q0;
+        d.Lk = a.seq_k[s + 1] - d.k0;
+    }
+    return d;
+}
+// Past the `steps` steps of this CTA's piece of the pair.
+__device__ __forceinline__ void walk_on(const PromptArgs& a, Walk& w, int steps) {
+    w.left -= steps;
+    w.e0 = 0;
+    if (w.left <= 0 || ++w.t < w.pairs) return;
+    w.t = 0;
+    do {                                               // steps are left: a document with rows comes
+        if (++w.doc == a.n_seq) { w.doc = 0; ++w.g; }
+        w.d = doc_of(a, w.doc);
+        w.pairs = doc_pairs(a, w.d.Lq);
+    } while (w.pairs == 0 && w.g < a.Hkv);
+}
+
+// What the second kernel joins: the parts of the pair that CTAs c0 .. c1 share, noted by CTA c0 + 1.
+struct Cut {
+    int c0, c1, first_slot;                            // c1 < 0: nothing; slot of CTA c0's part (the others' are their first ones)
+    int q0, g, Lq, i0[2], h0[2], rows[2];
 };
 
 template <int DH, bool kCap, bool kBias>
@@ -96,50 +170,119 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     using S = MmaShape<DH>;
     grid_dep_wait();
     extern __shared__ uint8_t smem_dyn[];
-    __shared__ __align__(8) uint64_t q_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], h_bar[2], o_bar[2], drain_bar;
+    __shared__ __align__(8) uint64_t q_bar, q_free_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], h_bar[2], o_bar[2], o_free_bar[2], drain_bar[2];
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort;
-    __shared__ __align__(16) float s_pos[2][2][kN];    // [tile][buffer]: positions of the keys
+    __shared__ __align__(16) float s_pos[2][2][kN];    // [item][buffer]: positions of the keys
+    __shared__ Walk s_walk[8];                         // the rows' warps keep their way along the line here: in registers it would cost spills
+    __shared__ int s_at[4];
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int g = blockIdx.x % a.Hkv;
-    const int G = a.G;
-    const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hkv, [G](int Lq) { return (int)(((long long)((Lq + kM - 1) / kM) * G + 1) / 2); });
-    if (d.tile < 0) return;                            // uniform
-
-    // the pair's items: 2 t and 2 t + 1 of the document's (tile, head) pairs
-    const int n_items = (d.Lq + kM - 1) / kM * G;
-    int i0[2], head[2], rows[2], lo = 0, n[2] = {0, 0};   // first row, query head, rows, key tiles of each item
-    int hi = 0;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int item = 2 * d.tile + x;
-        const bool there = item < n_items;
-        const int t = there ? item / G : 0;
-        i0[x] = t * kM;
-        head[x] = g * G + (there ? item - t * G : 0);
-        rows[x] = there ? min(kM, d.Lq - i0[x]) : 0;
-        n[x] = there ? (prompt_keys(a, d, i0[x] + rows[x] - 1) + kN - 1) / kN : 0;
-        hi = max(hi, n[x]);
-    }
-    if (a.splits > 1) {
-        const int all = hi;
-        lo = (int)((long long)all * blockIdx.y / a.splits);
-        hi = (int)((long long)all * (blockIdx.y + 1) / a.splits);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) n[x] = max(0, min(n[x], hi) - lo);
-    // key tiles lo + nt - 1 down to lo: the nearest ones first, which a bias makes the largest; item x joins in at step st[x]
-    const int nt = max(n[0], n[1]), st[2] = {nt - n[0], nt - n[1]};
-    auto tile_key = [&](int j) { return (lo + nt - 1 - j) * kN; };
-
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     auto q_addr = [&](int x) { return smem_base + (uint32_t)x * S::kTile; };
     auto kv_addr = [&](int s) { return smem_base + (uint32_t)(2 + s) * S::kTile; };
+    Cut* cuts = reinterpret_cast<Cut*>(a.cuts);
+
+    // ---- the line: steps of the documents before each (the tiles' memory serves for it), then this CTA's piece
+    long long* s_pre = reinterpret_cast<long long*>(smem_dyn + (kv_addr(0) - smem_u32(smem_dyn)));
+    int bad = 0;
+    for (int s = threadIdx.x; a.seq_q && s < a.n_seq; s += kThreads) {
+        const int q0 = a.seq_q[s], q1 = a.seq_q[s + 1], k0 = a.seq_k[s], k1 = a.seq_k[s + 1];
+        bad |= q0 < 0 || q1 < q0 || q1 > a.n_q || k0 < 0 || k1 < k0 || k1 > a.n_k;
+    }
+    if (a.seq_q) bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+        if (blockIdx.x == 0) *a.status = bad ? METOK_ERR_INVALID_ARG : METOK_OK;
+        cuts[blockIdx.x].c1 = -1;
+    }
+    if (bad) return;
+    for (int s = warp; s < a.n_seq; s += kThreads / 32) {
+        const PromptDoc d = doc_of(a, s);
+        const int pairs = doc_pairs(a, d.Lq);
+        long long sum = 0;
+        for (int t = lane; t < pairs; t += 32) sum += pair_steps(a, d, t);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == 0) s_pre[s + 1] = sum;
+    }
+    if (threadIdx.x == 0) s_pre[0] = 0;
+    __syncthreads();
+    if (warp == 0 && a.n_seq > 1) {                    // running sums, a run of documents per lane
+        const int per = (a.n_seq + 31) / 32, s0 = lane * per, s1 = min(a.n_seq, s0 + per);
+        long long sum = 0;
+        for (int s = s0; s < s1; ++s) sum += s_pre[s + 1];
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        long long run = incl - sum;
+        for (int s = s0; s < s1; ++s) {
+            run += s_pre[s + 1];
+            s_pre[s + 1] = run;
+        }
+    }
+    __syncthreads();
+    const long long per_head = s_pre[a.n_seq], all = per_head * a.Hkv;
+    const long long ctas = max(1LL, min((long long)gridDim.x, all / kFewest));
+    if (blockIdx.x >= ctas || all == 0) return;        // uniform
+    const long long begin = all * blockIdx.x / ctas, end = all * (blockIdx.x + 1) / ctas;
+    if (warp == 0) {
+        const int g = (int)(begin / per_head);
+        const long long at = begin - g * per_head;
+        int lo = 0, hi = a.n_seq;                      // the document: s_pre[lo] <= at < s_pre[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_pre[mid] <= at) lo = mid;
+            else hi = mid;
+        }
+        const PromptDoc d = doc_of(a, lo);
+        const int pairs = doc_pairs(a, d.Lq);
+        int rest = 0;
+        long long before = s_pre[lo];
+        int t0 = 0;
+        for (; t0 < pairs; t0 += 32) {
+            const int mine = t0 + lane < pairs ? pair_steps(a, d, t0 + lane) : 0;
+            int incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            const uint32_t any = __ballot_sync(0xFFFFFFFFu, before + incl > at);
+            if (any) {
+                const int l = __ffs(any) - 1;
+                rest = (int)(at - before) - __shfl_sync(0xFFFFFFFFu, incl - mine, l);
+                t0 += l;
+                break;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        }
+        if (lane == 0) {
+            s_at[0] = g;
+            s_at[1] = lo;
+            s_at[2] = t0;
+            s_at[3] = rest;
+        }
+    }
+    fence_proxy_async();                               // what was written here by threads, before copies write it
+    __syncthreads();
+    Walk walk;
+    walk.g = s_at[0];
+    walk.doc = s_at[1];
+    walk.t = s_at[2];
+    walk.e0 = s_at[3];
+    walk.d = doc_of(a, walk.doc);
+    walk.pairs = doc_pairs(a, walk.d.Lq);
+    walk.left = end - begin;
+
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&q_bar), 1);
-        mbar_init(smem_u32(&drain_bar), 1);
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); mbar_init(smem_u32(&h_bar[x]), 1); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
+        mbar_init(smem_u32(&q_free_bar), 2);
+        mbar_init(smem_u32(&drain_bar[0]), 1);
+        mbar_init(smem_u32(&drain_bar[1]), 1);
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 2); }
+        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); mbar_init(smem_u32(&h_bar[x]), 1); mbar_init(smem_u32(&o_free_bar[x]), 4); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
         s_abort = 0;
         mbar_fence_init();
     }
@@ -153,149 +296,219 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem_base, 0);
     volatile int* abort_flag = &s_abort;
 
+    // this CTA's part of the walk's pair: steps e0 .. e1 - 1, which are key tiles lo + nt - 1 down to lo; item x joins in at step st[x]
+    struct Part {
+        Pair p;
+        int steps, e1, lo, nt, st[2];
+        bool whole;
+    };
+    auto part_of = [&](const Walk& w) {
+        Part q;
+        q.p = pair_of(a, w.d, w.t);
+        const int steps = max(1, q.p.nt);
+        q.steps = (int)min((long long)(steps - w.e0), w.left);
+        q.e1 = w.e0 + q.steps;
+        q.whole = q.steps == steps;
+        q.lo = max(0, q.p.nt - q.e1);
+        q.nt = q.p.nt ? q.steps : 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) q.st[x] = q.nt - max(0, min(q.p.n[x] - q.lo, q.nt));
+        return q;
+    };
+    auto tile_key = [](int top, int j) { return (top - j) * kN; };       // `top`: the part's highest key tile
+    // (into the warp's uniform registers, which a product's descriptors are made in)
+    auto uniform = [](int v) { return __reduce_max_sync(0xFFFFFFFFu, v); };
+
     if (warp == 8) {
-        // ---- TMA: Q of both items, then K and V tiles in turn
-        int it = 0;
-        if (nt > 0) {
-            if (elect_one()) {
-                prefetch_tmap(&maps.k);
-                prefetch_tmap(&maps.v);
-                const int both = rows[1] > 0 ? 2 : 1;
-                mbar_arrive_expect_tx(smem_u32(&q_bar), (uint32_t)both * S::kTile);
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (x < both) {
-#pragma unroll
-                        for (int kb = 0; kb < S::KB; ++kb)
-                            tma_load_3d(q_addr(x) + kb * S::kBlk, &maps.q, kb * 64, d.q0 + i0[x], head[x] * maps.q_step, smem_u32(&q_bar));
-                    }
-            }
-            __syncwarp();
-            for (; it < 2 * nt; ++it) {
-                const int s = it % S::kStages, row = d.k0 + tile_key(it >> 1);
-                if (!mbar_wait_warp(smem_u32(&empty_bar[s]), ((uint32_t)(it / S::kStages) & 1u) ^ 1u, abort_flag)) break;
+        // ---- TMA: per part Q of both items, then K and V tiles in turn
+        int it = 0, np = 0;
+        bool ok = true;
+        if (elect_one()) { prefetch_tmap(&maps.q); prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
+        __syncwarp();
+        while (ok && walk.left > 0) {
+            const Part q = part_of(walk);
+            const int nt = uniform(q.nt), top = uniform(q.lo + q.nt - 1), k0 = uniform(walk.d.k0), gk = uniform(walk.g * maps.k_step), gv = uniform(walk.g * maps.v_step);
+            if (nt > 0) {
+                if (!mbar_wait_warp(smem_u32(&q_free_bar), (uint32_t)(np & 1) ^ 1u, abort_flag)) { ok = false; break; }
                 if (elect_one()) {
-                    const uint32_t fb = smem_u32(&full_bar[s]);
-                    mbar_arrive_expect_tx(fb, S::kTile);
+                    const int both = q.p.rows[1] > 0 ? 2 : 1;
+                    mbar_arrive_expect_tx(smem_u32(&q_bar), (uint32_t)both * S::KB * (uint32_t)(item_rows(a) * a.heads_item) * 128u);
 #pragma unroll
-                    for (int kb = 0; kb < S::KB; ++kb) {
-                        if (it & 1) tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.v, kb * 64, row, g * maps.v_step, fb);
-                        else tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.k, kb * 64, row, g * maps.k_step, fb);
+                    for (int x = 0; x < 2; ++x)
+                        if (x < both) {
+#pragma unroll
+                            for (int kb = 0; kb < S::KB; ++kb)
+                                tma_load_3d(q_addr(x) + kb * S::kBlk, &maps.q, kb * 64, walk.g * a.G + q.p.h0[x], walk.d.q0 + q.p.i0[x], smem_u32(&q_bar));
+                        }
+                }
+                __syncwarp();
+                ++np;
+                for (int j = 0; ok && j < 2 * nt; ++j, ++it) {
+                    const int s = it % S::kStages, row = k0 + tile_key(top, j >> 1);
+                    if (!mbar_wait_warp(smem_u32(&empty_bar[s]), ((uint32_t)(it / S::kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                    if (elect_one()) {
+                        const uint32_t fb = smem_u32(&full_bar[s]);
+                        mbar_arrive_expect_tx(fb, S::kTile);
+#pragma unroll
+                        for (int kb = 0; kb < S::KB; ++kb) {
+                            if (j & 1) tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.v, kb * 64, row, gv, fb);
+                            else tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.k, kb * 64, row, gk, fb);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            walk_on(a, walk, q.steps);
+        }
+        // every copy has landed before the shared memory goes away
+        if (np > 0) mbar_wait_warp(smem_u32(&q_bar), (uint32_t)(np - 1) & 1u, abort_flag);
+        for (int back = 1; back <= S::kStages && back <= it; ++back) {
+            const int j = it - back;
+            mbar_wait_warp(smem_u32(&full_bar[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u, abort_flag);
+        }
+    } else if (warp >= 9) {
+        // ---- products of item x
+        constexpr uint32_t idesc_s = make_idesc_bf16(kM, kN), idesc_o = make_idesc_bf16(kM, DH) | (1u << 16);
+        const int x = warp - 9;
+        const uint32_t t_s = tmem + (uint32_t)x * kN, t_o = tmem + 2 * kN + (uint32_t)x * DH;
+        const uint32_t q_lo = desc_k128_lo(q_addr(x)), k_lo0 = desc_k128_lo(kv_addr(0)), v_lo0 = desc_v_lo(kv_addr(0), S::kBlk);
+        bool ok = true;
+        int it0 = 0, np = 0, tiles = 0, outs = 0;      // key and value tiles, parts, the item's tiles and outputs so far
+        auto wait_full = [&](int it) { return mbar_wait_warp(smem_u32(&full_bar[it % S::kStages]), (uint32_t)(it / S::kStages) & 1u, abort_flag); };
+        while (ok && walk.left > 0) {
+            const Part q = part_of(walk);
+            const int nt = uniform(q.nt), top = uniform(q.lo + q.nt - 1), st = uniform(x ? q.st[1] : q.st[0]), Lk = uniform(walk.d.Lk);
+            auto logits = [&](int it) {                // S of the key tile at `it`
+                const uint32_t k_lo = k_lo0 + (uint32_t)(it % S::kStages) * (S::kTile >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < DH / 16; ++kk) {
+                        constexpr uint32_t kNext = S::kBlk >> 4;
+                        umma_bf16_words(t_s, q_lo + (kk >> 2) * kNext + (kk & 3) * 2, k_lo + (kk >> 2) * kNext + (kk & 3) * 2, idesc_s, kk != 0 ? 1u : 0u);
+                    }
+                    umma_commit(smem_u32(&s_bar[x]));
+                    umma_commit(smem_u32(&empty_bar[it % S::kStages]));
+                }
+                __syncwarp();
+            };
+            // a tile that the item does not take part in: the other one does
+            auto pass = [&](int it) {
+                if (!wait_full(it)) return false;
+                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[it % S::kStages]));
+                __syncwarp();
+                return true;
+            };
+            if (nt > 0) {
+                for (int j = 0; ok && j < 2 * min(st, nt); ++j) ok = pass(it0 + j);
+                if (ok && st < nt) {
+                    ok = mbar_wait_warp(smem_u32(&q_bar), (uint32_t)np & 1u, abort_flag) && wait_full(it0 + 2 * st);
+                    if (ok) {
+                        tc_fence_after();
+                        logits(it0 + 2 * st);
                     }
                 }
-                __syncwarp();
-            }
-            // every copy has landed before the shared memory goes away
-            mbar_wait_warp(smem_u32(&q_bar), 0u, abort_flag);
-            for (int back = 1; back <= S::kStages && back <= it; ++back) {
-                const int j = it - back;
-                mbar_wait_warp(smem_u32(&full_bar[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u, abort_flag);
-            }
-        }
-    } else if (warp == 9) {
-        // ---- products
-        constexpr uint32_t idesc_s = make_idesc_bf16(kM, kN), idesc_o = make_idesc_bf16(kM, DH) | (1u << 16);
-        bool ok = nt == 0 || mbar_wait_warp(smem_u32(&q_bar), 0u, abort_flag);
-        auto wait_full = [&](int it) { return mbar_wait_warp(smem_u32(&full_bar[it % S::kStages]), (uint32_t)(it / S::kStages) & 1u, abort_flag); };
-        auto logits = [&](int x, int j) {              // S_x of key tile j
-            const uint32_t kb = kv_addr((2 * j) % S::kStages), qb = q_addr(x), dst = tmem + (uint32_t)x * kN;
-            if (elect_one()) {
+                for (int j = st; ok && j < nt; ++j) {
+                    const int vi = it0 + 2 * j + 1, vs = vi % S::kStages, seen = tiles + j - st;
+                    if (!(ok = wait_full(vi))) break;
+                    const int left = Lk - tile_key(top, j);        // rows of the document in this tile
+                    if (left < kN) {                   // those behind count as zeros, whatever they hold (both items' warps write them)
+                        for (int c = lane; c < (kN - left) * S::KB * 8; c += 32) {
+                            const int r = left + c / (S::KB * 8), e = c % (S::KB * 8);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_addr(vs) + (uint32_t)(e >> 3) * S::kBlk + (uint32_t)r * 128u + (uint32_t)(e & 7) * 16u), "r"(0) : "memory");
+                        }
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
+                    // the rows have taken the output of the part before
+                    if (j == st && !(ok = mbar_wait_warp(smem_u32(&o_free_bar[x]), (uint32_t)(outs & 1) ^ 1u, abort_flag))) break;
+                    const uint32_t v_lo = v_lo0 + (uint32_t)vs * (S::kTile >> 4);
 #pragma unroll
-                for (int kk = 0; kk < DH / 16; ++kk)
-                    umma_bf16(dst, make_desc_k128(qb + (kk >> 2) * S::kBlk + (kk & 3) * 32), make_desc_k128(kb + (kk >> 2) * S::kBlk + (kk & 3) * 32),
-                              idesc_s, kk != 0 ? 1u : 0u);
-                umma_commit(smem_u32(&s_bar[x]));
-            }
-            __syncwarp();
-        };
-        auto values = [&](int x, int j, int half) {    // O_x += P_x V of 64 keys of tile j
-            const int vs = (2 * j + 1) % S::kStages, jx = j - st[x];
-            if (!mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)jx & 1u, abort_flag)) return false;
-            tc_fence_after();
-            if (elect_one()) {
+                    for (int half = 0; half < 2; ++half) {         // O += P V of 64 keys: the first ones' weights are there while the others are made
+                        if (!(ok = mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)seen & 1u, abort_flag))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    umma_bf16_ts(tmem + 2 * kN + (uint32_t)x * DH, tmem + (uint32_t)x * kN + half * 32 + kk * 8, desc_v(kv_addr(vs) + (half * 4 + kk) * 2048, S::kBlk), idesc_o,
-                                 jx > 0 || half || kk > 0 ? 1u : 0u);
-                if (!half) umma_commit(smem_u32(&h_bar[x]));
-                else if (j + 1 == nt) umma_commit(smem_u32(&o_bar[x]));
-            }
-            __syncwarp();
-            return true;
-        };
-        auto release = [&](int it) {
-            if (elect_one()) umma_commit(smem_u32(&empty_bar[it % S::kStages]));
-            __syncwarp();
-        };
-        // One item's second half and next logits lie between the other's halves, so that the products go on while either's weights
-        // are made: per step  O_0 first half | O_1 second half of the step before, S_1 | O_0 second half, next S_0 | O_1 first half.
-        if (ok && nt > 0 && (ok = wait_full(0))) {
-            tc_fence_after();
-            for (int x = 0; x < 2; ++x)
-                if (st[x] == 0) logits(x, 0);
-        }
-        for (int j = 0; ok && j < nt; ++j) {
-            const int vi = 2 * j + 1, vs = vi % S::kStages;
-            if (!(ok = wait_full(vi))) break;
-            const int left = d.Lk - tile_key(j);       // rows of the document in this tile
-            if (left < kN) {                           // those behind count as zeros, whatever they hold
-                for (int c = lane; c < (kN - left) * S::KB * 8; c += 32) {
-                    const int r = left + c / (S::KB * 8), e = c % (S::KB * 8);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_addr(vs) + (uint32_t)(e >> 3) * S::kBlk + (uint32_t)r * 128u + (uint32_t)(e & 7) * 16u), "r"(0) : "memory");
+                            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                                umma_bf16_ts(t_o, t_s + kk * 8, v_lo + kk * 128, idesc_o, kk > 0 || j > st ? 1u : 0u);
+                            if (!half) umma_commit(smem_u32(&h_bar[x]));
+                            else umma_commit(smem_u32(&empty_bar[vs]));
+                            if (half && j + 1 == nt) umma_commit(smem_u32(&o_bar[x]));
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (j + 1 < nt) {
+                        if (!(ok = wait_full(vi + 1))) break;
+                        logits(vi + 1);
+                    }
                 }
-                fence_proxy_async();
-                __syncwarp();
+                // Q has been read, or was not wanted
+                if (ok) {
+                    if (st < nt) {
+                        if (elect_one()) umma_commit(smem_u32(&q_free_bar));
+                    } else if (mbar_wait_warp(smem_u32(&q_bar), (uint32_t)np & 1u, abort_flag)) {
+                        if (lane == 0) mbar_arrive(smem_u32(&q_free_bar));
+                    } else {
+                        ok = false;
+                    }
+                    __syncwarp();
+                }
+                ++np;
+                it0 += 2 * nt;
+                tiles += max(0, nt - st);
+                outs += st < nt;
             }
-            if (j >= st[0] && !(ok = values(0, j, 0))) break;
-            if (j > 0) {
-                if (j > st[1] && !(ok = values(1, j - 1, 1))) break;
-                if (j >= st[1]) logits(1, j);
-                release(vi - 2);
-            }
-            release(2 * j);                            // (S_1's, or S_0's in the first step)
-            if (j >= st[0] && !(ok = values(0, j, 1))) break;
-            if (j + 1 < nt) {
-                if (!(ok = wait_full(2 * j + 2))) break;
-                if (j + 1 >= st[0]) logits(0, j + 1);
-            }
-            if (j >= st[1] && !(ok = values(1, j, 0))) break;
+            walk_on(a, walk, q.steps);
         }
-        if (ok && n[1] > 0) ok = values(1, nt - 1, 1);
         if (!ok) {                                     // whatever was issued has retired before the tensor memory goes
-            if (elect_one()) umma_commit(smem_u32(&drain_bar));
+            if (elect_one()) umma_commit(smem_u32(&drain_bar[x]));
             __syncwarp();
-            mbar_wait_warp(smem_u32(&drain_bar), 0u, abort_flag);
+            mbar_wait_warp(smem_u32(&drain_bar[x]), 0u, abort_flag);
         }
     } else {
         // ---- rows
         const int x = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
-        const int my_n = x ? n[1] : n[0], my_rows = x ? rows[1] : rows[0], my_i0 = x ? i0[1] : i0[0], my_head = x ? head[1] : head[0];
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t t_s = tmem + lane_base + (uint32_t)x * kN, t_o = tmem + lane_base + 2 * kN + (uint32_t)x * DH;
         const float ninf = __int_as_float(0xFF800000);
-        const int keys = r < my_rows ? prompt_keys(a, d, my_i0 + r) : 0;
-        const int sure = my_rows > 0 ? prompt_keys(a, d, my_i0) : 0;    // keys that all rows of the tile see
-        float m = ninf, l = 0.f;
-        bool ok = true;
+        const int my_i = r / a.heads_item, my_h = r - my_i * a.heads_item;      // row and head of the tile
+        bool ok = true, first_part = true;
+        int seen = 0, outs = 0;                        // tiles and outputs of this item so far
+        Walk* my_walk = &s_walk[warp];
+        if (lane == 0) *my_walk = walk;
+        __syncwarp();
+        while (my_walk->left > 0) {
+        // what the tiles' loop needs; the rest is worked out again behind it
+        int my_n, my_lo, keys, sure, k_first, k_rows;  // tiles, the lowest of them, keys that the row and that all rows of the item see; the document's keys
         float slope = 0.f, my_pos = 0.f, next_pos = 0.f;
-        if (kBias && my_n > 0) {
-            slope = a.slopes[my_head] * kAttnLog2e;
-            my_pos = prompt_position(a, d, d.Lk - d.Lq + my_i0 + r);
-            next_pos = prompt_position(a, d, (lo + my_n - 1) * kN + r);
+        {
+            const PromptDoc d = my_walk->d;
+            const Part q = part_of(*my_walk);
+            const int i0 = x ? q.p.i0[1] : q.p.i0[0], h0 = x ? q.p.h0[1] : q.p.h0[0], rows = x ? q.p.rows[1] : q.p.rows[0];
+            my_n = q.nt - (x ? q.st[1] : q.st[0]);
+            my_lo = q.lo;
+            const bool mine = r < rows && h0 + my_h < a.G;
+            keys = mine ? prompt_keys(a, d, i0 + my_i) : 0;
+            sure = rows > 0 ? prompt_keys(a, d, i0) : 0;
+            k_first = d.k0;
+            k_rows = d.Lk;
+            if (kBias && my_n > 0) {
+                slope = mine ? a.slopes[my_walk->g * a.G + h0 + my_h] * kAttnLog2e : 0.f;
+                my_pos = prompt_position(a, d.k0, d.Lk, d.Lk - d.Lq + i0 + my_i);
+                next_pos = prompt_position(a, k_first, k_rows, (my_lo + my_n - 1) * kN + r);
+            }
         }
-        for (int j = 0; j < my_n; ++j) {
-            const int k0 = (lo + my_n - 1 - j) * kN;
+        float m = ninf, l = 0.f;
+        for (int j = 0; j < my_n; ++j, ++seen) {
+            const int k0 = (my_lo + my_n - 1 - j) * kN;
             if constexpr (kBias) {                     // (two buffers: who writes one again has met the others since it was read)
-                s_pos[x][j & 1][r] = next_pos;
-                next_pos = prompt_position(a, d, k0 - kN + r);
+                s_pos[x][seen & 1][r] = next_pos;
+                next_pos = prompt_position(a, k_first, k_rows, k0 - kN + r);
                 named_bar_sync(1 + x, 128);
             }
-            if (ok && !mbar_wait(smem_u32(&s_bar[x]), (uint32_t)j & 1u, abort_flag)) ok = false;
+            if (ok && !mbar_wait(smem_u32(&s_bar[x]), (uint32_t)seen & 1u, abort_flag)) ok = false;
             ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) {
-                if constexpr (kBias) continue;         // keeps meeting the tile's other warps
-                break;
-            }
+            if (!ok) continue;                         // (keeps meeting the item's other warps where they meet)
             tc_fence_after();
             const bool masked = k0 + kN > sure;
             // Logits of columns 32 c .. in log2 units less `base`; those of keys that the row does not see are -infinity.
@@ -312,7 +525,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 if constexpr (kBias) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][j & 1][c * 32 + i]);
+                        const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][seen & 1][c * 32 + i]);
                         v[i] = fmaf(-slope, fabsf(my_pos - p.x), v[i]);
                         v[i + 1] = fmaf(-slope, fabsf(my_pos - p.y), v[i + 1]);
                         v[i + 2] = fmaf(-slope, fabsf(my_pos - p.z), v[i + 2]);
@@ -364,16 +577,22 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
             uint32_t raw[2][32];
             tmem_ld32_issue(t_s, raw[0]);
-#pragma unroll
+#pragma unroll 1                                       // (unrolled, the rows' code no longer fits the instruction cache)
             for (int half = 0; half < 2; ++half) {
                 uint32_t p[32];
+                constexpr bool kAhead = !(kCap && kBias);   // (both: no registers for a load on its way)
                 tmem_ld32_wait(raw[0]);
-                tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
+                if (kAhead) tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
                 float sum = weights(raw[0], half * 2, p);
+                if (!kAhead) tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
                 tmem_ld32_wait(raw[1]);
-                if (!half) tmem_ld32_issue(t_s + 64, raw[0]);
+                if (kAhead && !half) tmem_ld32_issue(t_s + 64, raw[0]);
                 sum += weights(raw[1], half * 2 + 1, p + 16);
-                const bool far = !(sum < kMost);
+                if (!kAhead && !half) {
+                    tmem_ld32_issue(t_s + 64, raw[0]);
+                    tmem_ld32_wait(raw[0]);
+                }
+                const bool far = keys > 0 && !(sum < kMost);   // (a tile's unused rows may hold anything)
                 if (__any_sync(0xFFFFFFFFu, far)) {    // again, against the maximum of these
                     if (!half) tmem_ld32_wait(raw[0]); // (in order: nothing is on its way while registers are short)
                     const float mx = largest(half * 2, half * 2 + 2);
@@ -382,7 +601,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     if (grow) m = mx + kRoom;
                     l *= f;
                     // the product before this one on O_x is complete: that of the tile before since S_x is there, that of the first half when its barrier says so
-                    if (half && ok && !mbar_wait(smem_u32(&h_bar[x]), (uint32_t)j & 1u, abort_flag)) ok = false;
+                    if (half && ok && !mbar_wait(smem_u32(&h_bar[x]), (uint32_t)seen & 1u, abort_flag)) ok = false;
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     tc_fence_after();
                     if (j > 0 || half) {
@@ -396,14 +615,13 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                             tmem_st32(t_o + c * 32, o);
                         }
                     }
-                    sum = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t again[32];
-                        tmem_ld32_issue(t_s + half * 64 + c * 32, again);
-                        tmem_ld32_wait(again);
-                        sum += weights(again, half * 2 + c, p + c * 16);
-                    }
+                    uint32_t again[32];
+                    tmem_ld32_issue(t_s + half * 64, again);
+                    tmem_ld32_wait(again);
+                    sum = weights(again, half * 2, p);
+                    tmem_ld32_issue(t_s + half * 64 + 32, again);
+                    tmem_ld32_wait(again);
+                    sum += weights(again, half * 2 + 1, p + 16);
                 }
                 l += sum;
                 tmem_st32(t_s + half * 32, p);         // 64 keys' weights: their product may begin
@@ -413,14 +631,17 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][half]));
             }
         }
-        if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), 0u, abort_flag)) ok = false;
+        if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), (uint32_t)outs & 1u, abort_flag)) ok = false;
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_fence_after();
-        const bool mine = r < my_rows;
-        const long long row = d.q0 + my_i0 + r;
-        const long long at = ((long long)blockIdx.y * a.Hq + my_head) * a.n_q + row;
-        const float scale = a.splits > 1 ? 1.f : l > 0.f ? 1.f / l : 0.f;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + my_head * a.out_head + row * a.out_row;
+        const PromptDoc d = my_walk->d;
+        const Part part = part_of(*my_walk);
+        const int my_i0 = x ? part.p.i0[1] : part.p.i0[0], h0 = x ? part.p.h0[1] : part.p.h0[0], my_head = my_walk->g * a.G + h0 + my_h;
+        const bool mine = r < (x ? part.p.rows[1] : part.p.rows[0]) && h0 + my_h < a.G, whole = part.whole;
+        const long long row = d.q0 + my_i0 + my_i;
+        const long long at = (2LL * blockIdx.x + (first_part ? 0 : 1)) * (2 * kM) + x * kM + r;    // row of this CTA's two partial pairs
+        const float scale = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)my_head * a.out_head + row * a.out_row;
         if (ok) {
 #pragma unroll
             for (int c = 0; c < DH / 32; ++c) {
@@ -431,20 +652,54 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = 0.f;
                 }
-                if (mine && a.splits > 1) {
+                if (!mine) continue;
+                if (!whole) {
                     if (my_n > 0) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(a.part_o + at * DH + c * 32 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     }
-                } else if (mine) {
+                } else {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8)
                         *reinterpret_cast<uint4*>(out + c * 32 + i) = make_uint4(pack_bf16(o[i] * scale, o[i + 1] * scale), pack_bf16(o[i + 2] * scale, o[i + 3] * scale),
                                                                                  pack_bf16(o[i + 4] * scale, o[i + 5] * scale), pack_bf16(o[i + 6] * scale, o[i + 7] * scale));
                 }
             }
-            if (mine && a.splits > 1) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(l > 0.f ? m : ninf, l);
+            if (mine && !whole) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(l > 0.f ? m : ninf, l);
             else if (mine && a.lse) a.lse[(long long)my_head * a.n_q + row] = kAttnLn2 * (m + log2f(l));
+        }
+        if (my_n > 0) {                                // O_x may be written again
+            ++outs;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&o_free_bar[x]));
+        }
+        // a pair that began in another CTA: the second of those that share it notes what there is to join
+        if (threadIdx.x == 0 && first_part && my_walk->e0 > 0) {
+            const int steps = max(1, part.p.nt);
+            const long long f0 = begin - my_walk->e0;      // the pair's place in the line; CTA c's piece begins at all * c / ctas
+            const long long c0 = ((f0 + 1) * ctas - 1) / all, c1 = ((f0 + steps) * ctas - 1) / all;
+            if (c0 + 1 == (long long)blockIdx.x) {
+                Cut cut;
+                cut.c0 = (int)c0;
+                cut.c1 = (int)c1;
+                cut.first_slot = 2 * (int)c0 + (all * c0 / ctas >= f0 ? 0 : 1);
+                cut.q0 = d.q0;
+                cut.g = my_walk->g;
+                cut.Lq = d.Lq;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    cut.i0[y] = part.p.i0[y];
+                    cut.h0[y] = part.p.h0[y];
+                    cut.rows[y] = part.p.rows[y];
+                }
+                cuts[blockIdx.x] = cut;
+            }
+        }
+        first_part = false;
+        __syncwarp();
+        if (lane == 0) walk_on(a, *my_walk, part.steps);
+        __syncwarp();
         }
     }
     tc_fence_before();
@@ -453,42 +708,100 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
+// Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut; a warp per row.
+constexpr int kCutWarps = 8, kCutBlocks = 2 * kM / kCutWarps;
+template <int DH>
+__global__ void __launch_bounds__(kCutWarps * 32)
+prompt_cut_join_kernel(const PromptArgs a) {
+    grid_dep_wait();
+    const Cut cut = reinterpret_cast<const Cut*>(a.cuts)[blockIdx.x];
+    if (cut.c1 < 0) return;
+    const int lane = threadIdx.x & 31, rr = blockIdx.y * kCutWarps + (threadIdx.x >> 5), x = rr / kM, r = rr - x * kM;
+    const int i = r / a.heads_item, h = (x ? cut.h0[1] : cut.h0[0]) + r - i * a.heads_item;
+    if (r >= (x ? cut.rows[1] : cut.rows[0]) || h >= a.G) return;
+    const int parts = cut.c1 - cut.c0 + 1, head = cut.g * a.G + h;
+    const long long row = cut.q0 + (x ? cut.i0[1] : cut.i0[0]) + i;
+    auto place = [&](int p) { return (long long)(p == 0 ? cut.first_slot : 2 * (cut.c0 + p)) * (2 * kM) + rr; };
+    const float ninf = __int_as_float(0xFF800000);
+    float M = ninf;
+    for (int p = lane; p < parts; p += 32) M = fmaxf(M, a.part_ml[place(p) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+    constexpr int E = DH / 32, kAhead = 4;
+    float acc[E], L = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        float2 ml[kAhead];
+        float o[kAhead][E];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            ml[u] = make_float2(ninf, 0.f);
+            if (p0 + u < parts) ml[u] = *reinterpret_cast<const float2*>(a.part_ml + place(p0 + u) * 2);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[u][e] = p0 + u < parts ? a.part_o[place(p0 + u) * DH + lane * E + e] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (!(ml[u].y > 0.f)) continue;            // a part of no keys has written no output
+            const float f = sm100::fast_exp2(ml[u].x - M);
+            L += f * ml[u].y;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] += f * o[u][e];
+        }
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)head * a.out_head + row * a.out_row;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[lane * E + e] = __float2bfloat16_rn(acc[e] * inv);
+    if (lane == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
+}
+
 template <int DH, bool kCap, bool kBias>
-int launch(const PromptArgs& a, long long ctas, const MmaMaps& maps, cudaStream_t st) {
+int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
     auto kern = prompt_attn_mma_kernel<DH, kCap, kBias>;
     METOK_ALLOW_SMEM(kern, MmaShape<DH>::kSmem);
-    METOK_TIMED("prompt_attn_mma", st);
-    launch_chained(kern, dim3((unsigned)ctas, a.splits), dim3(kThreads), MmaShape<DH>::kSmem, st, a, maps);
+    {
+        METOK_TIMED("prompt_attn_mma", st);
+        launch_chained(kern, dim3(kNumSMs), dim3(kThreads), MmaShape<DH>::kSmem, st, a, maps);
+    }
+    METOK_LAUNCH_CHECK();
+    {
+        METOK_TIMED("prompt_cut_join", st);
+        launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks), dim3(kCutWarps * 32), 0, st, a);
+    }
     METOK_LAUNCH_CHECK();
     return METOK_OK;
 }
 template <int DH>
-int launch_dh(const PromptArgs& a, long long ctas, const MmaMaps& maps, cudaStream_t st) {
-    if (a.cap_log2 > 0.f) return a.slopes ? launch<DH, true, true>(a, ctas, maps, st) : launch<DH, true, false>(a, ctas, maps, st);
-    return a.slopes ? launch<DH, false, true>(a, ctas, maps, st) : launch<DH, false, false>(a, ctas, maps, st);
+int launch_dh(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
+    if (a.cap_log2 > 0.f) return a.slopes ? launch<DH, true, true>(a, maps, st) : launch<DH, true, false>(a, maps, st);
+    return a.slopes ? launch<DH, false, true>(a, maps, st) : launch<DH, false, false>(a, maps, st);
 }
 
 }  // namespace
 
-// CTAs for the pairs of items of all documents, at most: one document has ceil(n_q / 128) G items, several at most a started tile more each.
-long long prompt_mma_ctas(int Hkv, int G, int n_q, int n_seq) {
-    const long long docs = std::min(n_seq, n_q), tiles = n_seq == 1 ? ceil_div(n_q, kM) : n_q / kM + docs;
-    return std::max(1LL, (tiles * G + docs) / 2) * Hkv;
+void prompt_mma_carve(Carver& cv, int dh, PromptArgs* a) {
+    a->cuts = cv.take<Cut>(kNumSMs);
+    a->part_ml = cv.take<float>((size_t)2 * kNumSMs * 2 * kM * 2);
+    a->part_o = cv.take<float>((size_t)2 * kNumSMs * 2 * kM * dh);
 }
 
-int launch_prompt_attn_mma(const PromptArgs& a, int dh, long long ctas, cudaStream_t st) {
+int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st) {
     MmaMaps maps = {};
-    maps.q_step = a.Hq > 1 && a.q_head > 0;
+    a.heads_item = std::min(a.G, kM);
+    a.head_chunks = ceil_div(a.G, a.heads_item);
     maps.k_step = a.Hkv > 1 && a.k_head > 0;
     maps.v_step = a.Hkv > 1 && a.v_head > 0;
     if (a.n_q > 0) {
-        int rc = make_tmap_heads(&maps.q, a.q, a.n_q, dh, maps.q_step ? a.Hq : 1, a.q_row, a.q_head, kM);
+        // Q: heads of a row side by side
+        int rc = make_tmap_3d(&maps.q, a.q, dh, a.Hq, a.n_q, a.Hq > 1 ? a.q_head : a.q_row, a.q_row, a.heads_item, kM / a.heads_item);
         // where there are no keys no tile of them is asked for, and any rows will do
-        if (rc == METOK_OK) rc = a.n_k ? make_tmap_heads(&maps.k, a.k, a.n_k, dh, maps.k_step ? a.Hkv : 1, a.k_row, a.k_head, kN) : (maps.k = maps.q, METOK_OK);
-        if (rc == METOK_OK) rc = a.n_k ? make_tmap_heads(&maps.v, a.v, a.n_k, dh, maps.v_step ? a.Hkv : 1, a.v_row, a.v_head, kN) : (maps.v = maps.q, METOK_OK);
+        if (rc == METOK_OK) rc = a.n_k ? make_tmap_3d(&maps.k, a.k, dh, a.n_k, maps.k_step ? a.Hkv : 1, a.k_row, maps.k_step ? a.k_head : a.k_row, kN, 1) : (maps.k = maps.q, METOK_OK);
+        if (rc == METOK_OK) rc = a.n_k ? make_tmap_3d(&maps.v, a.v, dh, a.n_k, maps.v_step ? a.Hkv : 1, a.v_row, maps.v_step ? a.v_head : a.v_row, kN, 1) : (maps.v = maps.q, METOK_OK);
         if (rc != METOK_OK) return rc;
     }
-    return dh == 64 ? launch_dh<64>(a, ctas, maps, st) : launch_dh<128>(a, ctas, maps, st);
+    return dh == 64 ? launch_dh<64>(a, maps, st) : launch_dh<128>(a, maps, st);
 }
 
 }  // namespace metok

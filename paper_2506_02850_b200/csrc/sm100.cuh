@@ -323,9 +323,9 @@ __device__ __forceinline__ void named_bar_sync(int id, int nthreads) {
 // 2-D bf16 tensor [rows][cols] (cols contiguous), box = box_rows x 64 columns, 128-byte swizzle,
 // out-of-bounds elements read as zero.  Returns a METOK status.
 int make_tmap_bf16_2d(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
-// The same for bf16 [heads][rows][cols] with strides in elements: box = 1 x box_rows x 128 bytes.
-int make_tmap_heads(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t row_stride, uint64_t head_stride,
-                    uint32_t box_rows);
+// The same for bf16 [n2][n1][cols] with strides in elements: box = b2 x b1 x 128 bytes.
+int make_tmap_3d(CUtensorMap* out, const void* base, uint64_t cols, uint64_t n1, uint64_t n2, uint64_t stride1, uint64_t stride2, uint32_t b1,
+                 uint32_t b2);
 // The same for either dtype: box = box_rows x 128 bytes.
 int make_tmap_rows(CUtensorMap* out, int dtype, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 

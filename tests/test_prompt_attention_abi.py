@@ -39,7 +39,7 @@ def test_refusals(lib):
                dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(softcap=-2.0), dict(softcap=float("inf")), dict(softcap=float("nan")),
                dict(seq_q=p0 + 2), dict(positions=p0 + 1), dict(slopes=p0 + 3), dict(lse=p0 + 2), dict(prefix_len=p0 + 1)]:
         assert call(**kw) == (-1, 0), kw
-    for kw in [dict(dh=96), dict(dh=256), dict(n_q=(1 << 24) + 1), dict(n_k=(1 << 24) + 1), dict(n_seq=65537), dict(Hq=65536, Hkv=1)]:
+    for kw in [dict(dh=96), dict(dh=256), dict(n_q=(1 << 24) + 1), dict(n_k=(1 << 24) + 1), dict(n_seq=8193), dict(Hq=65536, Hkv=1)]:
         assert call(**kw) == (-2, 0), kw
     # few rows over many keys are split, which takes a workspace
     few = dict(n_k=20000, seq_q=None, seq_k=None, n_seq=1)
