@@ -13,10 +13,10 @@
 // few rows over many keys and a number of pairs that is no multiple of the SMs all keep every SM busy to the end.  Every CTA finds its
 // piece by itself, from the documents' offsets.
 //
-// Key tiles of a pair are taken from the last one down.  A row's reference m is the maximum of the first tile that it sees; later tiles'
-// weights are taken against it with no maximum of their own, since any m within the range of the exponent gives the same
-// result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x and the sum are
-// scaled: by the row's own thread, when the products before on O_x are complete (one thread issues all of them, in order).
+// Key tiles of a pair are taken from the last one down (a bias makes the nearest ones the largest).  A row's reference m is the maximum of
+// the first 64 keys that it sees, and grows only where a later logit passes it by more than 2^16: any m within the range of
+// the exponent gives the same result, and a change costs a pass over O_x.  The row's own thread makes it, when the products before on
+// O_x are complete (one thread issues all of them, in order).
 //
 // Warps 0-3 and 4-7: the rows of items 0 and 1; warp 8: TMA; warps 9 and 10: the products of items 0 and 1, each with waits of its
 // own (an issuing warp is held up while products run, so one warp's waits for both items lie open).  Every wait is bounded.  A row's 128 logits are read
@@ -32,7 +32,8 @@ namespace metok {
 namespace {
 
 constexpr int kM = 128, kN = 128, kThreads = 352;
-constexpr float kMost = 1.0e18f, kRoom = 32.f;         // sum of 64 weights beyond which a row's reference grows, and by how many octaves above their maximum
+constexpr float kGrow = 16.f;                          // octaves by which a logit may pass the row's reference
+constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
 constexpr int kFewest = 2;                             // steps of the line that a CTA is given at least, on average
 
@@ -83,6 +84,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 2^x for x < 127 on the FMA pipe (exp2_fma_pair); arguments below -125 are held there, a NaN gives something that is no weight.
+__device__ __forceinline__ uint64_t exp2_low_pair(uint64_t x) {
+    float a, b;
+    sm100::unpair(x, a, b);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(-125.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(-125.f));
+    return sm100::exp2_fma_core(sm100::pair(a, b));
+}
+// 16 registers of this thread's lane to 16 tensor-memory columns.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+        : "memory");
 }
 
 struct MmaMaps {
@@ -511,94 +535,86 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             if (!ok) continue;                         // (keeps meeting the item's other warps where they meet)
             tc_fence_after();
             const bool masked = k0 + kN > sure;
-            // Logits of columns 32 c .. in log2 units less `base`; those of keys that the row does not see are -infinity.
-            auto logit = [&](const uint32_t (&raw)[32], int c, float base, float (&v)[32]) {
+#pragma unroll 1                                       // (one copy of the code: the instruction cache is short)
+            for (int half = 0; half < 2; ++half) {     // 64 keys
+                uint32_t raw[2][32];
+                tmem_ld32_issue(t_s + half * 64, raw[0]);
+                tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
+                tmem_ld32_wait(raw[0]);
+                tmem_ld32_wait(raw[1]);
+                uint64_t v[32];                        // logits in log2 units, in pairs
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = pair(__uint_as_float(raw[i >> 4][2 * (i & 15)]), __uint_as_float(raw[i >> 4][2 * (i & 15) + 1]));
                 if constexpr (kCap) {
+                    // y = product * scale / cap.  Up to |y| = 1 tanh(y) = y P(y^2), P the polynomial of degree 6 of least largest error (2e-8; 1e-7 in
+                    // fp32); beyond, 1 - 2 / (1 + e^2y), of which every part costs the special-function unit a step.
+                    float most = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        v[i] = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(__uint_as_float(raw[i]) * (2.f * kAttnLog2e * a.cap_scale), 80.f)));
-                } else {
+                    for (int i = 0; i < 32; ++i) {
+                        v[i] = mul_pair(v[i], pair(a.cap_scale, a.cap_scale));
+                        float y0, y1;
+                        unpair(v[i], y0, y1);
+                        most = fmaxf(most, fmaxf(fabsf(y0), fabsf(y1)));
+                    }
+                    if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2)
-                        unpair(fma_pair(pair(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), pair(a.scale_log2, a.scale_log2), pair(-base, -base)), v[i], v[i + 1]);
+                        for (int i = 0; i < 32; ++i) {
+                            float y0, y1;
+                            unpair(v[i], y0, y1);
+                            y0 = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y0 * (2.f * kAttnLog2e), 80.f)));
+                            y1 = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y1 * (2.f * kAttnLog2e), 80.f)));
+                            v[i] = pair(y0, y1);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const uint64_t u = mul_pair(v[i], v[i]);
+                            uint64_t t = fma_pair(u, pair(0.000963772187f, 0.000963772187f), pair(-0.00595128048f, -0.00595128048f));
+                            t = fma_pair(t, u, pair(0.0199732827f, 0.0199732827f));
+                            t = fma_pair(t, u, pair(-0.0532658353f, -0.0532658353f));
+                            t = fma_pair(t, u, pair(0.133195837f, 0.133195837f));
+                            t = fma_pair(t, u, pair(-0.333321293f, -0.333321293f));
+                            t = fma_pair(t, u, pair(0.999999693f, 0.999999693f));
+                            v[i] = mul_pair(mul_pair(v[i], t), pair(a.cap_log2, a.cap_log2));
+                        }
+                    }
+                } else if constexpr (kBias) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = mul_pair(v[i], pair(a.scale_log2, a.scale_log2));
                 }
                 if constexpr (kBias) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][seen & 1][c * 32 + i]);
-                        v[i] = fmaf(-slope, fabsf(my_pos - p.x), v[i]);
-                        v[i + 1] = fmaf(-slope, fabsf(my_pos - p.y), v[i + 1]);
-                        v[i + 2] = fmaf(-slope, fabsf(my_pos - p.z), v[i + 2]);
-                        v[i + 3] = fmaf(-slope, fabsf(my_pos - p.w), v[i + 3]);
+                    for (int i = 0; i < 32; i += 2) {
+                        const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][seen & 1][half * 64 + 2 * i]);
+                        float v0, v1, v2, v3;
+                        unpair(v[i], v0, v1);
+                        unpair(v[i + 1], v2, v3);
+                        v[i] = pair(fmaf(-slope, fabsf(my_pos - p.x), v0), fmaf(-slope, fabsf(my_pos - p.y), v1));
+                        v[i + 1] = pair(fmaf(-slope, fabsf(my_pos - p.z), v2), fmaf(-slope, fabsf(my_pos - p.w), v3));
                     }
                 }
-                if (masked) {
+                if (masked) {                          // keys that the row does not see
+                    const int see = keys - k0 - half * 64;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = k0 + c * 32 + i < keys ? v[i] : ninf;
+                    for (int i = 0; i < 32; ++i) {
+                        float v0, v1;
+                        unpair(v[i], v0, v1);
+                        v[i] = pair(2 * i < see ? v0 : ninf, 2 * i + 1 < see ? v1 : ninf);
+                    }
                 }
-            };
-            // the largest of columns [32 c0, 32 c1)
-            auto largest = [&](int c0, int c1) {
-                float mx = ninf;
-#pragma unroll 1
-                for (int c = c0; c < c1; ++c) {
-                    uint32_t raw[32];
-                    float v[32];
-                    tmem_ld32_issue(t_s + c * 32, raw);
-                    tmem_ld32_wait(raw);
-                    logit(raw, c, 0.f, v);
-                    float t8[8];
+                const float sc = kCap || kBias ? 1.f : a.scale_log2;    // still to be multiplied in
+                float top[4] = {ninf, ninf, ninf, ninf};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) t8[i] = fmaxf(fmaxf(v[i], v[i + 8]), fmaxf(v[i + 16], v[i + 24]));
-                    mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7]))));
+                for (int i = 0; i < 32; ++i) {
+                    float v0, v1;
+                    unpair(v[i], v0, v1);
+                    top[i & 3] = fmaxf(top[i & 3], fmaxf(v0, v1));
                 }
-                return mx;
-            };
-            // 32 weights of the row, and their sum
-            auto weights = [&](const uint32_t (&raw)[32], int c, uint32_t* p) {
-                float v[32];
-                logit(raw, c, m == ninf ? 0.f : m, v);
-                uint64_t sum0 = 0ull, sum1 = 0ull;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w0 = fast_exp2(v[2 * i]), w1 = fast_exp2(v[2 * i + 1]);
-                    if (i & 1) sum1 = add_pair(sum1, pair(w0, w1));
-                    else sum0 = add_pair(sum0, pair(w0, w1));
-                    p[i] = pack_bf16(w0, w1);
-                }
-                float s0, s1;
-                unpair(add_pair(sum0, sum1), s0, s1);
-                return s0 + s1;
-            };
-            const bool first = m == ninf && keys > k0; // the first tile of which the row sees something
-            if (__any_sync(0xFFFFFFFFu, first)) {
-                const float mx = largest(0, 4);
-                if (first) m = mx;
-            }
-            uint32_t raw[2][32];
-            tmem_ld32_issue(t_s, raw[0]);
-#pragma unroll 1                                       // (unrolled, the rows' code no longer fits the instruction cache)
-            for (int half = 0; half < 2; ++half) {
-                uint32_t p[32];
-                constexpr bool kAhead = !(kCap && kBias);   // (both: no registers for a load on its way)
-                tmem_ld32_wait(raw[0]);
-                if (kAhead) tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
-                float sum = weights(raw[0], half * 2, p);
-                if (!kAhead) tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
-                tmem_ld32_wait(raw[1]);
-                if (kAhead && !half) tmem_ld32_issue(t_s + 64, raw[0]);
-                sum += weights(raw[1], half * 2 + 1, p + 16);
-                if (!kAhead && !half) {
-                    tmem_ld32_issue(t_s + 64, raw[0]);
-                    tmem_ld32_wait(raw[0]);
-                }
-                const bool far = keys > 0 && !(sum < kMost);   // (a tile's unused rows may hold anything)
-                if (__any_sync(0xFFFFFFFFu, far)) {    // again, against the maximum of these
-                    if (!half) tmem_ld32_wait(raw[0]); // (in order: nothing is on its way while registers are short)
-                    const float mx = largest(half * 2, half * 2 + 2);
-                    const bool grow = far && mx > m;
-                    const float f = grow ? fast_exp2(m - (mx + kRoom)) : 1.f;
-                    if (grow) m = mx + kRoom;
+                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+                const bool grow = mx > m + kGrow;      // (also where there is none yet)
+                if (__any_sync(0xFFFFFFFFu, grow)) {
+                    const float f = grow ? fast_exp2(m - mx) : 1.f;
+                    if (grow) m = mx;
                     l *= f;
                     // the product before this one on O_x is complete: that of the tile before since S_x is there, that of the first half when its barrier says so
                     if (half && ok && !mbar_wait(smem_u32(&h_bar[x]), (uint32_t)seen & 1u, abort_flag)) ok = false;
@@ -606,31 +622,42 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     tc_fence_after();
                     if (j > 0 || half) {
 #pragma unroll 1
-                        for (int c = 0; c < DH / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32_issue(t_o + c * 32, o);
-                            tmem_ld32_wait(o);
+                        for (int c = 0; c < DH / 16; ++c) {
+                            float o[16];
+                            tmem_ld16(t_o + c * 16, o);
+                            uint32_t w[16];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(t_o + c * 32, o);
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+                            tmem_st16(t_o + c * 16, w);
                         }
                     }
-                    uint32_t again[32];
-                    tmem_ld32_issue(t_s + half * 64, again);
-                    tmem_ld32_wait(again);
-                    sum = weights(again, half * 2, p);
-                    tmem_ld32_issue(t_s + half * 64 + 32, again);
-                    tmem_ld32_wait(again);
-                    sum += weights(again, half * 2 + 1, p + 16);
                 }
-                l += sum;
-                tmem_st32(t_s + half * 32, p);         // 64 keys' weights: their product may begin
+                const float base = m == ninf ? 0.f : m;
+                uint64_t sum0 = 0ull, sum1 = 0ull;
+                uint32_t p[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const uint64_t y = kCap || kBias ? add_pair(v[i], pair(-base, -base)) : fma_pair(v[i], pair(sc, sc), pair(-base, -base));
+                    // some on the FMA pipe, so that both work; y is at most kGrow.  (There a hidden key's weight is 2^-125, not 0: nothing beside any weight
+                    // that counts, and a row that sees no key is known by its m.)
+                    const uint64_t w = kShare(i) ? exp2_low_pair(y) : exp2_pair(y);
+                    if (i & 1) sum1 = add_pair(sum1, w);
+                    else sum0 = add_pair(sum0, w);
+                    float w0, w1;
+                    unpair(w, w0, w1);
+                    p[i] = pack_bf16(w0, w1);
+                }
+                float s0, s1;
+                unpair(add_pair(sum0, sum1), s0, s1);
+                l += s0 + s1;
+                tmem_st32(t_s + half * 32, p);         // their product may begin
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][half]));
             }
         }
+        if (m == ninf) l = 0.f;                        // no key seen
         if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), (uint32_t)outs & 1u, abort_flag)) ok = false;
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_fence_after();

@@ -263,6 +263,21 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
     unpair(x, a, b);
     return pair(fast_exp2(a), fast_exp2(b));
 }
+// (the arithmetic of exp2_fma_pair, for -125 <= x < 127)
+__device__ __forceinline__ uint64_t exp2_fma_core(uint64_t x) {
+    const uint64_t t = add_pair(x, pair(12582912.0f, 12582912.0f));
+    const uint64_t f = fma_pair(add_pair(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
+    uint64_t p = pair(0.001326472731307149f, 0.001326472731307149f);
+    p = fma_pair(p, f, pair(0.009671512991189957f, 0.009671512991189957f));
+    p = fma_pair(p, f, pair(0.05550733581185341f, 0.05550733581185341f));
+    p = fma_pair(p, f, pair(0.24022242426872253f, 0.24022242426872253f));
+    p = fma_pair(p, f, pair(0.6931470036506653f, 0.6931470036506653f));
+    p = fma_pair(p, f, pair(1.0f, 1.0f));
+    float p0, p1, t0, t1;
+    unpair(p, p0, p1);
+    unpair(t, t0, t1);
+    return pair(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
+}
 // The same for x < 127 on the FMA pipe: round x to an integer with the 1.5 * 2^23 trick, a degree-5 polynomial for 2^f on f in
 // [-0.5, 0.5] (relative error 2e-7, that of ex2.approx), and the integer added to the exponent.  Used for a share of an
 // epilogue's exponentials so that both pipes work.  The addition runs into the sign bit from x = 129 on: a huge argument
@@ -279,19 +294,7 @@ __device__ __forceinline__ uint64_t exp2_fma_pair(uint64_t x) {
         a = fminf(a, 126.0f);
         b = fminf(b, 126.0f);
     }
-    x = pair(a, b);
-    const uint64_t t = add_pair(x, pair(12582912.0f, 12582912.0f));
-    const uint64_t f = fma_pair(add_pair(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
-    uint64_t p = pair(0.001326472731307149f, 0.001326472731307149f);
-    p = fma_pair(p, f, pair(0.009671512991189957f, 0.009671512991189957f));
-    p = fma_pair(p, f, pair(0.05550733581185341f, 0.05550733581185341f));
-    p = fma_pair(p, f, pair(0.24022242426872253f, 0.24022242426872253f));
-    p = fma_pair(p, f, pair(0.6931470036506653f, 0.6931470036506653f));
-    p = fma_pair(p, f, pair(1.0f, 1.0f));
-    float p0, p1, t0, t1;
-    unpair(p, p0, p1);
-    unpair(t, t0, t1);
-    return pair(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
+    return exp2_fma_core(pair(a, b));
 }
 
 // Shared-memory matrix descriptor of a K-major tile stored as rows of 128 bytes
