@@ -3,10 +3,12 @@
 // An item is a tile of 128 query rows: 128 / G consecutive rows of a document with all G query heads of one K/V head, so that
 // few rows fill a tile too, and a tile's rows end at nearly the same key.  A CTA works on two items side by side (a pair: neighbours
 // in the document), which use the same K and V tiles.  Per tile of 128 keys and item x:
-//   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, fp32 in tensor memory (128 columns)
-//   P_x = 2^(logit - m)  one thread per row; bf16, written over S_x in tensor memory (64 columns)
+//   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, fp32 in tensor memory
+//   P_x = 2^(logit - m)  one thread per row; bf16, written over S_x in tensor memory
 //   O_x += P_x V         tcgen05.mma, P_x from tensor memory, V as it lies (keys x dh: the second operand's other order)
-// S_0, S_1, O_0 and O_1 fill the 512 columns.  While one item's rows are in their exponentials the other's products run.
+// S_0, S_1, O_0 and O_1 fill the 512 columns (128 each).  The halves of S_x, of 64 keys each, go round by themselves: while the rows make one
+// half's weights, the other's are multiplied with V and the next tile's logits take its place, so that the rows never wait for
+// a product.  (S_x whole, the rows waited for two products a tile: 28 heads, 4624 rows, 370 us.)
 //
 // The key tiles of all pairs of all documents and K/V heads form one line, and every CTA (one per SM) takes an equal piece of it:
 // a piece may begin and end inside a pair, whose parts are then joined by a second kernel.  So a batch of documents of any lengths,
@@ -194,7 +196,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     using S = MmaShape<DH>;
     grid_dep_wait();
     extern __shared__ uint8_t smem_dyn[];
-    __shared__ __align__(8) uint64_t q_bar, q_free_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2], p_bar[2][2], h_bar[2], o_bar[2], o_free_bar[2], drain_bar[2];
+    __shared__ __align__(8) uint64_t q_bar, q_free_bar, full_bar[S::kStages], empty_bar[S::kStages], s_bar[2][2], p_bar[2][2], h_bar[2], o_bar[2], o_free_bar[2], drain_bar[2];
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort;
     __shared__ __align__(16) float s_pos[2][2][kN];    // [item][buffer]: positions of the keys
@@ -306,7 +308,12 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         mbar_init(smem_u32(&drain_bar[0]), 1);
         mbar_init(smem_u32(&drain_bar[1]), 1);
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 2); }
-        for (int x = 0; x < 2; ++x) { mbar_init(smem_u32(&s_bar[x]), 1); mbar_init(smem_u32(&o_bar[x]), 1); mbar_init(smem_u32(&h_bar[x]), 1); mbar_init(smem_u32(&o_free_bar[x]), 4); for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&p_bar[x][p]), 4); }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(smem_u32(&o_bar[x]), 1);
+            mbar_init(smem_u32(&h_bar[x]), 1);
+            mbar_init(smem_u32(&o_free_bar[x]), 4);
+            for (int p = 0; p < 2; ++p) { mbar_init(smem_u32(&s_bar[x][p]), 1); mbar_init(smem_u32(&p_bar[x][p]), 4); }
+        }
         s_abort = 0;
         mbar_fence_init();
     }
@@ -392,7 +399,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         }
     } else if (warp >= 9) {
         // ---- products of item x
-        constexpr uint32_t idesc_s = make_idesc_bf16(kM, kN), idesc_o = make_idesc_bf16(kM, DH) | (1u << 16);
+        constexpr uint32_t idesc_s = make_idesc_bf16(kM, kN / 2), idesc_o = make_idesc_bf16(kM, DH) | (1u << 16);
         const int x = warp - 9;
         const uint32_t t_s = tmem + (uint32_t)x * kN, t_o = tmem + 2 * kN + (uint32_t)x * DH;
         const uint32_t q_lo = desc_k128_lo(q_addr(x)), k_lo0 = desc_k128_lo(kv_addr(0)), v_lo0 = desc_v_lo(kv_addr(0), S::kBlk);
@@ -402,16 +409,16 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         while (ok && walk.left > 0) {
             const Part q = part_of(walk);
             const int nt = uniform(q.nt), top = uniform(q.lo + q.nt - 1), st = uniform(x ? q.st[1] : q.st[0]), Lk = uniform(walk.d.Lk);
-            auto logits = [&](int it) {                // S of the key tile at `it`
-                const uint32_t k_lo = k_lo0 + (uint32_t)(it % S::kStages) * (S::kTile >> 4);
+            auto logits = [&](int it, int half) {      // S of 64 keys of the tile at `it`
+                const uint32_t k_lo = k_lo0 + (uint32_t)(it % S::kStages) * (S::kTile >> 4) + (uint32_t)half * 512u;
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < DH / 16; ++kk) {
                         constexpr uint32_t kNext = S::kBlk >> 4;
-                        umma_bf16_words(t_s, q_lo + (kk >> 2) * kNext + (kk & 3) * 2, k_lo + (kk >> 2) * kNext + (kk & 3) * 2, idesc_s, kk != 0 ? 1u : 0u);
+                        umma_bf16_words(t_s + half * 64, q_lo + (kk >> 2) * kNext + (kk & 3) * 2, k_lo + (kk >> 2) * kNext + (kk & 3) * 2, idesc_s, kk != 0 ? 1u : 0u);
                     }
-                    umma_commit(smem_u32(&s_bar[x]));
-                    umma_commit(smem_u32(&empty_bar[it % S::kStages]));
+                    umma_commit(smem_u32(&s_bar[x][half]));
+                    if (half) umma_commit(smem_u32(&empty_bar[it % S::kStages]));
                 }
                 __syncwarp();
             };
@@ -428,7 +435,8 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     ok = mbar_wait_warp(smem_u32(&q_bar), (uint32_t)np & 1u, abort_flag) && wait_full(it0 + 2 * st);
                     if (ok) {
                         tc_fence_after();
-                        logits(it0 + 2 * st);
+                        logits(it0 + 2 * st, 0);
+                        logits(it0 + 2 * st, 1);
                     }
                 }
                 for (int j = st; ok && j < nt; ++j) {
@@ -447,23 +455,22 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     if (j == st && !(ok = mbar_wait_warp(smem_u32(&o_free_bar[x]), (uint32_t)(outs & 1) ^ 1u, abort_flag))) break;
                     const uint32_t v_lo = v_lo0 + (uint32_t)vs * (S::kTile >> 4);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {         // O += P V of 64 keys: the first ones' weights are there while the others are made
+                    for (int half = 0; half < 2; ++half) {         // O += P V of 64 keys; then the next tile's logits go to their place
                         if (!(ok = mbar_wait_warp(smem_u32(&p_bar[x][half]), (uint32_t)seen & 1u, abort_flag))) break;
                         tc_fence_after();
                         if (elect_one()) {
 #pragma unroll
-                            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                                umma_bf16_ts(t_o, t_s + kk * 8, v_lo + kk * 128, idesc_o, kk > 0 || j > st ? 1u : 0u);
-                            if (!half) umma_commit(smem_u32(&h_bar[x]));
-                            else umma_commit(smem_u32(&empty_bar[vs]));
+                            for (int kk = 0; kk < 4; ++kk)
+                                umma_bf16_ts(t_o, t_s + half * 64 + kk * 8, v_lo + (half * 4 + kk) * 128, idesc_o, half || kk > 0 || j > st ? 1u : 0u);
+                            umma_commit(smem_u32(&h_bar[x]));
+                            if (half) umma_commit(smem_u32(&empty_bar[vs]));
                             if (half && j + 1 == nt) umma_commit(smem_u32(&o_bar[x]));
                         }
                         __syncwarp();
-                    }
-                    if (!ok) break;
-                    if (j + 1 < nt) {
-                        if (!(ok = wait_full(vi + 1))) break;
-                        logits(vi + 1);
+                        if (j + 1 < nt) {
+                            if (!half && !(ok = wait_full(vi + 1))) break;
+                            logits(vi + 1, half);
+                        }
                     }
                 }
                 // Q has been read, or was not wanted
@@ -530,13 +537,13 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 next_pos = prompt_position(a, k_first, k_rows, k0 - kN + r);
                 named_bar_sync(1 + x, 128);
             }
-            if (ok && !mbar_wait(smem_u32(&s_bar[x]), (uint32_t)seen & 1u, abort_flag)) ok = false;
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) continue;                         // (keeps meeting the item's other warps where they meet)
-            tc_fence_after();
             const bool masked = k0 + kN > sure;
 #pragma unroll 1                                       // (one copy of the code: the instruction cache is short)
             for (int half = 0; half < 2; ++half) {     // 64 keys
+                if (ok && !mbar_wait(smem_u32(&s_bar[x][half]), (uint32_t)seen & 1u, abort_flag)) ok = false;
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) continue;                     // (keeps meeting the item's other warps where they meet)
+                tc_fence_after();
                 uint32_t raw[2][32];
                 tmem_ld32_issue(t_s + half * 64, raw[0]);
                 tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
@@ -616,11 +623,10 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     const float f = grow ? fast_exp2(m - mx) : 1.f;
                     if (grow) m = mx;
                     l *= f;
-                    // the product before this one on O_x is complete: that of the tile before since S_x is there, that of the first half when its barrier says so
-                    if (half && ok && !mbar_wait(smem_u32(&h_bar[x]), (uint32_t)seen & 1u, abort_flag)) ok = false;
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    tc_fence_after();
-                    if (j > 0 || half) {
+                    if (j > 0 || half) {               // when the product before this one on O_x is complete
+                        if (!mbar_wait(smem_u32(&h_bar[x]), (uint32_t)(half ^ 1), abort_flag)) ok = false;
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        tc_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < DH / 16; ++c) {
                             float o[16];
@@ -650,7 +656,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 float s0, s1;
                 unpair(add_pair(sum0, sum1), s0, s1);
                 l += s0 + s1;
-                tmem_st32(t_s + half * 32, p);         // their product may begin
+                tmem_st32(t_s + half * 64, p);         // their product may begin
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
