@@ -18,7 +18,8 @@ struct PromptArgs {
     float scale_log2, cap_scale, cap_log2;     // softcap > 0: x = cap_log2 * tanh(dot * cap_scale); else cap_log2 is 0 (log2 units)
     int causal;
     int splits;                                // fp32: parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
-    int heads_item, head_chunks;               // bf16: query heads of a tile of 128 rows, such tiles for all heads of a K/V head
+    int heads_item, head_chunks, rows_item;    // bf16: query heads of a tile of 128 rows, such tiles for all heads of a K/V head, document rows of a tile
+    uint32_t rows_magic;                       // ceil(2^32 / rows_item)
     float *part_o, *part_ml;                   // unnormalised outputs and (maximum, sum) of the parts; fp32: [splits][Hq][n_q]
     void* cuts;                                // bf16: what the second kernel joins
     int32_t* status;

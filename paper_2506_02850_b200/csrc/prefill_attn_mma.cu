@@ -37,15 +37,14 @@ constexpr int kM = 128, kN = 128, kThreads = 352;
 constexpr float kGrow = 16.f;                          // octaves by which a logit may pass the row's reference
 constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
-constexpr int kFewest = 2;                             // steps of the line that a CTA is given at least, on average
-
 template <int DH>
 struct MmaShape {
     static constexpr int KB = DH / 64;                 // 128-byte pieces of a row
     static constexpr uint32_t kBlk = 128 * 128;        // bytes of a piece of a tile's 128 rows
     static constexpr uint32_t kTile = KB * kBlk;
     static constexpr int kStages = DH == 128 ? 4 : 8;  // K and V tiles on their way
-    static constexpr size_t kSmem = (size_t)(2 + kStages) * kTile + 1024;
+    static constexpr uint32_t kStagePad = 2048;        // a rows' warp turns 32 columns of its output round in this
+    static constexpr size_t kSmem = (size_t)(2 + kStages) * kTile + 8 * kStagePad + 1024;
 };
 
 // 32 registers of this thread's lane to 32 tensor-memory columns.
@@ -116,27 +115,26 @@ struct MmaMaps {
     int k_step, v_step;                                // 1, or 0 where all K/V heads are the same rows
 };
 
-// How rows and heads make items.
-__device__ __forceinline__ int item_rows(const PromptArgs& a) { return a.heads_item < kM ? kM / a.heads_item : 1; }
+// x / rows_item for x up to 2^25 - 1 (rows_item <= 128: the host's reciprocal is exact there).
+__device__ __forceinline__ int div_rows(const PromptArgs& a, int x) { return a.rows_item == 1 ? x : (int)__umulhi((uint32_t)x, a.rows_magic); }
+// Item -> (block of rows, chunk of heads).
+__device__ __forceinline__ int item_block(const PromptArgs& a, int item) { return a.head_chunks == 1 ? item : item / a.head_chunks; }
 
 // A pair's place in its document, and what its items need.
 struct Pair {
     int i0[2], h0[2], rows[2], n[2];                   // first row, first head (of the K/V head's), rows of the tile in use, key tiles
     int nt;                                            // key tiles of the pair
 };
-__device__ __forceinline__ int doc_items(const PromptArgs& a, int Lq) {
-    const int r = item_rows(a);
-    return (Lq + r - 1) / r * a.head_chunks;
-}
+__device__ __forceinline__ int doc_items(const PromptArgs& a, int Lq) { return div_rows(a, Lq + a.rows_item - 1) * a.head_chunks; }
 __device__ __forceinline__ Pair pair_of(const PromptArgs& a, const PromptDoc& d, int t) {
     Pair p;
-    const int r = item_rows(a), items = doc_items(a, d.Lq);
+    const int r = a.rows_item, items = doc_items(a, d.Lq);
     p.nt = 0;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int item = 2 * t + x;
         const bool there = item < items;
-        const int blk = there ? item / a.head_chunks : 0, ch = there ? item - blk * a.head_chunks : 0;
+        const int blk = there ? item_block(a, item) : 0, ch = there ? item - blk * a.head_chunks : 0;
         p.i0[x] = blk * r;
         p.h0[x] = ch * a.heads_item;
         const int nr = there ? min(r, d.Lq - p.i0[x]) : 0;
@@ -148,7 +146,7 @@ __device__ __forceinline__ Pair pair_of(const PromptArgs& a, const PromptDoc& d,
 }
 // Steps of a pair in the line: its key tiles, and one where it has none.
 __device__ __forceinline__ int pair_steps(const PromptArgs& a, const PromptDoc& d, int t) {
-    const int last = min(2 * t + 1, doc_items(a, d.Lq) - 1) / a.head_chunks, r = item_rows(a);
+    const int last = item_block(a, min(2 * t + 1, doc_items(a, d.Lq) - 1)), r = a.rows_item;
     return max(1, (prompt_keys(a, d, min(d.Lq, (last + 1) * r) - 1) + kN - 1) / kN);
 }
 __device__ __forceinline__ int doc_pairs(const PromptArgs& a, int Lq) { return (doc_items(a, Lq) + 1) / 2; }
@@ -182,6 +180,22 @@ __device__ __forceinline__ void walk_on(const PromptArgs& a, Walk& w, int steps)
         w.pairs = doc_pairs(a, w.d.Lq);
     } while (w.pairs == 0 && w.g < a.Hkv);
 }
+
+// The line of `all` steps in `ctas` pieces that differ by one step at most: the longer ones first.
+struct Line {
+    long long piece;
+    int ctas, longer;
+    __device__ __forceinline__ Line(long long all, int n) {
+        ctas = (int)max(1LL, min((long long)n, all));
+        piece = all < (1LL << 31) ? (long long)((uint32_t)all / (uint32_t)ctas) : all / ctas;
+        longer = (int)(all - piece * ctas);
+    }
+    __device__ __forceinline__ long long begin(int c) const { return piece * c + min(c, longer); }
+    __device__ __forceinline__ int holder(long long step) const {      // the CTA whose piece has the step
+        const long long edge = (piece + 1) * longer;
+        return step < edge ? (int)(step / (piece + 1)) : longer + (int)((step - edge) / piece);
+    }
+};
 
 // What the second kernel joins: the parts of the pair that CTAs c0 .. c1 share, noted by CTA c0 + 1.
 struct Cut {
@@ -250,11 +264,13 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     }
     __syncthreads();
     const long long per_head = s_pre[a.n_seq], all = per_head * a.Hkv;
-    const long long ctas = max(1LL, min((long long)gridDim.x, all / kFewest));
-    if (blockIdx.x >= ctas || all == 0) return;        // uniform
-    const long long begin = all * blockIdx.x / ctas, end = all * (blockIdx.x + 1) / ctas;
+    if (all == 0) return;                              // uniform, as below
+    const Line line(all, gridDim.x);
+    if (blockIdx.x >= line.ctas) return;
+    const long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
     if (warp == 0) {
-        const int g = (int)(begin / per_head);
+        int g = 0;
+        if (a.Hkv > 1) g = all < (1LL << 31) ? (int)((uint32_t)begin / (uint32_t)per_head) : (int)(begin / per_head);
         const long long at = begin - g * per_head;
         int lo = 0, hi = a.n_seq;                      // the document: s_pre[lo] <= at < s_pre[hi]
         while (hi - lo > 1) {
@@ -363,7 +379,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 if (!mbar_wait_warp(smem_u32(&q_free_bar), (uint32_t)(np & 1) ^ 1u, abort_flag)) { ok = false; break; }
                 if (elect_one()) {
                     const int both = q.p.rows[1] > 0 ? 2 : 1;
-                    mbar_arrive_expect_tx(smem_u32(&q_bar), (uint32_t)both * S::KB * (uint32_t)(item_rows(a) * a.heads_item) * 128u);
+                    mbar_arrive_expect_tx(smem_u32(&q_bar), (uint32_t)both * S::KB * (uint32_t)(a.rows_item * a.heads_item) * 128u);
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
                         if (x < both) {
@@ -672,11 +688,30 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         const int my_i0 = x ? part.p.i0[1] : part.p.i0[0], h0 = x ? part.p.h0[1] : part.p.h0[0], my_head = my_walk->g * a.G + h0 + my_h;
         const bool mine = r < (x ? part.p.rows[1] : part.p.rows[0]) && h0 + my_h < a.G, whole = part.whole;
         const long long row = d.q0 + my_i0 + my_i;
-        const long long at = (2LL * blockIdx.x + (first_part ? 0 : 1)) * (2 * kM) + x * kM + r;    // row of this CTA's two partial pairs
-        const float scale = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)my_head * a.out_head + row * a.out_row;
-        if (ok) {
+        // partial outputs lie [slot][16-byte piece][row]: a warp's rows side by side
+        const long long slot = 2LL * blockIdx.x + (first_part ? 0 : 1), at = slot * (2 * kM) + x * kM + r;
+        if (ok && !whole && my_n > 0) {
+            float4* part_o = reinterpret_cast<float4*>(a.part_o) + slot * (2 * kM) * (DH / 4) + x * kM + r;
+#pragma unroll 1                                       // (code that runs once per part comes from memory: short is fast)
+            for (int c = 0; c < DH / 16; ++c) {
+                float o[16];
+                tmem_ld16(t_o + c * 16, o);
+                if (mine) {
 #pragma unroll
+                    for (int i = 0; i < 4; ++i) part_o[(c * 4 + i) * (2 * kM)] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                }
+            }
+        }
+        if (ok && whole) {
+            // 32 columns at a time through shared memory, so that four lanes write 64 bytes of a row (each lane its own row: a store instruction
+            // of 32 lines, 4 us a part)
+            const float scale = l > 0.f ? 1.f / l : 0.f;
+            const long long to = mine ? (long long)my_head * a.out_head + row * a.out_row : -1;
+            const uint32_t pad = smem_base + (2 + S::kStages) * S::kTile + (uint32_t)warp * S::kStagePad;
+            long long dst[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = __shfl_sync(0xFFFFFFFFu, to, i * 8 + (lane >> 2));
+#pragma unroll 1
             for (int c = 0; c < DH / 32; ++c) {
                 float o[32];
                 if (my_n > 0) {
@@ -685,19 +720,26 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = 0.f;
                 }
-                if (!mine) continue;
-                if (!whole) {
-                    if (my_n > 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(a.part_o + at * DH + c * 32 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8)
-                        *reinterpret_cast<uint4*>(out + c * 32 + i) = make_uint4(pack_bf16(o[i] * scale, o[i + 1] * scale), pack_bf16(o[i + 2] * scale, o[i + 3] * scale),
-                                                                                 pack_bf16(o[i + 4] * scale, o[i + 5] * scale), pack_bf16(o[i + 6] * scale, o[i + 7] * scale));
+                for (int i = 0; i < 4; ++i) {
+                    const float* v = o + 8 * i;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(pad + (uint32_t)(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4))),
+                                 "r"(pack_bf16(v[0] * scale, v[1] * scale)), "r"(pack_bf16(v[2] * scale, v[3] * scale)), "r"(pack_bf16(v[4] * scale, v[5] * scale)),
+                                 "r"(pack_bf16(v[6] * scale, v[7] * scale)) : "memory");
                 }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int rr = i * 8 + (lane >> 2), e = lane & 3;
+                    uint4 v;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                 : "r"(pad + (uint32_t)(rr * 64 + ((e ^ ((rr >> 1) & 3)) << 4))) : "memory");
+                    if (dst[i] >= 0) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + dst[i] + c * 32 + e * 8) = v;
+                }
+                __syncwarp();
             }
+        }
+        if (ok) {
             if (mine && !whole) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(l > 0.f ? m : ninf, l);
             else if (mine && a.lse) a.lse[(long long)my_head * a.n_q + row] = kAttnLn2 * (m + log2f(l));
         }
@@ -710,13 +752,13 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         // a pair that began in another CTA: the second of those that share it notes what there is to join
         if (threadIdx.x == 0 && first_part && my_walk->e0 > 0) {
             const int steps = max(1, part.p.nt);
-            const long long f0 = begin - my_walk->e0;      // the pair's place in the line; CTA c's piece begins at all * c / ctas
-            const long long c0 = ((f0 + 1) * ctas - 1) / all, c1 = ((f0 + steps) * ctas - 1) / all;
-            if (c0 + 1 == (long long)blockIdx.x) {
+            const long long f0 = begin - my_walk->e0;  // the pair's place in the line
+            const int c0 = line.holder(f0), c1 = line.holder(f0 + steps - 1);
+            if (c0 + 1 == blockIdx.x) {
                 Cut cut;
-                cut.c0 = (int)c0;
-                cut.c1 = (int)c1;
-                cut.first_slot = 2 * (int)c0 + (all * c0 / ctas >= f0 ? 0 : 1);
+                cut.c0 = c0;
+                cut.c1 = c1;
+                cut.first_slot = 2 * c0 + (line.begin(c0) >= f0 ? 0 : 1);
                 cut.q0 = d.q0;
                 cut.g = my_walk->g;
                 cut.Lq = d.Lq;
@@ -741,53 +783,56 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
-// Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut; a warp per row.
-constexpr int kCutWarps = 8, kCutBlocks = 2 * kM / kCutWarps;
+// Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut.  A lane per row, a warp for DH / 8 columns of 32 rows,
+// two parts on their way.
+constexpr int kCutBlocks = 2 * kM / 32;
 template <int DH>
-__global__ void __launch_bounds__(kCutWarps * 32)
+__global__ void __launch_bounds__(256)
 prompt_cut_join_kernel(const PromptArgs a) {
     grid_dep_wait();
     const Cut cut = reinterpret_cast<const Cut*>(a.cuts)[blockIdx.x];
     if (cut.c1 < 0) return;
-    const int lane = threadIdx.x & 31, rr = blockIdx.y * kCutWarps + (threadIdx.x >> 5), x = rr / kM, r = rr - x * kM;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = blockIdx.y * 32 + lane, x = rr / kM, r = rr - x * kM;
     const int i = r / a.heads_item, h = (x ? cut.h0[1] : cut.h0[0]) + r - i * a.heads_item;
     if (r >= (x ? cut.rows[1] : cut.rows[0]) || h >= a.G) return;
     const int parts = cut.c1 - cut.c0 + 1, head = cut.g * a.G + h;
     const long long row = cut.q0 + (x ? cut.i0[1] : cut.i0[0]) + i;
-    auto place = [&](int p) { return (long long)(p == 0 ? cut.first_slot : 2 * (cut.c0 + p)) * (2 * kM) + rr; };
+    auto slot = [&](int p) { return (size_t)(p == 0 ? cut.first_slot : 2 * (cut.c0 + p)); };
     const float ninf = __int_as_float(0xFF800000);
-    float M = ninf;
-    for (int p = lane; p < parts; p += 32) M = fmaxf(M, a.part_ml[place(p) * 2]);
+    constexpr int E = DH / 32;                         // 16-byte pieces of a warp's columns
+    float M = ninf, L = 0.f;
+    float4 acc[E];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-    constexpr int E = DH / 32, kAhead = 4;
-    float acc[E], L = 0.f;
+    for (int e = 0; e < E; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < parts; p0 += 2) {
+        float2 ml[2];
+        float4 o[2][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int p0 = 0; p0 < parts; p0 += kAhead) {
-        float2 ml[kAhead];
-        float o[kAhead][E];
+        for (int u = 0; u < 2; ++u) {
+            const bool in = p0 + u < parts;
+            ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + (slot(p0 + u) * (2 * kM) + rr) * 2) : make_float2(ninf, 0.f);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            ml[u] = make_float2(ninf, 0.f);
-            if (p0 + u < parts) ml[u] = *reinterpret_cast<const float2*>(a.part_ml + place(p0 + u) * 2);
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[u][e] = p0 + u < parts ? a.part_o[place(p0 + u) * DH + lane * E + e] : 0.f;
+            for (int e = 0; e < E; ++e)
+                o[u][e] = in ? reinterpret_cast<const float4*>(a.part_o)[(slot(p0 + u) * (DH / 4) + warp * E + e) * (2 * kM) + rr] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < 2; ++u) {
             if (!(ml[u].y > 0.f)) continue;            // a part of no keys has written no output
-            const float f = sm100::fast_exp2(ml[u].x - M);
-            L += f * ml[u].y;
+            const float top = fmaxf(M, ml[u].x), f = sm100::fast_exp2(M - top), g = sm100::fast_exp2(ml[u].x - top);
+            M = top;
+            L = L * f + ml[u].y * g;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += f * o[u][e];
+            for (int e = 0; e < E; ++e)
+                acc[e] = make_float4(acc[e].x * f + o[u][e].x * g, acc[e].y * f + o[u][e].y * g, acc[e].z * f + o[u][e].z * g, acc[e].w * f + o[u][e].w * g);
         }
     }
     const float inv = L > 0.f ? 1.f / L : 0.f;
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)head * a.out_head + row * a.out_row;
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[lane * E + e] = __float2bfloat16_rn(acc[e] * inv);
-    if (lane == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
+    for (int e = 0; e < E; e += 2)
+        reinterpret_cast<uint4*>(out)[(warp * E + e) / 2] = make_uint4(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv),
+                                                                       pack_bf16(acc[e + 1].x * inv, acc[e + 1].y * inv), pack_bf16(acc[e + 1].z * inv, acc[e + 1].w * inv));
+    if (warp == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
 }
 
 template <int DH, bool kCap, bool kBias>
@@ -801,7 +846,7 @@ int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
     METOK_LAUNCH_CHECK();
     {
         METOK_TIMED("prompt_cut_join", st);
-        launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks), dim3(kCutWarps * 32), 0, st, a);
+        launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks), dim3(256), 0, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;
@@ -823,12 +868,14 @@ void prompt_mma_carve(Carver& cv, int dh, PromptArgs* a) {
 int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st) {
     MmaMaps maps = {};
     a.heads_item = std::min(a.G, kM);
+    a.rows_item = kM / a.heads_item;
+    a.rows_magic = a.rows_item > 1 ? (uint32_t)((0x100000000ULL + a.rows_item - 1) / a.rows_item) : 0u;
     a.head_chunks = ceil_div(a.G, a.heads_item);
     maps.k_step = a.Hkv > 1 && a.k_head > 0;
     maps.v_step = a.Hkv > 1 && a.v_head > 0;
     if (a.n_q > 0) {
         // Q: heads of a row side by side
-        int rc = make_tmap_3d(&maps.q, a.q, dh, a.Hq, a.n_q, a.Hq > 1 ? a.q_head : a.q_row, a.q_row, a.heads_item, kM / a.heads_item);
+        int rc = make_tmap_3d(&maps.q, a.q, dh, a.Hq, a.n_q, a.Hq > 1 ? a.q_head : a.q_row, a.q_row, a.heads_item, a.rows_item);
         // where there are no keys no tile of them is asked for, and any rows will do
         if (rc == METOK_OK) rc = a.n_k ? make_tmap_3d(&maps.k, a.k, dh, a.n_k, maps.k_step ? a.Hkv : 1, a.k_row, maps.k_step ? a.k_head : a.k_row, kN, 1) : (maps.k = maps.q, METOK_OK);
         if (rc == METOK_OK) rc = a.n_k ? make_tmap_3d(&maps.v, a.v, dh, a.n_k, maps.v_step ? a.Hkv : 1, a.v_row, maps.v_step ? a.v_head : a.v_row, kN, 1) : (maps.v = maps.q, METOK_OK);
