@@ -1,9 +1,11 @@
 // metok_prefill_attention: the C entry, the fp32 kernel, and the join of split keys.  (bf16: prefill_attn_mma.cu.)
 //
-// fp32, on the CUDA cores: a CTA of 256 threads takes 64 query rows of a head and walks their keys in tiles of 64.  Thread (ty, tx)
-// holds the logits of rows 4 ty + i and keys tx + 16 j, and the outputs of the same rows; a row's running maximum and
-// sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling from row to
-// row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
+// fp32, on the CUDA cores: a CTA of 256 threads takes 16 R query rows of a head and walks their keys in tiles of 64, of which the next
+// one is on its way while one is worked on.  Thread (ty, tx) holds the logits of rows R ty + i and keys tx + 16 j, and the outputs of the
+// same rows; a row's running maximum and sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with
+// n not falling from row to row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
+// R = 4 feeds the multiply-adds (two of them per shared-memory wavefront); R = 1 is for calls that leave most SMs without a tile, where a
+// tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4.
 #include <algorithm>
 
 #include "launchers.h"
@@ -14,46 +16,58 @@ namespace metok {
 
 namespace {
 
-constexpr int kSM = 64, kSN = 64, kSThreads = 256;
+constexpr int kSN = 64, kSThreads = 256;
 
-template <int DH>
+template <int DH, int R>
 struct SimtAttnSmem {
-    float q[kSM][DH + 4], k[kSN][DH + 4], v[kSN][DH], p[kSM][kSN + 4];
-    float pos[kSN];
+    float q[16 * R][DH + 4], k[2][kSN][DH + 4], v[2][kSN][DH], p[16 * R][kSN + 4];
+    float pos[2][kSN];
 };
 
-template <int DH>
+template <int DH, int R>
 __global__ void __launch_bounds__(kSThreads)
 prompt_attn_simt_kernel(const PromptArgs a) {
-    using T = float;
+    constexpr int kSM = 16 * R;
     grid_dep_wait();
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    SimtAttnSmem<DH>& sm = *reinterpret_cast<SimtAttnSmem<DH>*>(smem_raw);
+    SimtAttnSmem<DH, R>& sm = *reinterpret_cast<SimtAttnSmem<DH, R>*>(smem_raw);
     const int h = blockIdx.x % a.Hq, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hq, [](int Lq) { return (Lq + kSM - 1) / kSM; });
     if (d.tile < 0) return;
     const int i0 = d.tile * kSM, rows = min(kSM, d.Lq - i0), g = h / a.G;
     const int first_keys = prompt_keys(a, d, i0), all_keys = prompt_keys(a, d, i0 + rows - 1);
     const int nt = (all_keys + kSN - 1) / kSN, t_lo = (int)((long long)nt * blockIdx.y / a.splits), t_hi = (int)((long long)nt * (blockIdx.y + 1) / a.splits);
-    const T* q = reinterpret_cast<const T*>(a.q) + h * a.q_head + (long long)(d.q0 + i0) * a.q_row;
-    const T* k = reinterpret_cast<const T*>(a.k) + g * a.k_head + (long long)d.k0 * a.k_row;
-    const T* v = reinterpret_cast<const T*>(a.v) + g * a.v_head + (long long)d.k0 * a.v_row;
-    constexpr int VE = Vec16<T>::N, CPR = DH / VE;     // elements of a 16-byte piece, pieces of a row
+    const float* q = reinterpret_cast<const float*>(a.q) + h * a.q_head + (long long)(d.q0 + i0) * a.q_row;
+    const float* k = reinterpret_cast<const float*>(a.k) + g * a.k_head + (long long)d.k0 * a.k_row;
+    const float* v = reinterpret_cast<const float*>(a.v) + g * a.v_head + (long long)d.k0 * a.v_row;
+    constexpr int CPR = DH / 4;                        // 16-byte pieces of a row
+    auto fetch = [&](int t) {                          // rows behind the document's keys count as zeros
+        const int b = t & 1, j0 = t * kSN;
+        for (int c = tid; c < kSN * CPR; c += kSThreads) {
+            const int r = c / CPR, e = (c - r * CPR) * 4;
+            const uint32_t bytes = j0 + r < d.Lk ? 16u : 0u;
+            const long long row = bytes ? j0 + r : 0;
+            sm100::cp_async16_zfill(sm100::smem_u32(&sm.k[b][r][e]), k + row * a.k_row + e, bytes);
+            sm100::cp_async16_zfill(sm100::smem_u32(&sm.v[b][r][e]), v + row * a.v_row + e, bytes);
+        }
+        if (a.slopes && tid < kSN) sm.pos[b][tid] = prompt_position(a, d.k0, d.Lk, j0 + tid);
+        sm100::cp_async_commit();
+    };
+    if (t_lo < t_hi) fetch(t_lo);
     for (int c = tid; c < kSM * CPR; c += kSThreads) {
-        const int r = c / CPR, e = (c - r * CPR) * VE;
-        float x[VE];
-        if (r < rows) Vec16<T>::load(q + (long long)r * a.q_row + e, x);
-        else Vec16<T>::zero(x);
-#pragma unroll
-        for (int i = 0; i < VE; i += 4) *reinterpret_cast<float4*>(&sm.q[r][e + i]) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        const int r = c / CPR, e = (c - r * CPR) * 4;
+        float x[4];
+        if (r < rows) Vec16<float>::load(q + (long long)r * a.q_row + e, x);
+        else Vec16<float>::zero(x);
+        *reinterpret_cast<float4*>(&sm.q[r][e]) = make_float4(x[0], x[1], x[2], x[3]);
     }
-    int keys[4];
-    float my_pos[4], m[4], l[4], o[4][DH / 16];
+    int keys[R];
+    float my_pos[R], m[R], l[R], o[R][DH / 16];
     const float slope = a.slopes ? a.slopes[h] * kAttnLog2e : 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = i0 + ty * 4 + i;
-        keys[i] = ty * 4 + i < rows ? prompt_keys(a, d, r) : 0;
+    for (int i = 0; i < R; ++i) {
+        const int r = i0 + ty * R + i;
+        keys[i] = ty * R + i < rows ? prompt_keys(a, d, r) : 0;
         my_pos[i] = a.slopes ? prompt_position(a, d.k0, d.Lk, d.Lk - d.Lq + r) : 0.f;
         m[i] = __int_as_float(0xFF800000);
         l[i] = 0.f;
@@ -61,52 +75,41 @@ prompt_attn_simt_kernel(const PromptArgs a) {
         for (int c = 0; c < DH / 16; ++c) o[i][c] = 0.f;
     }
     for (int t = t_lo; t < t_hi; ++t) {
-        const int j0 = t * kSN;
-        __syncthreads();
-        for (int c = tid; c < kSN * CPR; c += kSThreads) {
-            const int r = c / CPR, e = (c - r * CPR) * VE;
-            float x[VE], y[VE];
-            if (j0 + r < d.Lk) {
-                Vec16<T>::load(k + (long long)(j0 + r) * a.k_row + e, x);
-                Vec16<T>::load(v + (long long)(j0 + r) * a.v_row + e, y);
-            } else {
-                Vec16<T>::zero(x);
-                Vec16<T>::zero(y);
-            }
-#pragma unroll
-            for (int i = 0; i < VE; i += 4) {
-                *reinterpret_cast<float4*>(&sm.k[r][e + i]) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-                *reinterpret_cast<float4*>(&sm.v[r][e + i]) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-            }
+        const int j0 = t * kSN, b = t & 1;
+        __syncthreads();                               // everybody is done with the tile before, whose place the next one takes
+        if (t + 1 < t_hi) {
+            fetch(t + 1);
+            sm100::cp_async_wait<1>();
+        } else {
+            sm100::cp_async_wait<0>();
         }
-        if (a.slopes && tid < kSN) sm.pos[tid] = prompt_position(a, d.k0, d.Lk, j0 + tid);
         __syncthreads();
-        float s[4][4];
+        float s[R][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
         for (int e = 0; e < DH; e += 4) {
-            float4 x[4], y[4];
+            float4 x[R], y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(&sm.q[ty * 4 + i][e]);
+            for (int i = 0; i < R; ++i) x[i] = *reinterpret_cast<const float4*>(&sm.q[ty * R + i][e]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][e]);
+            for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(&sm.k[b][tx + 16 * j][e]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < R; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
         }
         const bool masked = j0 + kSN > first_keys || rows < kSM;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R; ++i) {
             float top = m[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float x = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(s[i][j] * a.cap_scale) : s[i][j] * a.scale_log2;
-                if (a.slopes) x = fmaf(-slope, fabsf(my_pos[i] - sm.pos[tx + 16 * j]), x);
+                if (a.slopes) x = fmaf(-slope, fabsf(my_pos[i] - sm.pos[b][tx + 16 * j]), x);
                 if (masked && j0 + tx + 16 * j >= keys[i]) x = __int_as_float(0xFF800000);
                 s[i][j] = x;
                 top = fmaxf(top, x);
@@ -121,7 +124,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
             for (int j = 0; j < 4; ++j) {
                 s[i][j] = exp2f(s[i][j] - base);
                 sum += s[i][j];
-                sm.p[ty * 4 + i][tx + 16 * j] = s[i][j];
+                sm.p[ty * R + i][tx + 16 * j] = s[i][j];
             }
             l[i] = l[i] * f + sum;
 #pragma unroll
@@ -130,16 +133,16 @@ prompt_attn_simt_kernel(const PromptArgs a) {
         __syncwarp();                                  // a row's weights are written and read by one half of a warp
 #pragma unroll 2
         for (int j = 0; j < kSN; j += 4) {
-            float4 p[4];
+            float4 p[R];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.p[ty * 4 + i][j]);
+            for (int i = 0; i < R; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.p[ty * R + i][j]);
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
                 for (int c = 0; c < DH / 64; ++c) {
-                    const float4 x = *reinterpret_cast<const float4*>(&sm.v[j + jj][tx * 4 + 64 * c]);
+                    const float4 x = *reinterpret_cast<const float4*>(&sm.v[b][j + jj][tx * 4 + 64 * c]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < R; ++i) {
                         const float w = jj == 0 ? p[i].x : jj == 1 ? p[i].y : jj == 2 ? p[i].z : p[i].w;
                         o[i][4 * c] = fmaf(w, x.x, o[i][4 * c]);
                         o[i][4 * c + 1] = fmaf(w, x.y, o[i][4 * c + 1]);
@@ -150,33 +153,28 @@ prompt_attn_simt_kernel(const PromptArgs a) {
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
 #pragma unroll
         for (int w = 8; w >= 1; w >>= 1) l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], w);
-        const int r = ty * 4 + i;
+        const int r = ty * R + i;
         if (r >= rows) continue;
         const long long row = d.q0 + i0 + r;
-        if (a.splits > 1) {
-            const long long at = ((long long)blockIdx.y * a.Hq + h) * a.n_q + row;
-#pragma unroll
-            for (int c = 0; c < DH / 64; ++c)
-                *reinterpret_cast<float4*>(a.part_o + at * DH + tx * 4 + 64 * c) = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
-            if (tx == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m[i], l[i]);
-            continue;
-        }
-        const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
-        T* out = reinterpret_cast<T*>(a.out) + h * a.out_head + row * a.out_row;
+        const bool part = a.splits > 1;
+        const float inv = part ? 1.f : l[i] > 0.f ? 1.f / l[i] : 0.f;
+        const long long at = ((long long)blockIdx.y * a.Hq + h) * a.n_q + row;
+        float* out = part ? a.part_o + at * DH : reinterpret_cast<float*>(a.out) + h * a.out_head + row * a.out_row;
 #pragma unroll
         for (int c = 0; c < DH / 64; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) from_float(out[tx * 4 + 64 * c + e], o[i][4 * c + e] * inv);
-        if (tx == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (m[i] + log2f(l[i]));
+            *reinterpret_cast<float4*>(out + tx * 4 + 64 * c) = make_float4(o[i][4 * c] * inv, o[i][4 * c + 1] * inv, o[i][4 * c + 2] * inv, o[i][4 * c + 3] * inv);
+        if (tx != 0) continue;
+        if (part) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m[i], l[i]);
+        else if (a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (m[i] + log2f(l[i]));
     }
 }
 
 // Joins the parts of split keys: a warp per row of a head.
 constexpr int kJoinWarps = 8;
-template <typename T, int DH>
+template <int DH>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 prompt_join_kernel(const PromptArgs a) {
     grid_dep_wait();
@@ -204,23 +202,26 @@ prompt_join_kernel(const PromptArgs a) {
         for (int e = 0; e < E; ++e) acc[e] += f * a.part_o[at * DH + lane * E + e];
     }
     const float inv = L > 0.f ? 1.f / L : 0.f;
-    T* out = reinterpret_cast<T*>(a.out) + h * a.out_head + row * a.out_row;
+    float* out = reinterpret_cast<float*>(a.out) + h * a.out_head + row * a.out_row;
 #pragma unroll
-    for (int e = 0; e < E; ++e) from_float(out[lane * E + e], acc[e] * inv);
+    for (int e = 0; e < E; ++e) out[lane * E + e] = acc[e] * inv;
     if (lane == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (M + log2f(L));
 }
 
-// fp32: CTAs without splits, and splits of the keys.
+// fp32: query rows of a tile, CTAs without splits, and splits of the keys.
 struct PromptPlan {
+    int rows;
     long long ctas;
     int splits;
 };
 // Tiles of all documents: at most a started one more per document than whole ones fit into n_q.
 PromptPlan prompt_plan(const metok_attention_params* p) {
     PromptPlan pl;
-    pl.ctas = std::max(1LL, (long long)p->n_q / kSM + std::min(p->n_seq, p->n_q)) * p->Hq;
+    auto ctas = [&](int rows) { return std::max(1LL, p->n_seq == 1 ? (long long)ceil_div(p->n_q, rows) : (long long)p->n_q / rows + std::min(p->n_seq, p->n_q)) * p->Hq; };
+    pl.rows = ctas(64) < kNumSMs ? 16 : 64;
+    pl.ctas = ctas(pl.rows);
     // few rows: the keys are cut until every SM has work, no part shorter than four tiles
-    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (4 * kSN), 2 * kNumSMs / pl.ctas, 64LL}));
+    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (4 * kSN), kNumSMs / pl.ctas, 64LL}));
     return pl;
 }
 void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, PromptArgs* a) {
@@ -232,18 +233,18 @@ void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, Prompt
     a->part_ml = cv.take<float>(rows * 2);
 }
 
-template <int DH>
+template <int DH, int R>
 int launch_prompt_simt(const PromptArgs& a, const PromptPlan& pl, cudaStream_t st) {
-    auto kern = prompt_attn_simt_kernel<DH>;
-    METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<DH>));
+    auto kern = prompt_attn_simt_kernel<DH, R>;
+    METOK_ALLOW_SMEM(kern, sizeof(SimtAttnSmem<DH, R>));
     {
         METOK_TIMED("prompt_attn_simt", st);
-        launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<DH>), st, a);
+        launch_chained(kern, dim3((unsigned)pl.ctas, pl.splits), dim3(kSThreads), sizeof(SimtAttnSmem<DH, R>), st, a);
     }
     METOK_LAUNCH_CHECK();
     if (pl.splits > 1) {
         METOK_TIMED("prompt_join", st);
-        launch_chained(prompt_join_kernel<float, DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
+        launch_chained(prompt_join_kernel<DH>, dim3(ceil_div(a.n_q, kJoinWarps), a.Hq), dim3(kJoinWarps * 32), 0, st, a);
         METOK_LAUNCH_CHECK();
     }
     return METOK_OK;
@@ -306,5 +307,6 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     if (dtype == METOK_BF16) return launch_prompt_attn_mma(a, p->dh, st);
     const PromptPlan pl = prompt_plan(p);
     a.splits = pl.splits;
-    return p->dh == 64 ? launch_prompt_simt<64>(a, pl, st) : launch_prompt_simt<128>(a, pl, st);
+    if (pl.rows == 16) return p->dh == 64 ? launch_prompt_simt<64, 1>(a, pl, st) : launch_prompt_simt<128, 1>(a, pl, st);
+    return p->dh == 64 ? launch_prompt_simt<64, 4>(a, pl, st) : launch_prompt_simt<128, 4>(a, pl, st);
 }
