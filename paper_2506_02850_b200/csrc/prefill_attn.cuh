@@ -16,6 +16,7 @@ struct PromptArgs {
     const int32_t *seq_q, *seq_k, *prefix_len, *positions;
     const float* slopes;
     float scale_log2, cap_scale, cap_log2;     // softcap > 0: x = cap_log2 * tanh(dot * cap_scale); else cap_log2 is 0 (log2 units)
+    float cap_poly[7];                         // bf16: cap_log2 * tanh(y) / y in powers of y^2, y = dot * cap_scale
     int causal;
     int splits;                                // fp32: parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
     int heads_item, head_chunks, rows_item;    // bf16: query heads of a tile of 128 rows, such tiles for all heads of a K/V head, document rows of a tile

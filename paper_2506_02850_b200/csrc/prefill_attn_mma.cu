@@ -16,9 +16,9 @@
 // piece by itself, from the documents' offsets.
 //
 // Key tiles of a pair are taken from the last one down (a bias makes the nearest ones the largest).  A row's reference m is the maximum of
-// the first 64 keys that it sees, and grows only where a later logit passes it by more than 2^16: any m within the range of
-// the exponent gives the same result, and a change costs a pass over O_x.  The row's own thread makes it, when the products before on
-// O_x are complete (one thread issues all of them, in order).
+// the first 64 keys that it sees; later weights are taken against it with no maximum of their own, since any m within the range of the
+// exponent gives the same result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x
+// and the row's sum are scaled: by the row's own thread, when the product before on O_x is complete.
 //
 // Warps 0-3 and 4-7: the rows of items 0 and 1; warp 8: TMA; warps 9 and 10: the products of items 0 and 1, each with waits of its
 // own (an issuing warp is held up while products run, so one warp's waits for both items lie open).  Every wait is bounded.  A row's 128 logits are read
@@ -34,7 +34,8 @@ namespace metok {
 namespace {
 
 constexpr int kM = 128, kN = 128, kThreads = 352;
-constexpr float kGrow = 16.f;                          // octaves by which a logit may pass the row's reference
+// Sum of 64 weights beyond which a row's reference grows; by how many octaves a logit has passed it then, and how far above it the new one is.
+constexpr float kMost = 1.0e18f, kGrow = 16.f, kRoom = 32.f;
 constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
 template <int DH>
@@ -92,12 +93,14 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// 2^x for x < 127 on the FMA pipe (exp2_fma_pair); arguments below -125 are held there, a NaN gives something that is no weight.
-__device__ __forceinline__ uint64_t exp2_low_pair(uint64_t x) {
+// 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 126] are held there, a NaN gives something that is no weight.
+__device__ __forceinline__ uint64_t exp2_held_pair(uint64_t x) {
     float a, b;
     sm100::unpair(x, a, b);
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(-125.f));
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(-125.f));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(126.f));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(126.f));
     return sm100::exp2_fma_core(sm100::pair(a, b));
 }
 // 16 registers of this thread's lane to 16 tensor-memory columns.
@@ -560,118 +563,126 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) continue;                     // (keeps meeting the item's other warps where they meet)
                 tc_fence_after();
-                uint32_t raw[2][32];
-                tmem_ld32_issue(t_s + half * 64, raw[0]);
-                tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
-                tmem_ld32_wait(raw[0]);
-                tmem_ld32_wait(raw[1]);
-                uint64_t v[32];                        // logits in log2 units, in pairs
+                // whether a reference is wanted: at the first keys that a row sees, and where the weights came out too large for the one there is
+                bool check = __any_sync(0xFFFFFFFFu, m == ninf && keys > k0 + half * 64), again = false;
+                uint32_t p[32];
+                float sum;
+#pragma unroll 1
+                for (;;) {
+                    const float base = m == ninf ? 0.f : m;
+                    uint32_t raw[2][32];
+                    tmem_ld32_issue(t_s + half * 64, raw[0]);
+                    tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
+                    tmem_ld32_wait(raw[0]);
+                    tmem_ld32_wait(raw[1]);
+                    uint64_t v[32];                    // logits in log2 units less the reference, in pairs
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = pair(__uint_as_float(raw[i >> 4][2 * (i & 15)]), __uint_as_float(raw[i >> 4][2 * (i & 15) + 1]));
-                if constexpr (kCap) {
-                    // y = product * scale / cap.  Up to |y| = 1 tanh(y) = y P(y^2), P the polynomial of degree 6 of least largest error (2e-8; 1e-7 in
-                    // fp32); beyond, 1 - 2 / (1 + e^2y), of which every part costs the special-function unit a step.
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        v[i] = mul_pair(v[i], pair(a.cap_scale, a.cap_scale));
-                        float y0, y1;
-                        unpair(v[i], y0, y1);
-                        most = fmaxf(most, fmaxf(fabsf(y0), fabsf(y1)));
-                    }
-                    if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
+                    for (int i = 0; i < 32; ++i) v[i] = pair(__uint_as_float(raw[i >> 4][2 * (i & 15)]), __uint_as_float(raw[i >> 4][2 * (i & 15) + 1]));
+                    const uint64_t low = pair(-base, -base);
+                    if constexpr (kCap) {
+                        // y = product * scale / cap.  Up to |y| = 1 tanh(y) = y P(y^2), P the polynomial of degree 6 of least largest error (2e-8; 1e-7 in
+                        // fp32), with the cap in its coefficients; beyond, 1 - 2 / (1 + e^2y), of which every part costs the special-function unit a step.
+                        float most = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
+                            v[i] = mul_pair(v[i], pair(a.cap_scale, a.cap_scale));
                             float y0, y1;
                             unpair(v[i], y0, y1);
-                            y0 = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y0 * (2.f * kAttnLog2e), 80.f)));
-                            y1 = a.cap_log2 - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y1 * (2.f * kAttnLog2e), 80.f)));
-                            v[i] = pair(y0, y1);
+                            most = fmaxf(most, fmaxf(fabsf(y0), fabsf(y1)));
+                        }
+                        if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                float y0, y1;
+                                unpair(v[i], y0, y1);
+                                y0 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y0 * (2.f * kAttnLog2e), 80.f)));
+                                y1 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y1 * (2.f * kAttnLog2e), 80.f)));
+                                v[i] = pair(y0, y1);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const uint64_t u = mul_pair(v[i], v[i]);
+                                uint64_t t = pair(a.cap_poly[6], a.cap_poly[6]);
+#pragma unroll
+                                for (int c = 5; c >= 0; --c) t = fma_pair(t, u, pair(a.cap_poly[c], a.cap_poly[c]));
+                                v[i] = fma_pair(v[i], t, low);
+                            }
                         }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const uint64_t u = mul_pair(v[i], v[i]);
-                            uint64_t t = fma_pair(u, pair(0.000963772187f, 0.000963772187f), pair(-0.00595128048f, -0.00595128048f));
-                            t = fma_pair(t, u, pair(0.0199732827f, 0.0199732827f));
-                            t = fma_pair(t, u, pair(-0.0532658353f, -0.0532658353f));
-                            t = fma_pair(t, u, pair(0.133195837f, 0.133195837f));
-                            t = fma_pair(t, u, pair(-0.333321293f, -0.333321293f));
-                            t = fma_pair(t, u, pair(0.999999693f, 0.999999693f));
-                            v[i] = mul_pair(mul_pair(v[i], t), pair(a.cap_log2, a.cap_log2));
+                        for (int i = 0; i < 32; ++i) v[i] = fma_pair(v[i], pair(a.scale_log2, a.scale_log2), low);
+                    }
+                    if constexpr (kBias) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const float4 at = *reinterpret_cast<const float4*>(&s_pos[x][seen & 1][half * 64 + 2 * i]);
+                            float v0, v1, v2, v3;
+                            unpair(v[i], v0, v1);
+                            unpair(v[i + 1], v2, v3);
+                            v[i] = pair(fmaf(-slope, fabsf(my_pos - at.x), v0), fmaf(-slope, fabsf(my_pos - at.y), v1));
+                            v[i + 1] = pair(fmaf(-slope, fabsf(my_pos - at.z), v2), fmaf(-slope, fabsf(my_pos - at.w), v3));
                         }
                     }
-                } else if constexpr (kBias) {
+                    if (masked) {                      // keys that the row does not see
+                        const int see = keys - k0 - half * 64;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = mul_pair(v[i], pair(a.scale_log2, a.scale_log2));
-                }
-                if constexpr (kBias) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float4 p = *reinterpret_cast<const float4*>(&s_pos[x][seen & 1][half * 64 + 2 * i]);
-                        float v0, v1, v2, v3;
-                        unpair(v[i], v0, v1);
-                        unpair(v[i + 1], v2, v3);
-                        v[i] = pair(fmaf(-slope, fabsf(my_pos - p.x), v0), fmaf(-slope, fabsf(my_pos - p.y), v1));
-                        v[i + 1] = pair(fmaf(-slope, fabsf(my_pos - p.z), v2), fmaf(-slope, fabsf(my_pos - p.w), v3));
+                        for (int i = 0; i < 32; ++i) {
+                            float v0, v1;
+                            unpair(v[i], v0, v1);
+                            v[i] = pair(2 * i < see ? v0 : ninf, 2 * i + 1 < see ? v1 : ninf);
+                        }
                     }
-                }
-                if (masked) {                          // keys that the row does not see
-                    const int see = keys - k0 - half * 64;
+                    if (check) {
+                        float top[4] = {ninf, ninf, ninf, ninf};
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float v0, v1;
+                            unpair(v[i], v0, v1);
+                            top[i & 3] = fmaxf(top[i & 3], fmaxf(v0, v1));
+                        }
+                        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) + base;
+                        const bool grow = keys > 0 && (again ? mx > m + kGrow : m == ninf && mx > ninf);
+                        const float to = again ? mx + kRoom : mx, f = grow ? fast_exp2(m - to) : 1.f;
+                        if (grow) m = to;
+                        l *= f;
+                        const uint64_t less = grow ? pair(base - to, base - to) : 0ull;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = add_pair(v[i], less);
+                        if (j > 0 || half) {           // when the product before this one on O_x is complete
+                            if (!mbar_wait(smem_u32(&h_bar[x]), (uint32_t)(half ^ 1), abort_flag)) ok = false;
+                            ok = __all_sync(0xFFFFFFFFu, ok);
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < DH / 16; ++c) {
+                                float o[16];
+                                tmem_ld16(t_o + c * 16, o);
+                                uint32_t w[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+                                tmem_st16(t_o + c * 16, w);
+                            }
+                        }
+                    }
+                    uint64_t sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        float v0, v1;
-                        unpair(v[i], v0, v1);
-                        v[i] = pair(2 * i < see ? v0 : ninf, 2 * i + 1 < see ? v1 : ninf);
+                        // some on the FMA pipe, so that both work.  (There a hidden key's weight is 2^-125, not 0: nothing beside any weight that counts,
+                        // and a row that sees no key is known by its m.)
+                        const uint64_t w = kShare(i) ? exp2_held_pair(v[i]) : exp2_pair(v[i]);
+                        if (i & 1) sum1 = add_pair(sum1, w);
+                        else sum0 = add_pair(sum0, w);
+                        float w0, w1;
+                        unpair(w, w0, w1);
+                        p[i] = pack_bf16(w0, w1);
                     }
+                    float s0, s1;
+                    unpair(add_pair(sum0, sum1), s0, s1);
+                    sum = s0 + s1;
+                    if (again || !__any_sync(0xFFFFFFFFu, keys > 0 && !(sum < kMost))) break;      // (a tile's unused rows may hold anything)
+                    check = again = true;              // once
                 }
-                const float sc = kCap || kBias ? 1.f : a.scale_log2;    // still to be multiplied in
-                float top[4] = {ninf, ninf, ninf, ninf};
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float v0, v1;
-                    unpair(v[i], v0, v1);
-                    top[i & 3] = fmaxf(top[i & 3], fmaxf(v0, v1));
-                }
-                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
-                const bool grow = mx > m + kGrow;      // (also where there is none yet)
-                if (__any_sync(0xFFFFFFFFu, grow)) {
-                    const float f = grow ? fast_exp2(m - mx) : 1.f;
-                    if (grow) m = mx;
-                    l *= f;
-                    if (j > 0 || half) {               // when the product before this one on O_x is complete
-                        if (!mbar_wait(smem_u32(&h_bar[x]), (uint32_t)(half ^ 1), abort_flag)) ok = false;
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < DH / 16; ++c) {
-                            float o[16];
-                            tmem_ld16(t_o + c * 16, o);
-                            uint32_t w[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
-                            tmem_st16(t_o + c * 16, w);
-                        }
-                    }
-                }
-                const float base = m == ninf ? 0.f : m;
-                uint64_t sum0 = 0ull, sum1 = 0ull;
-                uint32_t p[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const uint64_t y = kCap || kBias ? add_pair(v[i], pair(-base, -base)) : fma_pair(v[i], pair(sc, sc), pair(-base, -base));
-                    // some on the FMA pipe, so that both work; y is at most kGrow.  (There a hidden key's weight is 2^-125, not 0: nothing beside any weight
-                    // that counts, and a row that sees no key is known by its m.)
-                    const uint64_t w = kShare(i) ? exp2_low_pair(y) : exp2_pair(y);
-                    if (i & 1) sum1 = add_pair(sum1, w);
-                    else sum0 = add_pair(sum0, w);
-                    float w0, w1;
-                    unpair(w, w0, w1);
-                    p[i] = pack_bf16(w0, w1);
-                }
-                float s0, s1;
-                unpair(add_pair(sum0, sum1), s0, s1);
-                l += s0 + s1;
+                l += sum;
                 tmem_st32(t_s + half * 64, p);         // their product may begin
                 tmem_st_wait();
                 tc_fence_before();
@@ -869,6 +880,9 @@ int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st) {
     MmaMaps maps = {};
     a.heads_item = std::min(a.G, kM);
     a.rows_item = kM / a.heads_item;
+    // tanh(y) / y in powers of y^2, |y| <= 1: least largest error of y times it
+    constexpr double kTanh[7] = {0.999999693, -0.333321293, 0.133195837, -0.0532658353, 0.0199732827, -0.00595128048, 0.000963772187};
+    for (int c = 0; c < 7; ++c) a.cap_poly[c] = (float)(kTanh[c] * a.cap_log2);
     a.rows_magic = a.rows_item > 1 ? (uint32_t)((0x100000000ULL + a.rows_item - 1) / a.rows_item) : 0u;
     a.head_chunks = ceil_div(a.G, a.heads_item);
     maps.k_step = a.Hkv > 1 && a.k_head > 0;
