@@ -795,8 +795,8 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
 }
 
 // Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut.  A lane per row, a warp for DH / 8 columns of 32 rows,
-// two parts on their way.
-constexpr int kCutBlocks = 2 * kM / 32;
+// kAhead parts on their way.
+constexpr int kCutBlocks = 2 * kM / 32, kAhead = 2;
 template <int DH>
 __global__ void __launch_bounds__(256)
 prompt_cut_join_kernel(const PromptArgs a) {
@@ -815,11 +815,11 @@ prompt_cut_join_kernel(const PromptArgs a) {
     float4 acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = 0; p0 < parts; p0 += 2) {
-        float2 ml[2];
-        float4 o[2][E];
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        float2 ml[kAhead];
+        float4 o[kAhead][E];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             const bool in = p0 + u < parts;
             ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + (slot(p0 + u) * (2 * kM) + rr) * 2) : make_float2(ninf, 0.f);
 #pragma unroll
@@ -827,7 +827,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
                 o[u][e] = in ? reinterpret_cast<const float4*>(a.part_o)[(slot(p0 + u) * (DH / 4) + warp * E + e) * (2 * kM) + rr] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             if (!(ml[u].y > 0.f)) continue;            // a part of no keys has written no output
             const float top = fmaxf(M, ml[u].x), f = sm100::fast_exp2(M - top), g = sm100::fast_exp2(ml[u].x - top);
             M = top;
@@ -855,11 +855,11 @@ int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
         launch_chained(kern, dim3(kNumSMs), dim3(kThreads), MmaShape<DH>::kSmem, st, a, maps);
     }
     METOK_LAUNCH_CHECK();
-    {
+    if (a.n_k > kN) {                                  // (pairs of one step are never cut)
         METOK_TIMED("prompt_cut_join", st);
         launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks), dim3(256), 0, st, a);
+        METOK_LAUNCH_CHECK();
     }
-    METOK_LAUNCH_CHECK();
     return METOK_OK;
 }
 template <int DH>
