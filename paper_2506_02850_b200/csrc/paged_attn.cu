@@ -795,6 +795,7 @@ paged_join_kernel(const PagedAttnArgs a) {
     long long* s_first = reinterpret_cast<long long*>(s_dyn);            // [subs]
     int* s_n = reinterpret_cast<int*>(s_first + subs);                   // [subs]
     float* s_lse = reinterpret_cast<float*>(s_n + subs);                 // [Hq]: log2 of the sum
+    long long* s_off = reinterpret_cast<long long*>(s_dyn + ((size_t)subs * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8);   // [Hq]: the head's logits of the sequence
     for (int sub = tid; sub < subs; sub += kJoinThreads) {
         const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
         s_first[sub] = sl.first;
@@ -824,24 +825,24 @@ paged_join_kernel(const PagedAttnArgs a) {
             L = L * sm100::fast_exp2(M - top) + l2 * sm100::fast_exp2(m2 - top);
             M = top;
         }
-        if (h < a.Hq && part == 0) s_lse[h] = M + log2f(L);
+        if (h < a.Hq && part == 0) {
+            const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads;
+            s_lse[h] = M + log2f(L);
+            s_off[h] = ((long long)(hk * a.NC + ch) * nt * a.heads + (g - ch * a.heads)) << a.tile_shift;
+        }
     }
     __syncthreads();
     const int row = row0 + tid;
     if (row >= len) return;
     const int tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
-    const float* x0 = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
+    const float* x = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
     float sum = 0.f;
-    for (int sub = 0; sub < subs; ++sub) {
-        const int hk = sub / a.NC, ch = sub - hk * a.NC, h0 = hk * a.G + ch * a.heads, nh = min(a.heads, a.G - ch * a.heads);
-        const float* x = x0 + (size_t)sub * nt * a.heads * rows_tile;
-        for (int g0 = 0; g0 < nh; g0 += 8) {           // eight loads on their way (a loop of nh of them would wait for each)
-            float v[8];
+    for (int h = 0; h < a.Hq; h += 8) {                // eight loads on their way (a loop of single ones would wait for each)
+        float v[8];
 #pragma unroll
-            for (int g = 0; g < 8; ++g) v[g] = g0 + g < nh ? x[(g0 + g) * rows_tile] : kLow;
+        for (int u = 0; u < 8; ++u) v[u] = h + u < a.Hq ? x[s_off[h + u]] : kLow;
 #pragma unroll
-            for (int g = 0; g < 8; ++g) sum += g0 + g < nh ? sm100::fast_exp2(v[g] - s_lse[h0 + g0 + g]) : 0.f;
-        }
+        for (int u = 0; u < 8; ++u) sum += h + u < a.Hq ? sm100::fast_exp2(v[u] - s_lse[h + u]) : 0.f;
     }
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
 }
@@ -885,7 +886,7 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
     {
         METOK_TIMED("paged_join", st);
         const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), a.mass ? (size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 : 0, st, a);
+        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;

@@ -1,9 +1,10 @@
 // metok_prefill_attention: the C entry, the fp32 kernel, and the join of split keys.  (bf16: prefill_attn_mma.cu.)
 //
-// fp32, on the CUDA cores: a CTA of 256 threads takes 16 R query rows of a head and walks their keys in tiles of 64, of which the next
-// one is on its way while one is worked on.  Thread (ty, tx) holds the logits of rows R ty + i and keys tx + 16 j, and the outputs of the
-// same rows; a row's running maximum and sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with
-// n not falling from row to row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
+// fp32, on the CUDA cores: a CTA of 256 threads takes a tile of 16 R query rows (consecutive rows of a document, each with all query heads
+// of one K/V head, so that few rows fill a tile too) and walks their keys in tiles of 64, of which the next one is on its way while
+// one is worked on.  Thread (ty, tx) holds the logits of rows R ty + i and keys tx + 16 j, and the outputs of the same rows; a row's
+// running maximum and sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling
+// from row to row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
 // R = 4 feeds the multiply-adds (two of them per shared-memory wavefront); R = 1 is for calls that leave most SMs without a tile, where a
 // tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4.
 #include <algorithm>
@@ -31,13 +32,16 @@ prompt_attn_simt_kernel(const PromptArgs a) {
     grid_dep_wait();
     extern __shared__ __align__(16) uint8_t smem_raw[];
     SimtAttnSmem<DH, R>& sm = *reinterpret_cast<SimtAttnSmem<DH, R>*>(smem_raw);
-    const int h = blockIdx.x % a.Hq, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-    const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hq, [](int Lq) { return (Lq + kSM - 1) / kSM; });
+    const int g = blockIdx.x % a.Hkv, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const PromptDoc d = prompt_tile(a, blockIdx.x / a.Hkv, [&](int Lq) { return (Lq + a.rows_item - 1) / a.rows_item * a.head_chunks; });
     if (d.tile < 0) return;
-    const int i0 = d.tile * kSM, rows = min(kSM, d.Lq - i0), g = h / a.G;
-    const int first_keys = prompt_keys(a, d, i0), all_keys = prompt_keys(a, d, i0 + rows - 1);
+    const int blk = d.tile / a.head_chunks, h0 = (d.tile - blk * a.head_chunks) * a.heads_item, i0 = blk * a.rows_item;
+    const int nr = min(a.rows_item, d.Lq - i0), heads = min(a.heads_item, a.G - h0);
+    const int first_keys = prompt_keys(a, d, i0), all_keys = prompt_keys(a, d, i0 + nr - 1);
     const int nt = (all_keys + kSN - 1) / kSN, t_lo = (int)((long long)nt * blockIdx.y / a.splits), t_hi = (int)((long long)nt * (blockIdx.y + 1) / a.splits);
-    const float* q = reinterpret_cast<const float*>(a.q) + h * a.q_head + (long long)(d.q0 + i0) * a.q_row;
+    // row r of the tile: document row i0 + r / heads_item, head h0 + r % heads_item of the K/V head's; -1 if it is none
+    auto row_of = [&](int r) { const int i = r / a.heads_item; return i < nr && r - i * a.heads_item < heads ? i0 + i : -1; };
+    auto head_of = [&](int r) { return g * a.G + h0 + r % a.heads_item; };
     const float* k = reinterpret_cast<const float*>(a.k) + g * a.k_head + (long long)d.k0 * a.k_row;
     const float* v = reinterpret_cast<const float*>(a.v) + g * a.v_head + (long long)d.k0 * a.v_row;
     constexpr int CPR = DH / 4;                        // 16-byte pieces of a row
@@ -57,18 +61,19 @@ prompt_attn_simt_kernel(const PromptArgs a) {
     for (int c = tid; c < kSM * CPR; c += kSThreads) {
         const int r = c / CPR, e = (c - r * CPR) * 4;
         float x[4];
-        if (r < rows) Vec16<float>::load(q + (long long)r * a.q_row + e, x);
+        const int i = row_of(r);
+        if (i >= 0) Vec16<float>::load(reinterpret_cast<const float*>(a.q) + head_of(r) * a.q_head + (long long)(d.q0 + i) * a.q_row + e, x);
         else Vec16<float>::zero(x);
         *reinterpret_cast<float4*>(&sm.q[r][e]) = make_float4(x[0], x[1], x[2], x[3]);
     }
     int keys[R];
-    float my_pos[R], m[R], l[R], o[R][DH / 16];
-    const float slope = a.slopes ? a.slopes[h] * kAttnLog2e : 0.f;
+    float my_pos[R], slope[R], m[R], l[R], o[R][DH / 16];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        const int r = i0 + ty * R + i;
-        keys[i] = ty * R + i < rows ? prompt_keys(a, d, r) : 0;
-        my_pos[i] = a.slopes ? prompt_position(a, d.k0, d.Lk, d.Lk - d.Lq + r) : 0.f;
+        const int r = ty * R + i, row = row_of(r);
+        keys[i] = row >= 0 ? prompt_keys(a, d, row) : 0;
+        my_pos[i] = a.slopes ? prompt_position(a, d.k0, d.Lk, d.Lk - d.Lq + row) : 0.f;
+        slope[i] = a.slopes && row >= 0 ? a.slopes[head_of(r)] * kAttnLog2e : 0.f;
         m[i] = __int_as_float(0xFF800000);
         l[i] = 0.f;
 #pragma unroll
@@ -102,14 +107,14 @@ prompt_attn_simt_kernel(const PromptArgs a) {
                 for (int j = 0; j < 4; ++j)
                     s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
         }
-        const bool masked = j0 + kSN > first_keys || rows < kSM;
+        const bool masked = j0 + kSN > first_keys;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             float top = m[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float x = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(s[i][j] * a.cap_scale) : s[i][j] * a.scale_log2;
-                if (a.slopes) x = fmaf(-slope, fabsf(my_pos[i] - sm.pos[b][tx + 16 * j]), x);
+                if (a.slopes) x = fmaf(-slope[i], fabsf(my_pos[i] - sm.pos[b][tx + 16 * j]), x);
                 if (masked && j0 + tx + 16 * j >= keys[i]) x = __int_as_float(0xFF800000);
                 s[i][j] = x;
                 top = fmaxf(top, x);
@@ -156,9 +161,10 @@ prompt_attn_simt_kernel(const PromptArgs a) {
     for (int i = 0; i < R; ++i) {
 #pragma unroll
         for (int w = 8; w >= 1; w >>= 1) l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], w);
-        const int r = ty * R + i;
-        if (r >= rows) continue;
-        const long long row = d.q0 + i0 + r;
+        const int r = ty * R + i, in_doc = row_of(r);
+        if (in_doc < 0) continue;
+        const int h = head_of(r);
+        const long long row = d.q0 + in_doc;
         const bool part = a.splits > 1;
         const float inv = part ? 1.f : l[i] > 0.f ? 1.f / l[i] : 0.f;
         const long long at = ((long long)blockIdx.y * a.Hq + h) * a.n_q + row;
@@ -208,20 +214,27 @@ prompt_join_kernel(const PromptArgs a) {
     if (lane == 0 && a.lse) a.lse[(long long)h * a.n_q + row] = kAttnLn2 * (M + log2f(L));
 }
 
-// fp32: query rows of a tile, CTAs without splits, and splits of the keys.
+// fp32: rows of a tile, how heads and rows make one, CTAs without splits, and splits of the keys.
 struct PromptPlan {
-    int rows;
+    int rows, heads_item, head_chunks, rows_item;
     long long ctas;
     int splits;
 };
-// Tiles of all documents: at most a started one more per document than whole ones fit into n_q.
 PromptPlan prompt_plan(const metok_attention_params* p) {
     PromptPlan pl;
-    auto ctas = [&](int rows) { return std::max(1LL, p->n_seq == 1 ? (long long)ceil_div(p->n_q, rows) : (long long)p->n_q / rows + std::min(p->n_seq, p->n_q)) * p->Hq; };
-    pl.rows = ctas(64) < kNumSMs ? 16 : 64;
-    pl.ctas = ctas(pl.rows);
-    // few rows: the keys are cut until every SM has work, no part shorter than four tiles
-    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (4 * kSN), kNumSMs / pl.ctas, 64LL}));
+    const int G = p->Hq / p->Hkv;
+    for (int rows : {64, 16}) {
+        pl.rows = rows;
+        pl.heads_item = std::min(G, rows);
+        pl.head_chunks = ceil_div(G, pl.heads_item);
+        pl.rows_item = rows / pl.heads_item;
+        // several documents: at most a started tile more each than whole ones fit into n_q
+        const long long tiles = p->n_seq == 1 ? ceil_div(p->n_q, pl.rows_item) : (long long)p->n_q / pl.rows_item + std::min(p->n_seq, p->n_q);
+        pl.ctas = std::max(1LL, tiles * pl.head_chunks) * p->Hkv;
+        if (pl.ctas >= kNumSMs) break;
+    }
+    // few rows: the keys are cut until every SM has work, no part shorter than two tiles
+    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (2 * kSN), kNumSMs / pl.ctas, 64LL}));
     return pl;
 }
 void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, PromptArgs* a) {
@@ -307,6 +320,7 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     if (dtype == METOK_BF16) return launch_prompt_attn_mma(a, p->dh, st);
     const PromptPlan pl = prompt_plan(p);
     a.splits = pl.splits;
+    a.heads_item = pl.heads_item; a.head_chunks = pl.head_chunks; a.rows_item = pl.rows_item;
     if (pl.rows == 16) return p->dh == 64 ? launch_prompt_simt<64, 1>(a, pl, st) : launch_prompt_simt<128, 1>(a, pl, st);
     return p->dh == 64 ? launch_prompt_simt<64, 4>(a, pl, st) : launch_prompt_simt<128, 4>(a, pl, st);
 }

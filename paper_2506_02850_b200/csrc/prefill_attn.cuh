@@ -19,8 +19,8 @@ struct PromptArgs {
     float cap_poly[7];                         // bf16: cap_log2 * tanh(y) / y in powers of y^2, y = dot * cap_scale
     int causal;
     int splits;                                // fp32: parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
-    int heads_item, head_chunks, rows_item;    // bf16: query heads of a tile of 128 rows, such tiles for all heads of a K/V head, document rows of a tile
-    uint32_t rows_magic;                       // ceil(2^32 / rows_item)
+    int heads_item, head_chunks, rows_item;    // query heads of a tile of rows, such tiles for all heads of a K/V head, document rows of a tile
+    uint32_t rows_magic;                       // bf16: ceil(2^32 / rows_item)
     float *part_o, *part_ml;                   // unnormalised outputs and (maximum, sum) of the parts; fp32: [splits][Hq][n_q]
     void* cuts;                                // bf16: what the second kernel joins
     int32_t* status;
