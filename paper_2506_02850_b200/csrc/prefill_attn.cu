@@ -5,8 +5,8 @@
 // one is worked on.  Thread (ty, tx) holds the logits of rows R ty + i and keys tx + 16 j, and the outputs of the same rows; a row's
 // running maximum and sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling
 // from row to row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
-// R = 4 feeds the multiply-adds (two of them per shared-memory wavefront); R = 1 is for calls that leave most SMs without a tile, where a
-// tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4.
+// R = 4 feeds the multiply-adds best (five of them per shared-memory wavefront, 1.8 with R = 1); R = 2 and 1 are for calls of few rows, and
+// those that leave most SMs without a tile, where a tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4, 12 with 1.
 #include <algorithm>
 
 #include "launchers.h"
@@ -223,7 +223,7 @@ struct PromptPlan {
 PromptPlan prompt_plan(const metok_attention_params* p) {
     PromptPlan pl;
     const int G = p->Hq / p->Hkv;
-    for (int rows : {64, 16}) {
+    for (int rows : {64, 32, 16}) {
         pl.rows = rows;
         pl.heads_item = std::min(G, rows);
         pl.head_chunks = ceil_div(G, pl.heads_item);
@@ -231,10 +231,12 @@ PromptPlan prompt_plan(const metok_attention_params* p) {
         // several documents: at most a started tile more each than whole ones fit into n_q
         const long long tiles = p->n_seq == 1 ? ceil_div(p->n_q, pl.rows_item) : (long long)p->n_q / pl.rows_item + std::min(p->n_seq, p->n_q);
         pl.ctas = std::max(1LL, tiles * pl.head_chunks) * p->Hkv;
-        if (pl.ctas >= kNumSMs) break;
+        // few rows: the keys are cut until every SM has work (documents of different lengths: several parts), no part shorter than two tiles
+        const long long most = std::max(1LL, std::min((long long)p->n_k / (2 * kSN), 64LL));
+        pl.splits = (int)std::max(1LL, std::min(most, (p->n_seq == 1 ? kNumSMs : 4 * kNumSMs) / pl.ctas));
+        // the largest tile that the average document fills by three quarters and that leaves a CTA for every SM
+        if (pl.ctas * most >= kNumSMs && 4LL * p->n_q * pl.heads_item >= 3LL * rows * p->n_seq) break;
     }
-    // few rows: the keys are cut until every SM has work, no part shorter than two tiles
-    pl.splits = (int)std::max(1LL, std::min({(long long)p->n_k / (2 * kSN), kNumSMs / pl.ctas, 64LL}));
     return pl;
 }
 void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, PromptArgs* a) {
@@ -321,6 +323,7 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     const PromptPlan pl = prompt_plan(p);
     a.splits = pl.splits;
     a.heads_item = pl.heads_item; a.head_chunks = pl.head_chunks; a.rows_item = pl.rows_item;
+    if (pl.rows == 32) return p->dh == 64 ? launch_prompt_simt<64, 2>(a, pl, st) : launch_prompt_simt<128, 2>(a, pl, st);
     if (pl.rows == 16) return p->dh == 64 ? launch_prompt_simt<64, 1>(a, pl, st) : launch_prompt_simt<128, 1>(a, pl, st);
     return p->dh == 64 ? launch_prompt_simt<64, 4>(a, pl, st) : launch_prompt_simt<128, 4>(a, pl, st);
 }
