@@ -615,7 +615,7 @@ METOK_API int metok_profile_end(char* out, size_t cap);
  * so that the waiting side runs into its limit, the CTA unwinds (copies drained, tensor memory
  * freed) and the call's status word -- int32 word 0 of the workspace -- reads METOK_ERR_TIMEOUT.
  * mask bits: 1 merge-assign, 2 attention statistics, 4 attention column sums, 8 averaging,
- * 16 hidden-row gather; 0 switches it off.  metok_debug_build() returns 1 | 2 for such a build and
+ * 16 hidden-row gather, 32 attention over a paged cache, 64 attention of a prompt's rows (bf16); 0 switches it off.  metok_debug_build() returns 1 | 2 for such a build and
  * 0 for the normal library, in which metok_debug_set returns METOK_ERR_UNSUPPORTED and does
  * nothing.  The paper has no counterpart of these two calls. */
 #define METOK_DEBUG_WITHHOLD_COPY 1

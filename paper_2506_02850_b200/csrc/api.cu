@@ -195,6 +195,13 @@ namespace metok {
 #if defined(METOK_DEBUG_SHORT_WAIT) || defined(METOK_DEBUG_BOUNDS)
 static int g_dbg_withhold = 0;
 #endif
+int debug_withheld() {
+#if defined(METOK_DEBUG_SHORT_WAIT) || defined(METOK_DEBUG_BOUNDS)
+    return g_dbg_withhold;
+#else
+    return 0;
+#endif
+}
 int debug_arm(int32_t* status, cudaStream_t st) {
 #if defined(METOK_DEBUG_SHORT_WAIT) || defined(METOK_DEBUG_BOUNDS)
     const int32_t words[2] = {g_dbg_withhold, 0};

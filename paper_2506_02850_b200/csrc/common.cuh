@@ -105,14 +105,24 @@ __device__ __forceinline__ void grid_dep_wait() {
 // Words 1 and 2 of the status area (the 64 int32 at the start of a workspace) belong to these builds:
 // word 1 = the copies to withhold (bit mask, written by the host when the call is made), word 2 = the
 // number of out-of-range indices met.
-enum { kDbgMergeAssign = 1, kDbgAttnStats = 2, kDbgAttnColsum = 4, kDbgMergeAvg = 8, kDbgGatherRows = 16 };
+enum { kDbgMergeAssign = 1, kDbgAttnStats = 2, kDbgAttnColsum = 4, kDbgMergeAvg = 8, kDbgGatherRows = 16,
+       kDbgPagedAttn = 32, kDbgPromptAttn = 64 };
 int debug_arm(int32_t* status, cudaStream_t st);          // debug builds: writes words 1 and 2; else does nothing
+int debug_withheld();                                     // the mask, for kernels that get it as an argument (0 in other builds)
 #ifdef __CUDACC__
 __device__ __forceinline__ bool dbg_withhold(const int32_t* status, int bit) {
 #ifdef METOK_DEBUG_SHORT_WAIT
     return (status[1] & bit) != 0;
 #else
     (void)status; (void)bit;
+    return false;
+#endif
+}
+__device__ __forceinline__ bool dbg_held(int mask, int bit) {
+#ifdef METOK_DEBUG_SHORT_WAIT
+    return (mask & bit) != 0;
+#else
+    (void)mask; (void)bit;
     return false;
 #endif
 }

@@ -121,8 +121,9 @@ struct EvictArgs {
 };
 
 // Whether a sequence may be touched: its length and pages are in range, no page is its own twice or another's.  A bit per page in
-// shared memory marks the sequence's own; then every other sequence's pages are looked up.
-constexpr int kEvictBitPages = 1 << 18;                // pages up to which that is done (32 KB); above, a kernel before it claims the pages
+// shared memory marks the sequence's own; then every other sequence's pages are looked up.  Beyond so many pages (32 KB of bits) or
+// sequences a kernel before it claims the pages (6 us with its clearing; this costs next to nothing for few).
+constexpr int kEvictBitPages = 1 << 18, kEvictBitSeqs = 256;
 __device__ __forceinline__ bool evict_sound(const EvictArgs& a, int b, uint32_t* s_bits) {
     const int tid = threadIdx.x, nthr = blockDim.x, len = a.kv_len[b], page_rows = 1 << a.d.page_shift;
     if (len < 0 || len > a.d.S_cap()) return false;    // uniform
@@ -447,7 +448,7 @@ extern "C" int metok_paged_evict(int dtype, const metok_paged_cache* c, void* co
     Carver cv(ws);
     evict_carve(cv, d, L, budget, &a);
     cudaStream_t st = (cudaStream_t)stream;
-    a.claimed = d.n_pages > kEvictBitPages;
+    a.claimed = d.n_pages > kEvictBitPages || d.n_seqs > kEvictBitSeqs;
     a.keys_fit = d.S_cap() <= kEvictKeys;
     if (a.claimed) {
         METOK_CUDA_TRY(cudaMemsetAsync(a.claim, 0, ((size_t)d.n_pages + d.n_seqs) * sizeof(int32_t), st));

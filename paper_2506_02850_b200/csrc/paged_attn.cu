@@ -41,7 +41,9 @@ struct PagedAttnArgs {
     float* mass;
     void* out;
     float *lse, *part_o, *part_ml, *logits;
+    long long* line;                                   // [n_seqs + 1]: tiles of the sequences before each, per unit; then of all
     int32_t* status;
+    int withhold;                                      // debug builds: the copies to leave out
 };
 
 // Tiles of sequence b's one unit (0 for a length out of range, which the second kernel reports).
@@ -50,36 +52,39 @@ __device__ __forceinline__ int unit_tiles(const PagedAttnArgs& a, int b) {
     return len > 0 && len <= a.d.S_cap() ? (len + (1 << a.tile_shift) - 1) >> a.tile_shift : 0;
 }
 
-// Tiles of the sequences before sequence b, per unit of a sequence, and of all; whole CTA.  Up to 32 sequences every warp finds
-// out by itself: no barrier.
-struct LineSums { long long before, all; };
-__device__ __forceinline__ LineSums line_sums(const PagedAttnArgs& a, int b, long long* s_sum) {
+// Tiles of all sequences, per unit; whole CTA.  Up to 32 sequences every warp finds out by itself: no barrier.
+__device__ __forceinline__ long long line_tiles(const PagedAttnArgs& a, long long* s_sum) {
     if (a.d.n_seqs <= 32) {
-        const int lane = threadIdx.x & 31, t = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
-        return {(long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? t : 0), (long long)__reduce_add_sync(0xFFFFFFFFu, t)};
+        const int lane = threadIdx.x & 31;
+        return (long long)__reduce_add_sync(0xFFFFFFFFu, lane < a.d.n_seqs ? unit_tiles(a, lane) : 0);
     }
-    long long before = 0, all = 0;
-    for (int i = threadIdx.x; i < a.d.n_seqs; i += blockDim.x) {
-        const int t = unit_tiles(a, i);
-        all += t;
-        if (i < b) before += t;
-    }
+    long long all = 0;
+    for (int i = threadIdx.x; i < a.d.n_seqs; i += blockDim.x) all += unit_tiles(a, i);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
-        all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        s_sum[2 * (threadIdx.x >> 5)] = before;
-        s_sum[2 * (threadIdx.x >> 5) + 1] = all;
-    }
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = all;
     __syncthreads();
-    LineSums r = {0, 0};
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
-        r.before += s_sum[2 * w];
-        r.all += s_sum[2 * w + 1];
+    all = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) all += s_sum[w];
+    return all;
+}
+
+// The line for the second kernel: one warp, 32 sequences at a time.
+__device__ __forceinline__ void write_line(const PagedAttnArgs& a) {
+    const int lane = threadIdx.x & 31;
+    long long before = 0;
+    for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
+        const int b = b0 + lane, mine = b < a.d.n_seqs ? unit_tiles(a, b) : 0;
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (b < a.d.n_seqs) a.line[b] = before + incl - mine;
+        before += __shfl_sync(0xFFFFFFFFu, incl, 31);
     }
-    return r;
+    if (lane == 0) a.line[a.d.n_seqs] = before;
 }
 
 // CTAs that have tiles: each of them at least one.
@@ -502,21 +507,24 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages];
     __shared__ __align__(16) float s_o[2][kUnitHeads * DH];
     __shared__ float s_ml[2][kUnitHeads * 2];
-    __shared__ long long s_sum[2 * (kWarps + 1)];
+    __shared__ long long s_sum[kWarps + 1];
     __shared__ long long s_start;
     __shared__ int s_b;
     __shared__ int s_abort;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     const int subs = a.d.Hkv * a.NC;
+    if (blockIdx.x == a.grid) {                        // one CTA more than pieces
+        if (warp == 0) write_line(a);
+        return;
+    }
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0) *a.status = METOK_OK;     // a wait that gives up writes it, seconds later
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), kWarps); }
         s_abort = 0;
         mbar_fence_init();
     }
-    const LineSums sums = line_sums(a, 0, s_sum);
-    const long long T_all = sums.all * subs, ctas = busy_ctas(a, T_all);
+    const long long T_all = line_tiles(a, s_sum) * subs, ctas = busy_ctas(a, T_all);
     if (blockIdx.x >= ctas) return;                    // uniform
     const long long t_lo = T_all * blockIdx.x / ctas, t_hi = T_all * (blockIdx.x + 1) / ctas;
     // the sequence that holds tile t_lo, 32 at a time: by every warp for itself where there are no more
@@ -575,6 +583,7 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
             for (int c = lane; c < per_tile * 2 * S::KB; c += 32) {
                 const int pc = c / (2 * S::KB), e = c - pc * (2 * S::KB), kb = e >> 1;
                 if (pc >= pieces) continue;
+                if (dbg_held(a.withhold, kDbgPagedAttn) && blockIdx.x == 0 && it == 0 && c == 0) continue;   // debug builds: one copy never sent
                 const int row = r0 + pc * piece;
                 int page = a.block_table[(size_t)p.b * a.d.max_pages + (row >> a.d.page_shift)];
                 if (page < 0 || page >= a.d.n_pages) page = 0;          // the second kernel drops the sequence
@@ -697,7 +706,6 @@ template <typename T, int DH>
 __global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const PagedAttnArgs a) {
     grid_dep_wait();
-    __shared__ long long s_sum[2 * (kJoinThreads / 32)];
     __shared__ __align__(16) float s_acc[kJoinThreads][4];
     __shared__ float s_l[kJoinThreads];
     __shared__ float s_w[kJoinThreads / 32];
@@ -725,8 +733,7 @@ paged_join_kernel(const PagedAttnArgs a) {
         if (tid == 0) *a.status = METOK_ERR_INVALID_ARG;
         return;
     }
-    const LineSums sums = line_sums(a, b, s_sum);
-    const long long all = sums.all * subs, base = sums.before * subs;
+    const long long all = a.line[a.d.n_seqs] * subs, base = a.line[b] * subs;
     const int nt = unit_tiles(a, b);
 
     if (!weights) {
@@ -870,6 +877,7 @@ PagedPlan paged_plan(int dtype, const PagedDims& d, int Hq) {
 void paged_carve(Carver& cv, const PagedPlan& p, const PagedDims& d, bool mass, PagedAttnArgs* a) {
     a->part_o = cv.take<float>(p.slots * p.heads * d.dh);
     a->part_ml = cv.take<float>(p.slots * p.heads * 2);
+    a->line = cv.take<long long>((size_t)d.n_seqs + 1);
     a->logits = mass ? cv.take<float>(p.tiles * p.heads << p.tile_shift) : nullptr;
 }
 
@@ -880,7 +888,7 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
     METOK_ALLOW_SMEM(kern, S::kRing);
     {
         METOK_TIMED("paged_attn", st);
-        launch_chained(kern, dim3(a.grid), dim3(kThreads), S::kRing, st, a, tk, tv);
+        launch_chained(kern, dim3(a.grid + 1), dim3(kThreads), S::kRing, st, a, tk, tv);
     }
     METOK_LAUNCH_CHECK();
     {
@@ -948,6 +956,7 @@ extern "C" int metok_paged_attention(int dtype, const metok_paged_cache* c, cons
     a.cap_scale = softcap > 0.f ? softmax_scale / softcap : 0.f;
     a.cap_log2 = softcap * kLog2e;
     a.mass = mass; a.lse = lse; a.status = status;
+    a.withhold = debug_withheld();
     Carver cv(ws);
     paged_carve(cv, p, d, mass != nullptr, &a);
     const uint64_t rows = (uint64_t)d.n_pages * d.Hkv << d.page_shift;

@@ -240,7 +240,7 @@ PromptPlan prompt_plan(const metok_attention_params* p) {
     return pl;
 }
 void prompt_carve(Carver& cv, int dtype, const metok_attention_params* p, PromptArgs* a) {
-    if (dtype == METOK_BF16) return prompt_mma_carve(cv, p->dh, a);
+    if (dtype == METOK_BF16) return prompt_mma_carve(cv, p, a);
     const int splits = prompt_plan(p).splits;
     if (splits == 1) return;
     const size_t rows = (size_t)splits * p->Hq * p->n_q;
@@ -272,6 +272,9 @@ int prompt_check(int dtype, const metok_attention_params* p) {
     if (p->dh != 64 && p->dh != 128) return METOK_ERR_UNSUPPORTED;
     if (p->n_q > (1 << 24) || p->n_k > (1 << 24) || p->n_seq > kPromptDocs || p->Hq > 65535) return METOK_ERR_UNSUPPORTED;
     if (dtype == METOK_F32 && prompt_plan(p).ctas > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    // (bf16: items of a K/V head)
+    const int G = p->Hq / p->Hkv;
+    if (((long long)p->n_q + p->n_seq) * ceil_div(G, 128) > (1LL << 30)) return METOK_ERR_UNSUPPORTED;
     return METOK_OK;
 }
 
@@ -316,6 +319,7 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     a.cap_log2 = p->softcap * kAttnLog2e;
     a.causal = p->causal != 0;
     a.status = status;
+    a.withhold = debug_withheld();
     Carver cv(ws);
     prompt_carve(cv, dtype, p, &a);
     cudaStream_t st = (cudaStream_t)stream;

@@ -24,12 +24,13 @@ struct PromptArgs {
     float *part_o, *part_ml;                   // unnormalised outputs and (maximum, sum) of the parts; fp32: [splits][Hq][n_q]
     void* cuts;                                // bf16: what the second kernel joins
     int32_t* status;
+    int withhold;                              // debug builds: the copies to leave out
 };
 
 constexpr int kPromptDocs = 8192;              // documents at most
 
 // The tensor-core kernels (bf16): their workspace, and the launch.
-void prompt_mma_carve(Carver& cv, int dh, PromptArgs* a);
+void prompt_mma_carve(Carver& cv, const metok_attention_params* p, PromptArgs* a);
 int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st);
 
 struct PromptDoc {
@@ -103,6 +104,7 @@ __device__ __forceinline__ PromptDoc prompt_tile(const PromptArgs& a, int at, Ti
 
 // Position of key j of the document whose Lk keys begin at k0 (or of the query that sits there).
 __device__ __forceinline__ float prompt_position(const PromptArgs& a, int k0, int Lk, int j) {
+    if (Lk < 1) return 0.f;                    // (there may be no key at k0)
     j = max(0, min(j, Lk - 1));
     return (float)(a.positions ? a.positions[k0 + j] : j);
 }

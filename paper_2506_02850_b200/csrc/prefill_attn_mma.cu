@@ -399,8 +399,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     if (elect_one()) {
                         const uint32_t fb = smem_u32(&full_bar[s]);
                         mbar_arrive_expect_tx(fb, S::kTile);
+                        const bool held = dbg_held(a.withhold, kDbgPromptAttn) && blockIdx.x == 0 && it == 0;       // debug builds: one copy never sent
 #pragma unroll
-                        for (int kb = 0; kb < S::KB; ++kb) {
+                        for (int kb = 0; kb < S::KB && !held; ++kb) {
                             if (j & 1) tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.v, kb * 64, row, gv, fb);
                             else tma_load_3d(kv_addr(s) + kb * S::kBlk, &maps.k, kb * 64, row, gk, fb);
                         }
@@ -870,10 +871,11 @@ int launch_dh(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
 
 }  // namespace
 
-void prompt_mma_carve(Carver& cv, int dh, PromptArgs* a) {
+void prompt_mma_carve(Carver& cv, const metok_attention_params* p, PromptArgs* a) {
     a->cuts = cv.take<Cut>(kNumSMs);
+    if (p->n_k <= kN) return;                          // pairs of one step are never cut
     a->part_ml = cv.take<float>((size_t)2 * kNumSMs * 2 * kM * 2);
-    a->part_o = cv.take<float>((size_t)2 * kNumSMs * 2 * kM * dh);
+    a->part_o = cv.take<float>((size_t)2 * kNumSMs * 2 * kM * p->dh);
 }
 
 int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st) {
