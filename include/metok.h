@@ -441,8 +441,8 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   aligned; all but q, k, v, out may be NULL.  seq_q and seq_k are both NULL for one
  *   document of all rows (n_seq = 1).  Positions lie in [0, 2^24).
  *   Rows of q, k, v, out and lse outside every document are neither used nor written,
- *   whatever they hold.  Inside a document v has to be finite: a row that a query does
- *   not see counts with weight 0.
+ *   whatever they hold.  Inside a document v has to be finite (below 2^100 for bf16): a row
+ *   that a query does not see counts with weight 0.
  *   status DEVICE int32: written METOK_OK; METOK_ERR_INVALID_ARG if seq_q or seq_k
  *   descends or leaves [0, n_q] / [0, n_k] (then no row is written); METOK_ERR_TIMEOUT.
  *
@@ -450,8 +450,9 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   fp32; the unnormalised weights are rounded to bf16 for the product with V.
  *   fp32: fp32 throughout.
  *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1 (n_q, n_k may be 0),
- *   Hq % Hkv, strides, softmax_scale not finite or <= 0, softcap < 0 or not finite, one of
- *   seq_q / seq_k without the other, n_seq != 1 without them); UNSUPPORTED (dh other
+ *   Hq % Hkv, strides, rows of out that overlap, softmax_scale not in (0, 1e38], softcap not in
+ *   [0, 1e38], softmax_scale / softcap > 1e38, one of seq_q / seq_k without the other, n_seq != 1
+ *   without them); UNSUPPORTED (dh other
  *   than 64 or 128, more than 2^24 rows, n_seq > 8192, Hq > 65535, more than 2^31 - 1 pieces of work);
  *   WORKSPACE.
  * ------------------------------------------------------------------------- */
@@ -491,8 +492,8 @@ METOK_API int metok_prefill_attention(int dtype, const metok_attention_params* p
  *   metok_paged_append writes new rows i = new_offsets[b] .. new_offsets[b+1]-1 of
  *   k_new / v_new ([Hkv][n_new][dh], strides in ELEMENTS between heads and between rows,
  *   multiples of 16 bytes, row strides >= dh) behind sequence b's kv_len[b] rows, with
- *   positions pos_new[i] (NULL: counted on from the position of the last row, from 0 in an
- *   empty sequence) and mass mass_new[i] (NULL: 0), and new_len[b] = kv_len[b] + the number
+ *   positions pos_new[i] (NULL: counted on from the position of the last row, which after an
+ *   eviction need not be the newest; from 0 in an empty sequence) and mass mass_new[i] (NULL: 0), and new_len[b] = kv_len[b] + the number
  *   of its rows.  new_offsets NULL: one row for every sequence (n_new = n_seqs).  kv_len is
  *   not written: the layers of a decoder append with the same kv_len; new_len must not
  *   overlap it.
@@ -542,8 +543,9 @@ METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const vo
  *   METOK_ERR_INVALID_ARG and its out, lse and mass are left as they were.
  *   The work is cut along the caches' lengths into equal pieces for all SMs and joined
  *   by a second kernel; a call's results depend on nothing but its inputs.
- *   Errors: INVALID_ARG (null or misaligned pointers, Hq % Hkv, strides, softmax_scale not
- *   finite or <= 0, softcap < 0 or not finite, and as in (6)); UNSUPPORTED (as in (6), Hq > 2048,
+ *   Errors: INVALID_ARG (null or misaligned pointers, Hq % Hkv, strides, rows of out that
+ *   overlap, softmax_scale not in (0, 1e38], softcap not in [0, 1e38], softmax_scale / softcap
+ *   > 1e38, and as in (6)); UNSUPPORTED (as in (6), Hq > 2048,
  *   more than 2^31 - 1 pieces of work); WORKSPACE.
  * ------------------------------------------------------------------------- */
 METOK_API size_t metok_paged_attention_workspace_bytes(int dtype, const metok_paged_cache* c, int Hq, int with_mass);
@@ -562,7 +564,9 @@ METOK_API int metok_paged_attention(int dtype, const metok_paged_cache* c, const
  *   where they are; the kept rows behind it, in ascending order, go to the places of the
  *   rows that leave, in ascending order: no row moves that need not.  So the rows are no
  *   longer in the order of their positions, which is why positions are wanted here and
- *   go with their rows; attention over the cache does not depend on the order.
+ *   go with their rows; attention over the cache does not depend on the order.  The last row
+ *   need not be the newest any more: the next metok_paged_append is told its rows'
+ *   positions (pos_new), and the next eviction comes after one.
  *     keep_idx[l][b][i] = the row that row i now holds (i < new_len[b]), -1 behind;
  *     K and V of every layer, positions and mass [L][n_seqs][S_cap] are moved;
  *     mass of the rows from new_len[b] to kv_len[b]-1 is set to 0.
@@ -574,7 +578,7 @@ METOK_API int metok_paged_attention(int dtype, const metok_paged_cache* c, const
  *   another sequence or has one twice, is left as it is in every layer and reports new_len = kv_len,
  *   keep_idx = -1 and status = METOK_ERR_INVALID_ARG.
  *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1, L < 1, budget < 1 or > S_cap,
- *   n_sink < 0, n_recent < 1, new_len overlapping kv_len, a pool given twice); UNSUPPORTED (as in (6);
+ *   n_sink < 0, n_recent < 1, new_len overlapping kv_len, pools that overlap); UNSUPPORTED (as in (6);
  *   L > 1024, L * n_seqs > 65535); WORKSPACE.
  * ------------------------------------------------------------------------- */
 METOK_API size_t metok_paged_evict_workspace_bytes(const metok_paged_cache* c, int L, int budget);

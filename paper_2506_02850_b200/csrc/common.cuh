@@ -1,6 +1,7 @@
 // Shared device/host helpers of the METok CUDA library (sm_100a).
 #pragma once
 
+#include <algorithm>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -140,6 +141,18 @@ __device__ __forceinline__ long long dbg_bound(long long idx, long long limit, i
 #endif
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }   // also true for NULL
+// Rows of dh elements in two dimensions of n0 and n1 of them with the strides s0 and s1: no two share an element.
+inline bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int dh) {
+    if (n0 < 2 || n1 < 2) return (n0 < 2 || s0 >= dh) && (n1 < 2 || s1 >= dh);
+    const int64_t a = std::min(s0, s1), b = std::max(s0, s1), n = s0 <= s1 ? n0 : n1;
+    return a >= dh && (b - dh) / a >= n - 1;           // all rows of the narrower dimension lie in one step of the other
+}
+// A softmax's scale and cap (0: none): what the kernels make of them is finite.
+inline bool softmax_numbers(float scale, float cap) {
+    constexpr float kMost = 1.0e38f;                   // times log2(e) it is still finite
+    return scale > 0.f && scale <= kMost && cap >= 0.f && cap <= kMost && (cap == 0.f || scale / cap <= kMost);
+}
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline int ceilq(double x) {

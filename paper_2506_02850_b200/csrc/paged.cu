@@ -432,12 +432,16 @@ extern "C" int metok_paged_evict(int dtype, const metok_paged_cache* c, void* co
         !aligned4(new_len) || !aligned4(status))
         return METOK_ERR_INVALID_ARG;
     if (L > 1024 || (long long)L * c->n_seqs > 65535) return METOK_ERR_UNSUPPORTED;
+    uintptr_t at[2 * 1024];
     for (int l = 0; l < L; ++l) {
-        if (!k_layers[l] || !v_layers[l] || !aligned16(k_layers[l]) || !aligned16(v_layers[l]) || k_layers[l] == v_layers[l]) return METOK_ERR_INVALID_ARG;
-        for (int m = 0; m < l; ++m)                                     // moved twice, a row would be lost
-            if (k_layers[l] == k_layers[m] || v_layers[l] == v_layers[m] || k_layers[l] == v_layers[m] || v_layers[l] == k_layers[m])
-                return METOK_ERR_INVALID_ARG;
+        if (!k_layers[l] || !v_layers[l] || !aligned16(k_layers[l]) || !aligned16(v_layers[l])) return METOK_ERR_INVALID_ARG;
+        at[2 * l] = reinterpret_cast<uintptr_t>(k_layers[l]);
+        at[2 * l + 1] = reinterpret_cast<uintptr_t>(v_layers[l]);
     }
+    std::sort(at, at + 2 * L);
+    const size_t pool = ((size_t)d.n_pages * d.Hkv << d.page_shift) * d.row_chunks * 16;
+    for (int i = 1; i < 2 * L; ++i)                                     // moved twice, a row would be lost
+        if (at[i] - at[i - 1] < pool) return METOK_ERR_INVALID_ARG;
     if (overlap(new_len, (size_t)c->n_seqs * 4, c->kv_len, (size_t)c->n_seqs * 4)) return METOK_ERR_INVALID_ARG;
     if (!ws || !aligned16(ws) || ws_bytes < metok_paged_evict_workspace_bytes(c, L, budget)) return METOK_ERR_WORKSPACE;
     EvictArgs a;

@@ -29,7 +29,6 @@ inline int paged_dims(int dtype, const metok_paged_cache* c, PagedDims* d) {
     *d = {c->n_pages, c->Hkv, shift, c->dh, c->n_seqs, c->max_pages, c->dh * esize / 16};
     return METOK_OK;
 }
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }   // also true for NULL
 // [a, a + an) and [b, b + bn) share an element
 inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);

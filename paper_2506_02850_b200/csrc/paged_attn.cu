@@ -894,7 +894,9 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
     {
         METOK_TIMED("paged_join", st);
         const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0, st, a);
+        const size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
+        METOK_ALLOW_SMEM((paged_join_kernel<T, DH>), smem);
+        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), smem, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;
@@ -934,6 +936,7 @@ extern "C" int metok_paged_attention(int dtype, const metok_paged_cache* c, cons
     if (rc != METOK_OK) return rc;
     if (!c->k_pool || !c->v_pool || !c->block_table || !c->kv_len || !q || !out || !status) return METOK_ERR_INVALID_ARG;
     if (Hq < 1 || Hq % d.Hkv) return METOK_ERR_INVALID_ARG;
+    if (Hq > 2048) return METOK_ERR_UNSUPPORTED;
     if (!aligned16(c->k_pool) || !aligned16(c->v_pool) || !aligned16(q) || !aligned16(out)) return METOK_ERR_INVALID_ARG;
     if (!aligned4(c->block_table) || !aligned4(c->kv_len) || !aligned4(slopes) || !aligned4(positions) || !aligned4(mass) ||
         !aligned4(lse) || !aligned4(status))
@@ -941,11 +944,10 @@ extern "C" int metok_paged_attention(int dtype, const metok_paged_cache* c, cons
     const int per = 16 / (dtype == METOK_F32 ? 4 : 2);
     if (q_seq < 0 || q_head < 0 || out_seq < 0 || out_head < 0 || (q_seq | q_head | out_seq | out_head) % per) return METOK_ERR_INVALID_ARG;
     // outputs of different heads and sequences do not overlap
-    if ((Hq > 1 && out_head < d.dh) || (d.n_seqs > 1 && out_seq < d.dh)) return METOK_ERR_INVALID_ARG;
-    if (!(softmax_scale > 0.f) || !(softmax_scale < 3.0e38f) || !(softcap >= 0.f) || !(softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
+    if (!rows_apart(d.n_seqs, out_seq, Hq, out_head, d.dh) || !softmax_numbers(softmax_scale, softcap)) return METOK_ERR_INVALID_ARG;
     const PagedPlan p = paged_plan(dtype, d, Hq);
     const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-    if (join > 0x7FFFFFFFLL || Hq > 2048) return METOK_ERR_UNSUPPORTED;
+    if (join > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     PagedAttnArgs a;
     a.d = d;

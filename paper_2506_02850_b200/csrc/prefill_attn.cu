@@ -295,7 +295,6 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     int rc = prompt_check(dtype, p);
     if (rc != METOK_OK) return rc;
     if ((p->n_q > 0 && (!p->q || !p->out)) || (p->n_k > 0 && (!p->k || !p->v)) || !status) return METOK_ERR_INVALID_ARG;
-    auto aligned4 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; };
     if (!aligned16(p->q) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->out)) return METOK_ERR_INVALID_ARG;
     if (!aligned4(p->lse) || !aligned4(p->seq_q) || !aligned4(p->seq_k) || !aligned4(p->prefix_len) || !aligned4(p->positions) ||
         !aligned4(p->slopes) || !aligned4(status))
@@ -303,9 +302,9 @@ extern "C" int metok_prefill_attention(int dtype, const metok_attention_params* 
     const int per = 16 / (dtype == METOK_F32 ? 4 : 2);
     if (p->q_head < 0 || p->k_head < 0 || p->v_head < 0 || p->out_head < 0) return METOK_ERR_INVALID_ARG;
     if (p->q_row < p->dh || p->k_row < p->dh || p->v_row < p->dh || p->out_row < p->dh) return METOK_ERR_INVALID_ARG;
-    if (p->Hq > 1 && (p->q_head < p->dh || p->out_head < p->dh)) return METOK_ERR_INVALID_ARG;
+    if ((p->Hq > 1 && p->q_head < p->dh) || !rows_apart(p->Hq, p->out_head, p->n_q, p->out_row, p->dh)) return METOK_ERR_INVALID_ARG;
     if ((p->q_head | p->k_head | p->v_head | p->out_head | p->q_row | p->k_row | p->v_row | p->out_row) % per) return METOK_ERR_INVALID_ARG;
-    if (!(p->softmax_scale > 0.f) || !(p->softmax_scale < 3.0e38f) || !(p->softcap >= 0.f) || !(p->softcap < 3.0e38f)) return METOK_ERR_INVALID_ARG;
+    if (!softmax_numbers(p->softmax_scale, p->softcap)) return METOK_ERR_INVALID_ARG;
     const size_t need = metok_prefill_attention_workspace_bytes(dtype, p);
     if (need > 0 && (!ws || !aligned16(ws) || ws_bytes < need)) return METOK_ERR_WORKSPACE;
     PromptArgs a = {};

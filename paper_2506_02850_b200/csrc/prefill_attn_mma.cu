@@ -34,8 +34,9 @@ namespace metok {
 namespace {
 
 constexpr int kM = 128, kN = 128, kThreads = 352;
-// Sum of 64 weights beyond which a row's reference grows; by how many octaves a logit has passed it then, and how far above it the new one is.
-constexpr float kMost = 1.0e18f, kGrow = 16.f, kRoom = 32.f;
+// Sum of 64 weights beyond which a row's reference grows; by how many octaves a logit has passed it then (one of 64 has by 18).  Weights stay
+// below 2^24, so V may be as large as 2^100, and the reference never lies above the maximum, so what underflows is below 2^-125 of it.
+constexpr float kMost = 0x1p24f, kGrow = 16.f;
 constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
 template <int DH>
@@ -93,7 +94,8 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 126] are held there, a NaN gives something that is no weight.
+// 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 126] are held there, a NaN gives something that is no weight.  2^-125 is
+// taken off (rounded away beside what counts), so that a hidden key's weight is 0 and its V, however large, adds nothing.
 __device__ __forceinline__ uint64_t exp2_held_pair(uint64_t x) {
     float a, b;
     sm100::unpair(x, a, b);
@@ -101,7 +103,7 @@ __device__ __forceinline__ uint64_t exp2_held_pair(uint64_t x) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(-125.f));
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(126.f));
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(126.f));
-    return sm100::exp2_fma_core(sm100::pair(a, b));
+    return sm100::add_pair(sm100::exp2_fma_core(sm100::pair(a, b)), sm100::pair(-0x1p-125f, -0x1p-125f));
 }
 // 16 registers of this thread's lane to 16 tensor-memory columns.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -644,10 +646,10 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                         }
                         const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) + base;
                         const bool grow = keys > 0 && (again ? mx > m + kGrow : m == ninf && mx > ninf);
-                        const float to = again ? mx + kRoom : mx, f = grow ? fast_exp2(m - to) : 1.f;
-                        if (grow) m = to;
+                        const float f = grow ? fast_exp2(m - mx) : 1.f;
+                        if (grow) m = mx;
                         l *= f;
-                        const uint64_t less = grow ? pair(base - to, base - to) : 0ull;
+                        const uint64_t less = grow ? pair(base - mx, base - mx) : 0ull;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = add_pair(v[i], less);
                         if (j > 0 || half) {           // when the product before this one on O_x is complete
@@ -668,8 +670,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     uint64_t sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        // some on the FMA pipe, so that both work.  (There a hidden key's weight is 2^-125, not 0: nothing beside any weight that counts,
-                        // and a row that sees no key is known by its m.)
+                        // some on the FMA pipe, so that both work
                         const uint64_t w = kShare(i) ? exp2_held_pair(v[i]) : exp2_pair(v[i]);
                         if (i & 1) sum1 = add_pair(sum1, w);
                         else sum0 = add_pair(sum0, w);
