@@ -502,7 +502,6 @@ __global__ void __launch_bounds__(kThreads)
 paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     using namespace sm100;
     using S = PagedShape<T, DH>;
-    grid_dep_wait();
     extern __shared__ uint8_t smem_dyn[];
     __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages];
     __shared__ __align__(16) float s_o[2][kUnitHeads * DH];
@@ -514,16 +513,19 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     const int subs = a.d.Hkv * a.NC;
-    if (blockIdx.x == a.grid) {                        // one CTA more than pieces
-        if (warp == 0) write_line(a);
-        return;
-    }
     if (threadIdx.x == 0) {
-        if (blockIdx.x == 0) *a.status = METOK_OK;     // a wait that gives up writes it, seconds later
+        prefetch_tmap(&tm_k);
+        prefetch_tmap(&tm_v);
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), kWarps); }
         s_abort = 0;
         mbar_fence_init();
     }
+    grid_dep_wait();
+    if (blockIdx.x == a.grid) {                        // one CTA more than pieces
+        if (warp == 0) write_line(a);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = METOK_OK;       // a wait that gives up writes it, seconds later
     const long long T_all = line_tiles(a, s_sum) * subs, ctas = busy_ctas(a, T_all);
     if (blockIdx.x >= ctas) return;                    // uniform
     const long long t_lo = T_all * blockIdx.x / ctas, t_hi = T_all * (blockIdx.x + 1) / ctas;
@@ -568,7 +570,6 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     volatile int* abort_flag = &s_abort;
 
     if (warp == kWarps) {                              // brings the tiles
-        if (lane == 0) { prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
         const int page_rows = 1 << a.d.page_shift, piece = min(page_rows, S::kTile), per_tile = S::kTile / piece;
         const uint32_t piece_bytes = (uint32_t)piece * 128u;
         int it = 0;
@@ -705,19 +706,17 @@ constexpr int kJoinThreads = 128, kMassRows = 128;
 template <typename T, int DH>
 __global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const PagedAttnArgs a) {
-    grid_dep_wait();
+    // Up to the wait: what needs only the call's inputs, which were complete when the first kernel was let go.
     __shared__ __align__(16) float s_acc[kJoinThreads][4];
-    __shared__ float s_l[kJoinThreads];
-    __shared__ float s_w[kJoinThreads / 32];
+    __shared__ float2 s_ml[kJoinThreads];
     extern __shared__ __align__(16) uint8_t s_dyn[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31;
     const int outs = a.d.n_seqs * a.Hq;
     const bool weights = (int)blockIdx.x >= outs;
     const int chunks = (a.d.S_cap() + kMassRows - 1) / kMassRows;
     const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / a.Hq;
     const int len = a.kv_len[b], subs = a.d.Hkv * a.NC;
     const int row0 = weights ? (((int)blockIdx.x - outs) - b * chunks) * kMassRows : 0;
-    if (weights && row0 >= len) return;
     // the sequence is sound: only then anything is written for it
     bool ok = len >= 0 && len <= a.d.S_cap();
     if (ok) {
@@ -729,36 +728,41 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         ok = __syncthreads_and(there);
     }
-    if (!ok) {
-        if (tid == 0) *a.status = METOK_ERR_INVALID_ARG;
-        return;
-    }
-    const long long all = a.line[a.d.n_seqs] * subs, base = a.line[b] * subs;
     const int nt = unit_tiles(a, b);
+    long long all = 0, base = 0;                       // tiles of the line, and of the sequences before b
+    const bool few = a.d.n_seqs <= 32;                 // one look at all lengths; else the line that the first kernel wrote
+    if (few) {
+        const int mine = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
+        all = (long long)__reduce_add_sync(0xFFFFFFFFu, mine) * subs;
+        base = (long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? mine : 0) * subs;
+    } else {
+        grid_dep_wait();
+        all = a.line[a.d.n_seqs] * subs;
+        base = a.line[b] * subs;
+    }
+
+    const auto sound = [&] {
+        if (few) grid_dep_wait();
+        if (!ok && tid == 0) *a.status = METOK_ERR_INVALID_ARG;
+        return ok;
+    };
 
     if (!weights) {
         const int h = (int)blockIdx.x - b * a.Hq, hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads;
         T* out = reinterpret_cast<T*>(a.out) + b * a.out_seq + h * a.out_head;
+        const int sub = hk * a.NC + ch;
+        const Slots sl = nt ? unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt) : Slots{0, 0};
+        if (!sound()) return;
         if (nt == 0) {
             for (int i = tid; i < DH; i += kJoinThreads) from_float(out[i], 0.f);
             if (tid == 0 && a.lse) a.lse[(size_t)b * a.Hq + h] = __int_as_float(0xFF800000);
             return;
         }
-        const int sub = hk * a.NC + ch;
-        const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
-        // DH / 4 threads side by side, kRuns slots at a time
+        // DH / 4 threads side by side, kRuns slots at a time, each run with a maximum of its own
         constexpr int kLanes = DH / 4, kRuns = kJoinThreads / kLanes;
         const int col = tid % kLanes, run = tid / kLanes;
-        float M = kLow;
-        for (int i = tid; i < sl.n; i += kJoinThreads) M = fmaxf(M, a.part_ml[((sl.first + i) * a.heads + hl) * 2]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-        if (lane == 0) s_w[warp] = M;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kJoinThreads / 32; ++w) M = fmaxf(M, s_w[w]);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float L = 0.f;
+        float M = kLow, L = 0.f;
         constexpr int kAhead = 6;                      // slots whose loads are on their way
         for (int i0 = run; i0 < sl.n; i0 += kRuns * kAhead) {
             float2 ml[kAhead];
@@ -770,6 +774,13 @@ paged_join_kernel(const PagedAttnArgs a) {
                 ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + at * 2) : make_float2(kLow, 0.f);
                 o[u] = in ? reinterpret_cast<const float4*>(a.part_o + at * DH)[col] : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+            float top = M;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) top = fmaxf(top, ml[u].x);
+            const float less = sm100::fast_exp2(M - top);
+            M = top;
+            L *= less;
+            acc.x *= less; acc.y *= less; acc.z *= less; acc.w *= less;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const float f = sm100::fast_exp2(ml[u].x - M);
@@ -778,14 +789,20 @@ paged_join_kernel(const PagedAttnArgs a) {
             }
         }
         *reinterpret_cast<float4*>(s_acc[tid]) = acc;
-        s_l[tid] = L;
+        s_ml[tid] = make_float2(M, L);
         __syncthreads();
         if (run == 0) {
 #pragma unroll
-            for (int r = 1; r < kRuns; ++r) {
+            for (int r = 1; r < kRuns; ++r) M = fmaxf(M, s_ml[r * kLanes + col].x);
+            L = 0.f;
+            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) {
                 const float4 o = *reinterpret_cast<const float4*>(s_acc[r * kLanes + col]);
-                acc.x += o.x; acc.y += o.y; acc.z += o.z; acc.w += o.w;
-                L += s_l[r * kLanes + col];
+                const float2 ml = s_ml[r * kLanes + col];
+                const float f = sm100::fast_exp2(ml.x - M);
+                acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
+                L += f * ml.y;
             }
             const float inv = 1.f / L;
             from_float(out[col * 4], acc.x * inv);
@@ -803,11 +820,12 @@ paged_join_kernel(const PagedAttnArgs a) {
     int* s_n = reinterpret_cast<int*>(s_first + subs);                   // [subs]
     float* s_lse = reinterpret_cast<float*>(s_n + subs);                 // [Hq]: log2 of the sum
     long long* s_off = reinterpret_cast<long long*>(s_dyn + ((size_t)subs * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8);   // [Hq]: the head's logits of the sequence
-    for (int sub = tid; sub < subs; sub += kJoinThreads) {
+    for (int sub = tid; sub < subs && nt; sub += kJoinThreads) {
         const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
         s_first[sub] = sl.first;
         s_n[sub] = sl.n;
     }
+    if (!sound() || row0 >= len) return;
     __syncthreads();
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
         const int h = h0 + (tid >> 3), part = tid & 7;

@@ -796,23 +796,25 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
-// Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut.  A lane per row, a warp for DH / 8 columns of 32 rows,
-// kAhead parts on their way.
-constexpr int kCutBlocks = 2 * kM / 32, kAhead = 2;
+// Joins the parts of the pairs that were cut: blockIdx.x is the CTA that noted the cut.  A lane per row, a warp for kCutPieces 16-byte
+// pieces of 32 rows' outputs, kAhead parts on their way (four pieces and two parts, on half as many CTAs: 28 heads of 64 rows over 18 496 keys,
+// which leave 18 parts a pair, 14.7 -> 12.9 us; two pieces with eight parts take 8 us longer where there are many pairs).
+constexpr int kCutBlocks = 2 * kM / 32, kCutPieces = 2, kAhead = 4;
 template <int DH>
 __global__ void __launch_bounds__(256)
 prompt_cut_join_kernel(const PromptArgs a) {
     grid_dep_wait();
     const Cut cut = reinterpret_cast<const Cut*>(a.cuts)[blockIdx.x];
     if (cut.c1 < 0) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = blockIdx.y * 32 + lane, x = rr / kM, r = rr - x * kM;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rr = (blockIdx.y % kCutBlocks) * 32 + lane, x = rr / kM, r = rr - x * kM;
     const int i = r / a.heads_item, h = (x ? cut.h0[1] : cut.h0[0]) + r - i * a.heads_item;
     if (r >= (x ? cut.rows[1] : cut.rows[0]) || h >= a.G) return;
     const int parts = cut.c1 - cut.c0 + 1, head = cut.g * a.G + h;
     const long long row = cut.q0 + (x ? cut.i0[1] : cut.i0[0]) + i;
     auto slot = [&](int p) { return (size_t)(p == 0 ? cut.first_slot : 2 * (cut.c0 + p)); };
     const float ninf = __int_as_float(0xFF800000);
-    constexpr int E = DH / 32;                         // 16-byte pieces of a warp's columns
+    constexpr int E = kCutPieces;
+    const int piece = (blockIdx.y / kCutBlocks * 8 + warp) * E;
     float M = ninf, L = 0.f;
     float4 acc[E];
 #pragma unroll
@@ -826,7 +828,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
             ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + (slot(p0 + u) * (2 * kM) + rr) * 2) : make_float2(ninf, 0.f);
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                o[u][e] = in ? reinterpret_cast<const float4*>(a.part_o)[(slot(p0 + u) * (DH / 4) + warp * E + e) * (2 * kM) + rr] : make_float4(0.f, 0.f, 0.f, 0.f);
+                o[u][e] = in ? reinterpret_cast<const float4*>(a.part_o)[(slot(p0 + u) * (DH / 4) + piece + e) * (2 * kM) + rr] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -843,9 +845,9 @@ prompt_cut_join_kernel(const PromptArgs a) {
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)head * a.out_head + row * a.out_row;
 #pragma unroll
     for (int e = 0; e < E; e += 2)
-        reinterpret_cast<uint4*>(out)[(warp * E + e) / 2] = make_uint4(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv),
+        reinterpret_cast<uint4*>(out)[(piece + e) / 2] = make_uint4(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv),
                                                                        pack_bf16(acc[e + 1].x * inv, acc[e + 1].y * inv), pack_bf16(acc[e + 1].z * inv, acc[e + 1].w * inv));
-    if (warp == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
+    if (piece == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
 }
 
 template <int DH, bool kCap, bool kBias>
@@ -859,7 +861,7 @@ int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
     METOK_LAUNCH_CHECK();
     if (a.n_k > kN) {                                  // (pairs of one step are never cut)
         METOK_TIMED("prompt_cut_join", st);
-        launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks), dim3(256), 0, st, a);
+        launch_chained(prompt_cut_join_kernel<DH>, dim3(kNumSMs, kCutBlocks * (DH / 32 / kCutPieces)), dim3(256), 0, st, a);
         METOK_LAUNCH_CHECK();
     }
     return METOK_OK;
