@@ -58,8 +58,8 @@ struct KernelTimer {
 // completion of a kernel implies completion of all kernels before it on the stream.  Before the wait a
 // CTA may read what was complete when the kernel before it was let go, that is, what kernels before
 // THAT one (or the caller) have written; and it may take tensor memory if the kernel before it takes
-// none.  Most kernels wait first; cs_event_topk_kernel, merge_assign_mma_kernel and merge_avg_kernel do
-// not.  The launch error is picked up by METOK_LAUNCH_CHECK().
+// none.  Most kernels wait first; cs_event_topk_kernel, merge_assign_mma_kernel, merge_avg_kernel and
+// paged_join_kernel do not.  The launch error is picked up by METOK_LAUNCH_CHECK().
 // `cluster` > 1 launches clusters of that many CTAs along x.
 template <typename... P, typename... A>
 inline void launch_chained_clusters(int cluster, void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,

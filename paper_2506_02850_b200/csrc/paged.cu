@@ -232,7 +232,7 @@ evict_select_kernel(const EvictArgs a) {
     __syncthreads();                                   // the bits are done with
     if (a.keys_fit)
         for (int i = tid; i < len; i += nthr) s_dyn[i] = evict_key(mass[i], pos[i], a.n_sink, recent_from);
-    auto key_of = [&](int i) { return a.keys_fit ? s_dyn[i] : evict_key(mass[i], pos[i], a.n_sink, recent_from); };   // by the same thread
+    auto key_of = [&](int i) { return a.keys_fit ? s_dyn[i] : evict_key(mass[i], pos[i], a.n_sink, recent_from); };
 
     // the n-th highest key, digit by digit from the top
     uint32_t prefix = 0u;                              // its digits so far
@@ -273,32 +273,48 @@ evict_select_kernel(const EvictArgs a) {
         if (s_all) break;                              // all rows with these digits stay
         __syncthreads();
     }
-    // keys of at least `prefix` with zeros behind it stay; among equal ones (all digits decided) the first `need`
-    if (done < 32) {
-        prefix <<= 32 - done;
-        need = len;
-    }
-    const bool by_order = done == 32;
+    // keys of at least `prefix` with zeros behind it stay; where not all equal ones do, the first `need` of them
+    if (done < 32) prefix <<= 32 - done;
+    const bool by_order = done == 32 && !s_all;
 
-    // rows in order: above the threshold, or among the first `need` equal to it, they stay
+    // rows in order, kRun of them per thread: above the threshold, or among the first `need` equal to it, they stay
+    constexpr int kRun = 4;
     int32_t *from = a.from + prob * a.budget, *to = a.to + prob * a.budget;
     int equal = 0, holes = 0, movers = 0;              // so far
 #pragma unroll 1
-    for (int base = 0; base < len; base += nthr) {
-        const int i = base + tid;
-        const uint32_t k = i < len ? key_of(i) : 0u;
-        const bool eq = i < len && k == prefix;
-        int total, eq_before = 0;
+    for (int base = 0; base < len; base += nthr * kRun) {
+        const int i0 = base + tid * kRun;
+        uint32_t k[kRun];
+        int total, eq_before = 0, x = 0;
+        bool stay[kRun];
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) k[u] = i0 + u < len ? key_of(i0 + u) : 0u;
         if (by_order) {
+            int eq = 0;
+#pragma unroll
+            for (int u = 0; u < kRun; ++u) eq += i0 + u < len && k[u] == prefix;
             eq_before = equal + block_scan(eq, s_warp, &total);
             equal += total;
         }
-        const bool stay = i < len && (k > prefix || (eq && eq_before < need));
-        const bool hole = i < n && !stay, mover = i >= n && stay;
-        const int x = block_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), s_warp, &total);   // at most 1024 of each
-        if (hole) to[holes + (x & 0xFFFF)] = i;
-        if (mover) from[movers + (x >> 16)] = i;
-        if (stay && i < n) keep[i] = i;
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+            const bool in = i0 + u < len, eq = in && k[u] == prefix;
+            stay[u] = in && (k[u] > prefix || (eq && (!by_order || eq_before < need)));
+            eq_before += eq;
+            x += i0 + u < n ? !stay[u] : stay[u] ? 1 << 16 : 0;           // holes below, movers above: at most 4096 of each
+        }
+        x = block_scan(x, s_warp, &total);
+        int hole = holes + (x & 0xFFFF), mover = movers + (x >> 16);
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+            const int i = i0 + u;
+            if (i < n) {
+                if (stay[u]) keep[i] = i;
+                else to[hole++] = i;
+            } else if (stay[u]) {
+                from[mover++] = i;
+            }
+        }
         holes += total & 0xFFFF;
         movers += total >> 16;
     }

@@ -814,8 +814,8 @@ paged_join_kernel(const PagedAttnArgs a) {
         return;
     }
 
-    // weights: where every unit's partials lie, then the heads' normalisers: eight threads per head, a running (maximum, sum) each
-    // with four loads on their way
+    // weights: where every unit's partials and every head's logits lie, then the heads' normalisers: eight threads per head, a running
+    // (maximum, sum) each with kAhead loads on their way; the first heads' logits come meanwhile
     long long* s_first = reinterpret_cast<long long*>(s_dyn);            // [subs]
     int* s_n = reinterpret_cast<int*>(s_first + subs);                   // [subs]
     float* s_lse = reinterpret_cast<float*>(s_n + subs);                 // [Hq]: log2 of the sum
@@ -825,8 +825,21 @@ paged_join_kernel(const PagedAttnArgs a) {
         s_first[sub] = sl.first;
         s_n[sub] = sl.n;
     }
-    if (!sound() || row0 >= len) return;
+    for (int h = tid; h < a.Hq; h += kJoinThreads) {
+        const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads;
+        s_off[h] = ((long long)(hk * a.NC + ch) * nt * a.heads + (g - ch * a.heads)) << a.tile_shift;
+    }
     __syncthreads();
+    if (!sound() || row0 >= len) return;
+    const int row = min(row0 + tid, len - 1), tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
+    const float* x = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
+    constexpr int kHeads = 16, kAhead = 10;
+    float v[kHeads];
+    auto logits_of = [&](int h0) {
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) v[u] = h0 + u < a.Hq ? x[s_off[h0 + u]] : kLow;
+    };
+    logits_of(0);
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
         const int h = h0 + (tid >> 3), part = tid & 7;
         float M = kLow, L = 0.f;
@@ -834,13 +847,16 @@ paged_join_kernel(const PagedAttnArgs a) {
             const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads, sub = hk * a.NC + ch;
             const Slots sl = {s_first[sub], s_n[sub]};
             const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + sl.first * a.heads + hl;
-            for (int i0 = part; i0 < sl.n; i0 += 32) {
-                float2 x[4];
+            for (int i0 = part; i0 < sl.n; i0 += 8 * kAhead) {
+                float2 p[kAhead];
+                float top = M;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) x[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
-                const float top = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), M);
-                L = L * sm100::fast_exp2(M - top) + (sm100::fast_exp2(x[0].x - top) * x[0].y + sm100::fast_exp2(x[1].x - top) * x[1].y) +
-                    (sm100::fast_exp2(x[2].x - top) * x[2].y + sm100::fast_exp2(x[3].x - top) * x[3].y);
+                for (int u = 0; u < kAhead; ++u) p[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) top = fmaxf(top, p[u].x);
+                L *= sm100::fast_exp2(M - top);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) L += sm100::fast_exp2(p[u].x - top) * p[u].y;
                 M = top;
             }
         }
@@ -850,24 +866,15 @@ paged_join_kernel(const PagedAttnArgs a) {
             L = L * sm100::fast_exp2(M - top) + l2 * sm100::fast_exp2(m2 - top);
             M = top;
         }
-        if (h < a.Hq && part == 0) {
-            const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads;
-            s_lse[h] = M + log2f(L);
-            s_off[h] = ((long long)(hk * a.NC + ch) * nt * a.heads + (g - ch * a.heads)) << a.tile_shift;
-        }
+        if (h < a.Hq && part == 0) s_lse[h] = M + log2f(L);
     }
     __syncthreads();
-    const int row = row0 + tid;
-    if (row >= len) return;
-    const int tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
-    const float* x = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
+    if (row0 + tid >= len) return;
     float sum = 0.f;
-    for (int h = 0; h < a.Hq; h += 8) {                // eight loads on their way (a loop of single ones would wait for each)
-        float v[8];
+    for (int h = 0; h < a.Hq; h += kHeads) {           // kHeads loads on their way (a loop of single ones would wait for each)
+        if (h) logits_of(h);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = h + u < a.Hq ? x[s_off[h + u]] : kLow;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum += h + u < a.Hq ? sm100::fast_exp2(v[u] - s_lse[h + u]) : 0.f;
+        for (int u = 0; u < kHeads; ++u) sum += h + u < a.Hq ? sm100::fast_exp2(v[u] - s_lse[h + u]) : 0.f;
     }
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
 }
