@@ -21,6 +21,7 @@ struct PromptArgs {
     int splits;                                // fp32: parts that a tile's keys are cut into; above 1 the parts are joined by another kernel
     int heads_item, head_chunks, rows_item;    // query heads of a tile of rows, such tiles for all heads of a K/V head, document rows of a tile
     uint32_t rows_magic;                       // bf16: ceil(2^32 / rows_item)
+    int pair_cost;                             // bf16: what a pair costs beside its key tiles, in tiles
     float *part_o, *part_ml;                   // unnormalised outputs and (maximum, sum) of the parts; fp32: [splits][Hq][n_q]
     void* cuts;                                // bf16: what the second kernel joins
     int32_t* status;

@@ -149,10 +149,10 @@ __device__ __forceinline__ Pair pair_of(const PromptArgs& a, const PromptDoc& d,
     }
     return p;
 }
-// Steps of a pair in the line: its key tiles, and one where it has none.
+// Steps of a pair in the line: what it costs beside its key tiles (first, without work of their own), then the tiles; one at least.
 __device__ __forceinline__ int pair_steps(const PromptArgs& a, const PromptDoc& d, int t) {
     const int last = item_block(a, min(2 * t + 1, doc_items(a, d.Lq) - 1)), r = a.rows_item;
-    return max(1, (prompt_keys(a, d, min(d.Lq, (last + 1) * r) - 1) + kN - 1) / kN);
+    return max(1, a.pair_cost + (prompt_keys(a, d, min(d.Lq, (last + 1) * r) - 1) + kN - 1) / kN);
 }
 __device__ __forceinline__ int doc_pairs(const PromptArgs& a, int Lq) { return (doc_items(a, Lq) + 1) / 2; }
 
@@ -220,7 +220,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     __shared__ int s_abort;
     __shared__ __align__(16) float s_pos[2][2][kN];    // [item][buffer]: positions of the keys
     __shared__ Walk s_walk[8];                         // the rows' warps keep their way along the line here: in registers it would cost spills
-    __shared__ int s_at[4];
+    __shared__ int s_at[5];
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     auto q_addr = [&](int x) { return smem_base + (uint32_t)x * S::kTile; };
@@ -273,10 +273,11 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     const Line line(all, gridDim.x);
     if (blockIdx.x >= line.ctas) return;
     const long long begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
-    if (warp == 0) {
+    if (warp < 2) {                                    // the pair where it begins (0), and where it ends (1)
+        const long long edge = warp ? end : begin;
         int g = 0;
-        if (a.Hkv > 1) g = all < (1LL << 31) ? (int)((uint32_t)begin / (uint32_t)per_head) : (int)(begin / per_head);
-        const long long at = begin - g * per_head;
+        if (a.Hkv > 1) g = all < (1LL << 31) ? (int)((uint32_t)edge / (uint32_t)per_head) : (int)(edge / per_head);
+        const long long at = warp && edge == all ? 0 : edge - g * per_head;
         int lo = 0, hi = a.n_seq;                      // the document: s_pre[lo] <= at < s_pre[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -305,7 +306,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
             before += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
-        if (lane == 0) {
+        if (lane == 0 && warp) {
+            s_at[4] = rest;
+        } else if (lane == 0) {
             s_at[0] = g;
             s_at[1] = lo;
             s_at[2] = t0;
@@ -321,7 +324,10 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     walk.e0 = s_at[3];
     walk.d = doc_of(a, walk.doc);
     walk.pairs = doc_pairs(a, walk.d.Lq);
-    walk.left = end - begin;
+    // A pair is not cut within its cost (a part without tiles would be no help, and pairs of one tile stay whole): such a cut is moved to the
+    // pair's first step.
+    walk.left = end - begin + (walk.e0 <= a.pair_cost ? walk.e0 : 0) - (s_at[4] <= a.pair_cost ? s_at[4] : 0);
+    if (walk.e0 <= a.pair_cost) walk.e0 = 0;
 
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&q_bar), 1);
@@ -348,21 +354,21 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem_base, 0);
     volatile int* abort_flag = &s_abort;
 
-    // this CTA's part of the walk's pair: steps e0 .. e1 - 1, which are key tiles lo + nt - 1 down to lo; item x joins in at step st[x]
+    // this CTA's part of the walk's pair: steps e0 .. e1 - 1, with key tiles lo + nt - 1 down to lo; item x joins in at tile st[x] of them
     struct Part {
         Pair p;
-        int steps, e1, lo, nt, st[2];
+        int steps, lo, nt, st[2];
         bool whole;
     };
     auto part_of = [&](const Walk& w) {
         Part q;
         q.p = pair_of(a, w.d, w.t);
-        const int steps = max(1, q.p.nt);
+        const int steps = max(1, q.p.nt + a.pair_cost);
         q.steps = (int)min((long long)(steps - w.e0), w.left);
-        q.e1 = w.e0 + q.steps;
         q.whole = q.steps == steps;
-        q.lo = max(0, q.p.nt - q.e1);
-        q.nt = q.p.nt ? q.steps : 0;
+        const int t0 = max(0, w.e0 - a.pair_cost), t1 = max(0, w.e0 + q.steps - a.pair_cost);
+        q.lo = max(0, q.p.nt - t1);
+        q.nt = q.p.nt ? t1 - t0 : 0;
 #pragma unroll
         for (int x = 0; x < 2; ++x) q.st[x] = q.nt - max(0, min(q.p.n[x] - q.lo, q.nt));
         return q;
@@ -764,9 +770,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         }
         // a pair that began in another CTA: the second of those that share it notes what there is to join
         if (threadIdx.x == 0 && first_part && my_walk->e0 > 0) {
-            const int steps = max(1, part.p.nt);
+            const int steps = max(1, part.p.nt + a.pair_cost);
             const long long f0 = begin - my_walk->e0;  // the pair's place in the line
-            const int c0 = line.holder(f0), c1 = line.holder(f0 + steps - 1);
+            const int c0 = line.holder(f0 + a.pair_cost), c1 = line.holder(f0 + steps - 1);
             if (c0 + 1 == blockIdx.x) {
                 Cut cut;
                 cut.c0 = c0;
@@ -890,6 +896,10 @@ int launch_prompt_attn_mma(PromptArgs a, int dh, cudaStream_t st) {
     for (int c = 0; c < 7; ++c) a.cap_poly[c] = (float)(kTanh[c] * a.cap_log2);
     a.rows_magic = a.rows_item > 1 ? (uint32_t)((0x100000000ULL + a.rows_item - 1) / a.rows_item) : 0u;
     a.head_chunks = ceil_div(a.G, a.heads_item);
+    // A pair costs its first reference, its output and code that the instruction cache does not hold beside its tiles: 5 500 to 6 500 clocks,
+    // where a tile takes 3 300 (no cap, no bias) to 5 600.  It counts where every CTA has pairs of its own (where they are cut among CTAs, each
+    // has two parts at most): nine documents of 7001 rows, 14 heads of 64, capped 96.2 -> 79.9 us; six of 3500, 28 heads of 128 65.5 -> 50.3.
+    a.pair_cost = a.n_k > kN && (long long)ceil_div(a.n_q, a.rows_item) * a.head_chunks * a.Hkv >= 2 * kNumSMs ? (a.cap_log2 > 0.f || a.slopes ? 1 : 2) : 0;
     maps.k_step = a.Hkv > 1 && a.k_head > 0;
     maps.v_step = a.Hkv > 1 && a.v_head > 0;
     if (a.n_q > 0) {

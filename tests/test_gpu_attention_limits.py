@@ -250,3 +250,17 @@ def test_rows_of_the_output_that_would_overlap_are_refused():
     with pytest.raises(B.MetokError):
         B.metok_paged_evict([a], [b], table, torch.tensor([100], dtype=torch.int32, device="cuda"), torch.zeros((1, 128), device="cuda"),
                             torch.zeros((1, 128), dtype=torch.int32, device="cuda"), 50, 1, 1)
+
+
+@pytest.mark.parametrize("softcap", [0.0, 6.0])
+@pytest.mark.parametrize("lens", [[1000], [500, 1, 130, 0, 369], [128] * 7 + [104], [30, 900, 70], [40] * 25])
+def test_more_pairs_of_tiles_than_processors(softcap, lens):
+    """Every processor has several pairs of tiles, cut where it suits the others."""
+    g = Q.gen(31)
+    q, k, v = Q.rows(g, 40, 1000, 64, torch.bfloat16, 1.5), Q.rows(g, 40, 1000, 64, torch.bfloat16), Q.rows(g, 40, 1000, 64, torch.bfloat16)
+    i = Q.offsets(lens)
+    Q.check(q, k, v, 0.125, i, i, softcap=softcap)
+    Q.check(q[:, :700], k, v, 0.125, Q.offsets([300, 0, 400]), Q.offsets([310, 90, 600]), softcap=softcap)
+    # most rows are in no document: less work than their number says
+    Q.check(q, k, v, 0.125, Q.offsets([5, 0, 90], 17), Q.offsets([5, 300, 90], 200), softcap=softcap)
+    Q.check(q, k, v, 0.125, Q.offsets([3], 900), Q.offsets([1], 900), softcap=softcap)
