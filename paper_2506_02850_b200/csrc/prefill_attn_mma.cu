@@ -8,7 +8,7 @@
 //   O_x += P_x V         tcgen05.mma, P_x from tensor memory, V as it lies (keys x dh: the second operand's other order)
 // S_0, S_1, O_0 and O_1 fill the 512 columns (128 each).  The halves of S_x, of 64 keys each, go round by themselves: while the rows make one
 // half's weights, the other's are multiplied with V and the next tile's logits take its place, so that the rows never wait for
-// a product.  (S_x whole, the rows waited for two products a tile: 28 heads, 4624 rows, 370 us.)
+// a product.  (S_x whole, the rows waited for two products a tile: 28 heads of 128, 4624 rows, 370 us instead of 265.)
 //
 // The key tiles of all pairs of all documents and K/V heads form one line, and every CTA (one per SM) takes an equal piece of it:
 // a piece may begin and end inside a pair, whose parts are then joined by a second kernel.  So a batch of documents of any lengths,
@@ -19,6 +19,12 @@
 // the first 64 keys that it sees; later weights are taken against it with no maximum of their own, since any m within the range of the
 // exponent gives the same result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x
 // and the row's sum are scaled: by the row's own thread, when the product before on O_x is complete.
+//
+// What bounds it: with heads of 128 the products (3300 clocks a pair of tiles, of which 1540 ns at 1.62 PFLOP/s are the products' own; 9472 rows of
+// four heads over 12 800 keys run at 1.22 PFLOP/s); with heads of 64, which halve the products and not the exponentials, the rows' arithmetic (14 heads,
+// 2664 x 12 800: 0.65 PFLOP/s; with a cap, whose polynomial costs seven multiply-adds more, 5600 clocks).  A bias adds 1250 clocks: sixteen 16-byte
+// reads of positions from the shared memory that the products read too, and three operations a weight (as packed pairs they took 40 us more
+// of 530).
 //
 // Warps 0-3 and 4-7: the rows of items 0 and 1; warp 8: TMA; warps 9 and 10: the products of items 0 and 1, each with waits of its
 // own (an issuing warp is held up while products run, so one warp's waits for both items lie open).  Every wait is bounded.  A row's 128 logits are read
