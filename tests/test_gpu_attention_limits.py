@@ -264,3 +264,11 @@ def test_more_pairs_of_tiles_than_processors(softcap, lens):
     # most rows are in no document: less work than their number says
     Q.check(q, k, v, 0.125, Q.offsets([5, 0, 90], 17), Q.offsets([5, 300, 90], 200), softcap=softcap)
     Q.check(q, k, v, 0.125, Q.offsets([3], 900), Q.offsets([1], 900), softcap=softcap)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hkv,dh", [(5, 64), (40, 64), (9, 128), (4, 64)])
+def test_evict_of_many_heads(dtype, Hkv, dh):
+    c = P.Cache([100, 31, 77, 500], Hkv, dh, 16, dtype, seed=Hkv, layers=2)
+    P.check_evict(c, 30, 2, 5)
+    P.check_evict(c, 90, 0, 40)
