@@ -20,9 +20,9 @@
 // exponent gives the same result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x
 // and the row's sum are scaled: by the row's own thread, when the product before on O_x is complete.
 //
-// What bounds it: with heads of 128 the products (3300 clocks a pair of tiles, of which 1540 ns at 1.62 PFLOP/s are the products' own; 9472 rows of
-// four heads over 12 800 keys run at 1.22 PFLOP/s); with heads of 64, which halve the products and not the exponentials, the rows' arithmetic (14 heads,
-// 2664 x 12 800: 0.65 PFLOP/s; with a cap, whose polynomial costs seven multiply-adds more, 5600 clocks).  A bias adds 1250 clocks: sixteen 16-byte
+// What bounds it: with heads of 128 the products (2.05 us per 128 keys of a pair, 1.54 at the 1.62 PFLOP/s of a large library product; 9472 rows
+// of four heads over 12 800 keys run at 1.22 PFLOP/s); with heads of 64, which halve the products and not the exponentials, the rows' arithmetic (14 heads,
+// 2664 x 12 800: 0.65 PFLOP/s, 3300 clocks per 128 keys; with a cap, whose polynomial costs seven multiply-adds more, 5600).  A bias adds 1250 clocks: sixteen 16-byte
 // reads of positions from the shared memory that the products read too, and three operations a weight (as packed pairs they took 40 us more
 // of 530).
 //
