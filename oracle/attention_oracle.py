@@ -28,7 +28,7 @@ def logits(q, k, scale, softcap=0.0, slope=0.0, far=None):
     err = err + 8 * STEP * np.abs(x)
     if far is not None:
         x = x - slope * far
-        err = err + 8 * STEP * slope * far + 2 * STEP * np.abs(x)
+        err = err + 8 * STEP * abs(slope) * far + 2 * STEP * np.abs(x)
     return x, err
 
 

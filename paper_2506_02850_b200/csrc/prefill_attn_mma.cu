@@ -584,7 +584,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 float sum;
 #pragma unroll 1
                 for (;;) {
-                    const float base = m == ninf ? 0.f : m;
+                    const float base = m == ninf || again ? 0.f : m;     // (again: a reference far from the logits would cost them digits)
                     uint32_t raw[2][32];
                     tmem_ld32_issue(t_s + half * 64, raw[0]);
                     tmem_ld32_issue(t_s + half * 64 + 32, raw[1]);
@@ -661,7 +661,8 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                         const float f = grow ? fast_exp2(m - mx) : 1.f;
                         if (grow) m = mx;
                         l *= f;
-                        const uint64_t less = grow ? pair(base - mx, base - mx) : 0ull;
+                        const float off = m == ninf ? 0.f : base - m;
+                        const uint64_t less = pair(off, off);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = add_pair(v[i], less);
                         if (j > 0 || half) {           // when the product before this one on O_x is complete

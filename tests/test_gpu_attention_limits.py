@@ -272,3 +272,62 @@ def test_evict_of_many_heads(dtype, Hkv, dh):
     c = P.Cache([100, 31, 77, 500], Hkv, dh, 16, dtype, seed=Hkv, layers=2)
     P.check_evict(c, 30, 2, 5)
     P.check_evict(c, 90, 0, 40)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("softcap", [0.0, 6.0])
+def test_slopes_of_either_sign_and_any_size(dtype, softcap):
+    g = Q.gen(41)
+    n = 500
+    q, k, v = Q.rows(g, 4, n, 64, dtype), Q.rows(g, 2, n, 64, dtype), Q.rows(g, 2, n, 64, dtype)
+    slopes = torch.tensor([-0.3, 1000.0, -2.0, 1e-6], device="cuda")
+    for kw in (dict(), dict(causal=False), dict(prefix_len=torch.tensor([333], dtype=torch.int32, device="cuda"))):
+        Q.check(q, k, v, 0.125, softcap=softcap, slopes=slopes, **kw)
+    c = P.Cache([300, 17], 2, 64, 32, dtype, seed=1)
+    one = torch.randn((2, 4, 64), generator=g, device="cuda").to(dtype)
+    got = B.metok_paged_attention(one, c.k[0], c.v[0], c.block_table, c.kv_len, 0.125, softcap=softcap, slopes=slopes)
+    torch.cuda.synchronize()
+    want = P.A.paged_attention(P.num(one), P.num(c.k[0]), P.num(c.v[0]), c.table_np, c.lens, 0.125, softcap, P.num(slopes))
+    assert (np.abs(P.num(got["out"]) - want["out"]) <= want["out_err"] + P.HALF[dtype] * np.abs(want["out"]) + 2.0 ** -16 * want["absv"]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_more_than_2_32_elements_apart(dtype):
+    """Every tensor of a call is a slice of one buffer whose rows lie 2^26 elements apart."""
+    n, far = 80, 1 << 26
+    room = torch.empty(n * far, dtype=dtype, device="cuda")
+    at = lambda col, heads: room[col:].as_strided((heads, n, 64), (64, far, 1))
+    g = Q.gen(51)
+    dense = [Q.rows(g, 4, n, 64, dtype), Q.rows(g, 2, n, 64, dtype), Q.rows(g, 2, n, 64, dtype)]
+    q, k, v, out = at(0, 4), at(512, 2), at(1024, 2), at(2048, 4)
+    for x, y in zip((q, k, v), dense):
+        x.copy_(y)
+    want = B.metok_prefill_attention(*dense, 0.125)["out"]
+    B.metok_prefill_attention(q, k, v, 0.125, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    # heads far apart, in the appended rows too
+    wide = lambda col: room[col:].as_strided((2, 70, 64), (20 * far, 128, 1))
+    kn, vn = wide(4096), wide(20480)
+    kd, vd = dense[1][:, :70].contiguous(), dense[2][:, :70].contiguous()
+    kn.copy_(kd)
+    vn.copy_(vd)
+    table = torch.arange(5, dtype=torch.int32, device="cuda").view(1, 5)
+    off, length = torch.tensor([0, 70], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pools = [[torch.zeros((5, 2, 16, 64), dtype=dtype, device="cuda") for _ in range(2)] for _ in range(2)]
+    for (a, b), (x, y) in zip(pools, ((kn, vn), (kd, vd))):
+        assert int(B.metok_paged_append(x, y, a, b, table, length, off)["new_len"]) == 70
+    assert torch.equal(pools[0][0], pools[1][0]) and torch.equal(pools[0][1], pools[1][1])
+
+
+def test_more_sequences_than_one_look():
+    """Hundreds of sequences of every length, with weights and a bias: where each lies in the line comes from the first kernel."""
+    lens = np.random.default_rng(8).integers(0, 200, 40).tolist() + [0, 900, 1, 0]
+    c = P.Cache(lens, 2, 64, 32, torch.bfloat16, seed=14)
+    P.check_attention(c, 6, bias=True)
+    c.kv_len[3] = -1
+    c.lens = list(c.lens)
+    out = torch.full((len(lens), 6, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    got = B.metok_paged_attention(torch.randn((len(lens), 6, 64), generator=c.g, device="cuda").bfloat16(), c.k[0], c.v[0], c.block_table, c.kv_len, 0.125, out=out)
+    torch.cuda.synchronize()
+    assert int(got["status"]) == -1 and (out[3] == 3).all() and torch.isfinite(out.float()).all()
