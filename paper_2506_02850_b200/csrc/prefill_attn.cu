@@ -6,7 +6,7 @@
 // running maximum and sum are shared by the sixteen threads of its ty by shuffles.  A row sees the keys [0, n) with n not falling
 // from row to row, so only tiles that reach beyond the first row's n are masked, by comparing indices.
 // R = 4 feeds the multiply-adds best (five of them per shared-memory wavefront, 1.8 with R = 1); R = 2 and 1 are for calls of few rows, and
-// those that leave most SMs without a tile, where a tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4, 12 with 1.
+// those that leave most SMs without a tile, where a tile's own latency counts: 132 rows of one head, capped: 21 us with R = 4, 12.8 with 1 (13.2 with its loops unrolled half as far).
 #include <algorithm>
 
 #include "launchers.h"
@@ -94,7 +94,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
+#pragma unroll (R == 1 ? 8 : 4)
         for (int e = 0; e < DH; e += 4) {
             float4 x[R], y[4];
 #pragma unroll
@@ -136,7 +136,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
             for (int c = 0; c < DH / 16; ++c) o[i][c] *= f;
         }
         __syncwarp();                                  // a row's weights are written and read by one half of a warp
-#pragma unroll 2
+#pragma unroll (R == 1 ? 4 : 2)
         for (int j = 0; j < kSN; j += 4) {
             float4 p[R];
 #pragma unroll
