@@ -442,7 +442,9 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   document of all rows (n_seq = 1).  Positions lie in [0, 2^24).
  *   Rows of q, k, v, out and lse outside every document are neither used nor written,
  *   whatever they hold.  Inside a document v has to be finite (below 2^100 for bf16): a row
- *   that a query does not see counts with weight 0.
+ *   that a query does not see counts with weight 0.  A NaN or +infinity among the logits that
+ *   a query sees makes its out and lse NaN; -infinity is a weight of 0 (a query that sees
+ *   nothing else gets what one that sees no key gets).
  *   status DEVICE int32: written METOK_OK; METOK_ERR_INVALID_ARG if seq_q or seq_k
  *   descends or leaves [0, n_q] / [0, n_k] (then no row is written); METOK_ERR_TIMEOUT.
  *
@@ -534,7 +536,8 @@ METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const vo
  *   with pos = `positions` ([n_seqs][S_cap]; NULL: the row's index).  If `mass` is
  *   given, mass[b][j] += (1/Hq) sum_h softmax(x)_j for every row j of b: the weight that
  *   metok_attention_scores takes the mean of, added up token by token.
- *   A sequence of no rows gets out = 0, lse = -infinity.
+ *   A sequence of no rows gets out = 0, lse = -infinity.  A NaN or +infinity among a head's
+ *   logits makes its out and lse, and the sequence's mass, NaN; -infinity is a weight of 0.
  *
  *   q, out  DEVICE [n_seqs][Hq][dh], strides in elements (multiples of 16 bytes, elements of
  *           a head contiguous); lse DEVICE float [n_seqs][Hq] or NULL; slopes DEVICE float [Hq] or NULL

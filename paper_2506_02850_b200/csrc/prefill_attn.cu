@@ -166,7 +166,7 @@ prompt_attn_simt_kernel(const PromptArgs a) {
         const int h = head_of(r);
         const long long row = d.q0 + in_doc;
         const bool part = a.splits > 1;
-        const float inv = part ? 1.f : l[i] > 0.f ? 1.f / l[i] : 0.f;
+        const float inv = part ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
         const long long at = ((long long)blockIdx.y * a.Hq + h) * a.n_q + row;
         float* out = part ? a.part_o + at * DH : reinterpret_cast<float*>(a.out) + h * a.out_head + row * a.out_row;
 #pragma unroll
@@ -201,13 +201,13 @@ prompt_join_kernel(const PromptArgs a) {
     for (int s = 0; s < a.splits; ++s) {
         const long long at = ((long long)s * a.Hq + h) * a.n_q + row;
         const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-        if (!(ml.y > 0.f)) continue;                   // a part of no keys has written no output
+        if (ml.y == 0.f) continue;                     // a part of no keys (M may be -infinity too); one of NaN counts
         const float f = exp2f(ml.x - M);
         L += f * ml.y;
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] += f * a.part_o[at * DH + lane * E + e];
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
     float* out = reinterpret_cast<float*>(a.out) + h * a.out_head + row * a.out_row;
 #pragma unroll
     for (int e = 0; e < E; ++e) out[lane * E + e] = acc[e] * inv;

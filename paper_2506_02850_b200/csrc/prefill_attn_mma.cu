@@ -100,16 +100,21 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 126] are held there, a NaN gives something that is no weight.  2^-125 is
-// taken off (rounded away beside what counts), so that a hidden key's weight is 0 and its V, however large, adds nothing.
+// 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 128] are held there.  2^-125 is taken off (rounded away beside what
+// counts), so that a hidden key's weight is 0 and its V, however large, adds nothing.  At 128 the exponent's bits are those of +infinity:
+// a NaN is held there too (a minimum takes the number of the two), and a sum of weights that is not finite is a row's sign of one.
 __device__ __forceinline__ uint64_t exp2_held_pair(uint64_t x) {
     float a, b;
     sm100::unpair(x, a, b);
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(-125.f));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(-125.f));
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(126.f));
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(126.f));
+    a = fmaxf(fminf(a, 128.f), -125.f);
+    b = fmaxf(fminf(b, 128.f), -125.f);
     return sm100::add_pair(sm100::exp2_fma_core(sm100::pair(a, b)), sm100::pair(-0x1p-125f, -0x1p-125f));
+}
+// The lesser of the two; NaN if one is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 // 16 registers of this thread's lane to 16 tensor-memory columns.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -610,8 +615,8 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                             for (int i = 0; i < 32; ++i) {
                                 float y0, y1;
                                 unpair(v[i], y0, y1);
-                                y0 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y0 * (2.f * kAttnLog2e), 80.f)));
-                                y1 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(fminf(y1 * (2.f * kAttnLog2e), 80.f)));
+                                y0 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(min_nan(y0 * (2.f * kAttnLog2e), 80.f)));
+                                y1 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(min_nan(y1 * (2.f * kAttnLog2e), 80.f)));
                                 v[i] = pair(y0, y1);
                             }
                         } else {
@@ -705,7 +710,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][half]));
             }
         }
-        if (m == ninf) l = 0.f;                        // no key seen
+        // A row that has seen no key has m = -infinity and l = 0.  Weights are finite where logits are, so a sum that is not comes of a NaN or
+        // +infinity among them: out and lse become NaN, here or in the join.
+        if (!(l < __int_as_float(0x7F800000))) l = __int_as_float(0x7FFFFFFF);
         if (my_n > 0 && ok && !mbar_wait(smem_u32(&o_bar[x]), (uint32_t)outs & 1u, abort_flag)) ok = false;
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_fence_after();
@@ -731,7 +738,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
         if (ok && whole) {
             // 32 columns at a time through shared memory, so that four lanes write 64 bytes of a row (each lane its own row: a store instruction
             // of 32 lines, 4 us a part)
-            const float scale = l > 0.f ? 1.f / l : 0.f;
+            const float scale = l == 0.f ? 0.f : 1.f / l;
             const long long to = mine ? (long long)my_head * a.out_head + row * a.out_row : -1;
             const uint32_t pad = smem_base + (2 + S::kStages) * S::kTile + (uint32_t)warp * S::kStagePad;
             long long dst[4];
@@ -766,7 +773,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
             }
         }
         if (ok) {
-            if (mine && !whole) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(l > 0.f ? m : ninf, l);
+            if (mine && !whole) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m, l);
             else if (mine && a.lse) a.lse[(long long)my_head * a.n_q + row] = kAttnLn2 * (m + log2f(l));
         }
         if (my_n > 0) {                                // O_x may be written again
@@ -845,7 +852,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (!(ml[u].y > 0.f)) continue;            // a part of no keys has written no output
+            if (ml[u].y == 0.f) continue;              // a part of no keys has written no output (one of NaN has)
             const float top = fmaxf(M, ml[u].x), f = sm100::fast_exp2(M - top), g = sm100::fast_exp2(ml[u].x - top);
             M = top;
             L = L * f + ml[u].y * g;
@@ -854,7 +861,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
                 acc[e] = make_float4(acc[e].x * f + o[u][e].x * g, acc[e].y * f + o[u][e].y * g, acc[e].z * f + o[u][e].z * g, acc[e].w * f + o[u][e].w * g);
         }
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (long long)head * a.out_head + row * a.out_row;
 #pragma unroll
     for (int e = 0; e < E; e += 2)

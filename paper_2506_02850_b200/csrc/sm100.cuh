@@ -263,7 +263,7 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
     unpair(x, a, b);
     return pair(fast_exp2(a), fast_exp2(b));
 }
-// (the arithmetic of exp2_fma_pair, for -125 <= x < 127)
+// (the arithmetic of exp2_fma_pair, for -125 <= x <= 128, where it gives +infinity)
 __device__ __forceinline__ uint64_t exp2_fma_core(uint64_t x) {
     const uint64_t t = add_pair(x, pair(12582912.0f, 12582912.0f));
     const uint64_t f = fma_pair(add_pair(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
