@@ -233,7 +233,8 @@ PromptPlan prompt_plan(const metok_attention_params* p) {
         pl.ctas = std::max(1LL, tiles * pl.head_chunks) * p->Hkv;
         // few rows: the keys are cut until every SM has work (documents of different lengths: several parts), no part shorter than two tiles
         const long long most = std::max(1LL, std::min((long long)p->n_k / (2 * kSN), 64LL));
-        pl.splits = (int)std::max(1LL, std::min(most, (p->n_seq == 1 ? kNumSMs : 4 * kNumSMs) / pl.ctas));
+        // (no rows: nothing to join)
+        pl.splits = p->n_q == 0 ? 1 : (int)std::max(1LL, std::min(most, (p->n_seq == 1 ? kNumSMs : 4 * kNumSMs) / pl.ctas));
         // the largest tile that the average document fills by three quarters and that leaves a CTA for every SM
         if (pl.ctas * most >= kNumSMs && 4LL * p->n_q * pl.heads_item >= 3LL * rows * p->n_seq) break;
     }
