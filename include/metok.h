@@ -537,7 +537,8 @@ METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const vo
  *   given, mass[b][j] += (1/Hq) sum_h softmax(x)_j for every row j of b: the weight that
  *   metok_attention_scores takes the mean of, added up token by token.
  *   A sequence of no rows gets out = 0, lse = -infinity.  A NaN or +infinity among a head's
- *   logits makes its out and lse, and the sequence's mass, NaN; -infinity is a weight of 0.
+ *   logits makes its out and lse, and the sequence's mass, NaN; -infinity is a weight of 0
+ *   (a head of nothing else gets out = 0, lse = -infinity).
  *
  *   q, out  DEVICE [n_seqs][Hq][dh], strides in elements (multiples of 16 bytes, elements of
  *           a head contiguous); lse DEVICE float [n_seqs][Hq] or NULL; slopes DEVICE float [Hq] or NULL

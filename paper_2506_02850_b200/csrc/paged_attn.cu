@@ -806,7 +806,7 @@ paged_join_kernel(const PagedAttnArgs a) {
                 acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
                 L += f * ml.y;
             }
-            const float inv = 1.f / L;
+            const float inv = L == 0.f ? 0.f : 1.f / L;                  // 0: every logit is -infinity
             from_float(out[col * 4], acc.x * inv);
             from_float(out[col * 4 + 1], acc.y * inv);
             from_float(out[col * 4 + 2], acc.z * inv);
@@ -868,7 +868,7 @@ paged_join_kernel(const PagedAttnArgs a) {
             L = L * sm100::fast_exp2(M - top) + l2 * sm100::fast_exp2(m2 - top);
             M = top;
         }
-        if (h < a.Hq && part == 0) s_lse[h] = M + log2f(L);
+        if (h < a.Hq && part == 0) s_lse[h] = L == 0.f ? 0.f : M + log2f(L);       // (every logit -infinity: weights of 0)
     }
     __syncthreads();
     if (row0 + tid >= len) return;

@@ -154,3 +154,20 @@ def test_nothing_but_minus_infinity(dtype):
         q[0, :, 3], q[1, :, 3] = -1.0, 1.0
         out, lse = call(q, k, v, 0.125)
         assert (out[0] == 0).all() and (lse[0] == -INF).all() and np.isnan(out[1]).all() and np.isnan(lse[1]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_cache_of_nothing_but_minus_infinity(dtype):
+    """A token all of whose logits are -infinity is as one of an empty cache; the other sequences are served."""
+    c = P.Cache([700, 33], 1, 64, 16, dtype, seed=5)
+    g = Q.gen(9)
+    q = Q.rows(g, 2, 4, 64, dtype)
+    q[0, :, 3] = -1.0
+    q[1, :, 3] = 0.0
+    k = c.k[0].clone()
+    k[[int(p) for p in c.table_np[0] if p < c.n_pages], :, :, 3] = INF
+    mass = c.mass[0].clone()
+    got = B.metok_paged_attention(q, k, c.v[0], c.block_table, c.kv_len, 0.125, mass=mass, with_lse=True)
+    torch.cuda.synchronize()
+    assert (got["out"][0] == 0).all() and (got["lse"][0] == -INF).all() and torch.equal(mass[0], c.mass[0, 0])
+    assert torch.isfinite(got["out"][1].float()).all() and torch.isfinite(got["lse"][1]).all() and (mass[1, :33] > c.mass[0, 1, :33]).any()
