@@ -501,10 +501,11 @@ METOK_API int metok_prefill_attention(int dtype, const metok_attention_params* p
  *   overlap it.
  *   No two rows of a call may go to the same place (pages that sequences share hold only rows
  *   that are there already), and the new rows are not in the pools.
- *   A sequence without room for its rows, with a length outside [0, S_cap], new_offsets that descend or
+ *   A sequence without room for its rows, with a length outside [0, S_cap], new_offsets that
  *   leave [0, n_new], or a page outside [0, n_pages) among those to be written, is reported
  *   by status = METOK_ERR_INVALID_ARG and new_len[b] = kv_len[b]; its rows behind kv_len are
- *   then unspecified, the other sequences are served as usual.
+ *   then unspecified, the other sequences are served as usual.  Where new_offsets descend
+ *   anywhere no row is written, and every sequence is reported so.
  *   DEVICE int32 / float arrays are 4-byte aligned; pools and new rows 16-byte aligned.
  *   Errors: INVALID_ARG (null or misaligned pointers, sizes < 1 (n_new may be 0), strides,
  *   pos_new without positions, mass_new without mass, n_new != n_seqs without new_offsets,

@@ -435,7 +435,8 @@ def metok_paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pool: torch.T
     layer's paged cache.  `new_offsets` (int32 [n_seqs + 1]) deals them out; without it every sequence gets one.  `positions` and `mass`
     ([n_seqs, max_pages * page_size]) get `pos_new` (default: counted on from the last row's, which after an eviction need not be the
     newest) and `mass_new` (default: 0).
-    Returns "new_len" (given, or new) and "status" (0, or -1 where a sequence had no room or a bad page)."""
+    Returns "new_len" (given, or new) and "status" (0, or -1 where a sequence had no room or a bad page: its length stays; none is
+    extended where `new_offsets` descend)."""
     res = _calls().paged_append(k_new, v_new, k_pool, v_pool, block_table, kv_len, new_offsets, positions, pos_new, mass, mass_new,
                                 new_len)
     if type(res) is int:

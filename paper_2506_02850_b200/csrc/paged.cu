@@ -26,8 +26,12 @@ struct AppendArgs {
     int32_t *new_len, *status;
 };
 
-// The sequence of new row i: the number of offsets[1 .. n) that are <= i.  Whole warp, 32-ary search; with offsets that
-// descend the answer is some sequence, which the caller finds not to hold the row.
+// Where the new rows of sequences lie, as given by ascending offsets; with offsets that descend anywhere nothing is appended, as a search
+// among them would find some sequences' rows and not others'.
+struct NewRows {
+    int b, lo, hi, len;                                // a sequence, its new rows, and the rows that it holds
+};
+// The sequence of new row i, one of more than 32: the number of offsets[1 .. n) that are <= i.  Whole warp, 32-ary search.
 __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ offsets, int n, int i, int lane) {
     int lo = 0, left = n - 1;                          // it lies in [lo, lo + left]
     while (left > 0) {
@@ -45,11 +49,30 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
 paged_append_kernel(const AppendArgs a) {
     grid_dep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, S_cap = a.d.S_cap();
+    const long long item = blockIdx.x ? (long long)(blockIdx.x - 1) * kAppendWarps + warp : 0;
+    const int i = (int)(item / a.parts), part = (int)(item - (long long)i * a.parts);
+    // Up to 32 sequences with offsets: every warp looks at all of them at once, a lane each.  Beyond that the CTA looks whether any descend,
+    // and the warps search.  (Steps in a graph, with the check and before there was one: 16 sequences 3.1 and 3.3 us, 40 sequences 4.1 and 3.8;
+    // 300 sequences of 200 rows 49.5 and 47.6.)
+    const bool few = a.offsets && a.d.n_seqs <= 32;
+    NewRows r = {i, i, i + 1, 0}, mine = {lane, 0, 0, 0};
+    bool none = false;
+    if (few) {
+        if (lane < a.d.n_seqs) mine = {lane, a.offsets[lane], a.offsets[lane + 1], a.kv_len[lane]};
+        none = __any_sync(0xFFFFFFFFu, mine.hi < mine.lo);
+    } else if (a.offsets) {
+        int down = 0;
+        for (int s = threadIdx.x; s < a.d.n_seqs; s += kAppendWarps * 32) down |= a.offsets[s + 1] < a.offsets[s];
+        none = __syncthreads_or(down);
+    }
+    auto of_few = [&](int b) { return NewRows{b, __shfl_sync(0xFFFFFFFFu, mine.lo, b), __shfl_sync(0xFFFFFFFFu, mine.hi, b), __shfl_sync(0xFFFFFFFFu, mine.len, b)}; };
+    auto of_many = [&](int b) { return NewRows{b, a.offsets ? a.offsets[b] : b, a.offsets ? a.offsets[b + 1] : b + 1, a.kv_len[b]}; };
     if (blockIdx.x == 0) {                             // the first CTA checks the sequences and writes their lengths
         int bad = 0;
         for (int b = warp; b < a.d.n_seqs; b += kAppendWarps) {
-            const int len = a.kv_len[b], lo = a.offsets ? a.offsets[b] : b, hi = a.offsets ? a.offsets[b + 1] : b + 1;
-            bool ok = lo >= 0 && hi >= lo && hi <= a.n_new && len >= 0 && len <= S_cap && hi - lo <= S_cap - len;
+            r = few ? of_few(b) : of_many(b);
+            const int len = r.len, lo = r.lo, hi = r.hi;
+            bool ok = !none && lo >= 0 && hi <= a.n_new && len >= 0 && len <= S_cap && hi - lo <= S_cap - len;
             if (ok && hi > lo) {
                 const int p1 = (len + hi - lo - 1) >> a.d.page_shift;
                 bool there = true;
@@ -66,11 +89,10 @@ paged_append_kernel(const AppendArgs a) {
         if (threadIdx.x == 0) *a.status = bad ? METOK_ERR_INVALID_ARG : METOK_OK;
         return;
     }
-    const long long item = (long long)(blockIdx.x - 1) * kAppendWarps + warp;
-    const int i = (int)(item / a.parts), part = (int)(item - (long long)i * a.parts);
-    if (i >= a.n_new) return;
-    const int b = a.offsets ? sequence_of(a.offsets, a.d.n_seqs, i, lane) : i;
-    const int lo = a.offsets ? a.offsets[b] : b, hi = a.offsets ? a.offsets[b + 1] : b + 1, len = a.kv_len[b];
+    if (none || i >= a.n_new) return;
+    if (few) r = of_few(__popc(__ballot_sync(0xFFFFFFFFu, lane < a.d.n_seqs - 1 && mine.hi <= i)));
+    else r = of_many(a.offsets ? sequence_of(a.offsets, a.d.n_seqs, i, lane) : i);
+    const int b = r.b, lo = r.lo, hi = r.hi, len = r.len;
     // the row is the sequence's, and the sequence has room
     if (i < lo || i >= hi || lo < 0 || hi > a.n_new || len < 0 || len > S_cap || hi - lo > S_cap - len) return;
     const int row = len + (i - lo);
