@@ -441,7 +441,7 @@ METOK_API int metok_kv_compact(void* const* k_layers, void* const* v_layers, int
  *   aligned; all but q, k, v, out may be NULL.  seq_q and seq_k are both NULL for one
  *   document of all rows (n_seq = 1).  Positions lie in [0, 2^24).
  *   Rows of q, k, v, out and lse outside every document are neither used nor written,
- *   whatever they hold.  Inside a document v has to be finite (below 2^100 for bf16): a row
+ *   whatever they hold.  Inside a document |v| has to be below 2^100: a row
  *   that a query does not see counts with weight 0.  A NaN or +infinity among the logits that
  *   a query sees makes its out and lse NaN; -infinity is a weight of 0 (a query that sees
  *   nothing else gets what one that sees no key gets).
@@ -544,6 +544,7 @@ METOK_API int metok_paged_append(int dtype, const metok_paged_cache* c, const vo
  *   q, out  DEVICE [n_seqs][Hq][dh], strides in elements (multiples of 16 bytes, elements of
  *           a head contiguous); lse DEVICE float [n_seqs][Hq] or NULL; slopes DEVICE float [Hq] or NULL
  *   Rows of a page behind the sequence's last row are not used, whatever they hold.
+ *   |V| of the sequence's rows has to be below 2^100: sums of up to 2^24 weights times it are fp32.
  *   A sequence whose length or pages are out of range is reported by status =
  *   METOK_ERR_INVALID_ARG and its out, lse and mass are left as they were.
  *   The work is cut along the caches' lengths into equal pieces for all SMs and joined

@@ -17,7 +17,7 @@
 //
 // Key tiles of a pair are taken from the last one down (a bias makes the nearest ones the largest).  A row's reference m is the maximum of
 // the first 64 keys that it sees; later weights are taken against it with no maximum of their own, since any m within the range of the
-// exponent gives the same result.  Where the sum of 64 weights leaves that range they are made again against their own maximum, and O_x
+// exponent gives the same result.  Where a row's sum leaves that range 64 weights are made again against a higher reference, and O_x
 // and the row's sum are scaled: by the row's own thread, when the product before on O_x is complete.
 //
 // What bounds it: with heads of 128 the products (2.05 us per 128 keys of a pair, 1.54 at the 1.62 PFLOP/s of a large library product; 9472 rows
@@ -40,8 +40,10 @@ namespace metok {
 namespace {
 
 constexpr int kM = 128, kN = 128, kThreads = 352;
-// Sum of 64 weights beyond which a row's reference grows; by how many octaves a logit has passed it then (one of 64 has by 18).  Weights stay
-// below 2^24, so V may be as large as 2^100, and the reference never lies above the maximum, so what underflows is below 2^-125 of it.
+// A row's reference grows where 64 weights add up to kMost (one of them has passed it by 18 octaves then), and where the row's sum has: by kGrow
+// octaves, or to the maximum of the 64 keys at hand where that is higher.  So the row's sum, looked at before every tile, stays below 2^26 however many keys
+// there are, and that of weight * V within fp32 for V up to 2^100.  With at most 2^24 keys, a sum of 2^24 takes a weight of 1 or more: the reference is at most 16
+// octaves above the maximum, and what underflows is below 2^-109 of it.
 constexpr float kMost = 0x1p24f, kGrow = 16.f;
 constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
@@ -577,6 +579,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 named_bar_sync(1 + x, 128);
             }
             const bool masked = k0 + kN > sure;
+            const bool full = __any_sync(0xFFFFFFFFu, keys > 0 && l >= kMost);       // (looked up while the logits are on their way)
 #pragma unroll 1                                       // (one copy of the code: the instruction cache is short)
             for (int half = 0; half < 2; ++half) {     // 64 keys
                 if (ok && !mbar_wait(smem_u32(&s_bar[x][half]), (uint32_t)seen & 1u, abort_flag)) ok = false;
@@ -584,7 +587,7 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                 if (!ok) continue;                     // (keeps meeting the item's other warps where they meet)
                 tc_fence_after();
                 // whether a reference is wanted: at the first keys that a row sees, and where the weights came out too large for the one there is
-                bool check = __any_sync(0xFFFFFFFFu, m == ninf && keys > k0 + half * 64), again = false;
+                bool check = full || __any_sync(0xFFFFFFFFu, m == ninf && keys > k0 + half * 64), again = false;
                 uint32_t p[32];
                 float sum;
 #pragma unroll 1
@@ -662,9 +665,9 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                             top[i & 3] = fmaxf(top[i & 3], fmaxf(v0, v1));
                         }
                         const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) + base;
-                        const bool grow = keys > 0 && (again ? mx > m + kGrow : m == ninf && mx > ninf);
-                        const float f = grow ? fast_exp2(m - mx) : 1.f;
-                        if (grow) m = mx;
+                        const bool grow = keys > 0 && (again ? mx > m + kGrow : m == ninf ? mx > ninf : l >= kMost);
+                        const float higher = fmaxf(mx, m + kGrow), f = grow ? fast_exp2(m - higher) : 1.f;
+                        if (grow) m = higher;
                         l *= f;
                         const float off = m == ninf ? 0.f : base - m;
                         const uint64_t less = pair(off, off);
@@ -835,6 +838,9 @@ prompt_cut_join_kernel(const PromptArgs a) {
     const float ninf = __int_as_float(0xFF800000);
     constexpr int E = kCutPieces;
     const int piece = (blockIdx.y / kCutBlocks * 8 + warp) * E;
+    // A part's sum is below 2^26 and there are fewer than 2^8 of them: with a 2^8th of each, their sum * V is in range too.
+    constexpr float kLess = 0x1p-8f;
+    static_assert(kNumSMs < 256);
     float M = ninf, L = 0.f;
     float4 acc[E];
 #pragma unroll
@@ -853,7 +859,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (ml[u].y == 0.f) continue;              // a part of no keys has written no output (one of NaN has)
-            const float top = fmaxf(M, ml[u].x), f = sm100::fast_exp2(M - top), g = sm100::fast_exp2(ml[u].x - top);
+            const float top = fmaxf(M, ml[u].x), f = sm100::fast_exp2(M - top), g = sm100::fast_exp2(ml[u].x - top) * kLess;
             M = top;
             L = L * f + ml[u].y * g;
 #pragma unroll
@@ -867,7 +873,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
     for (int e = 0; e < E; e += 2)
         reinterpret_cast<uint4*>(out)[(piece + e) / 2] = make_uint4(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv),
                                                                        pack_bf16(acc[e + 1].x * inv, acc[e + 1].y * inv), pack_bf16(acc[e + 1].z * inv, acc[e + 1].w * inv));
-    if (piece == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L));
+    if (piece == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L * (1.f / kLess)));
 }
 
 template <int DH, bool kCap, bool kBias>
