@@ -45,6 +45,10 @@ constexpr int kM = 128, kN = 128, kThreads = 352;
 // there are, and that of weight * V within fp32 for V up to 2^100.  With at most 2^24 keys, a sum of 2^24 takes a weight of 1 or more: the reference is at most 16
 // octaves above the maximum, and what underflows is below 2^-109 of it.
 constexpr float kMost = 0x1p24f, kGrow = 16.f;
+// Caps above this have a kernel of their own (kCap = 2).  1 - 2 / (1 + e^2y) is off by some 2^-21 of 1 however small y is, so a capped logit
+// by 2^-21 of the cap: up to here at most 2^-13, a thirty-second of what a weight's rounding to bf16 takes.  Beyond, rows that hold a logit past the cap
+// take the polynomial for their others.  (With that in all capped calls: 4624 rows of 28 heads, cap 20, 293 -> 340 us, cap 50 242 -> 252.)
+constexpr float kWideCap = 256.f;
 constexpr __device__ bool kShare(int i) { return (i & 3) == 3; }     // pairs of exponentials that go to the FMA pipe
 
 template <int DH>
@@ -221,7 +225,7 @@ struct Cut {
     int q0, g, Lq, i0[2], h0[2], rows[2];
 };
 
-template <int DH, bool kCap, bool kBias>
+template <int DH, int kCap, bool kBias>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps) {
     using namespace sm100;
@@ -604,7 +608,15 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                     const uint64_t low = pair(-base, -base);
                     if constexpr (kCap) {
                         // y = product * scale / cap.  Up to |y| = 1 tanh(y) = y P(y^2), P the polynomial of degree 6 of least largest error (2e-8; 1e-7 in
-                        // fp32), with the cap in its coefficients; beyond, 1 - 2 / (1 + e^2y), of which every part costs the special-function unit a step.
+                        // fp32), with the cap in its coefficients; where a warp has one beyond, 1 - 2 / (1 + e^2y), of which every part costs the
+                        // special-function unit a step.
+                        auto near = [&](uint64_t y) {
+                            const uint64_t u = mul_pair(y, y);
+                            uint64_t t = pair(a.cap_poly[6], a.cap_poly[6]);
+#pragma unroll
+                            for (int c = 5; c >= 0; --c) t = fma_pair(t, u, pair(a.cap_poly[c], a.cap_poly[c]));
+                            return fma_pair(y, t, low);
+                        };
                         float most = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
@@ -616,21 +628,17 @@ prompt_attn_mma_kernel(const PromptArgs a, const __grid_constant__ MmaMaps maps)
                         if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {
-                                float y0, y1;
+                                float y0, y1, near0, near1;
                                 unpair(v[i], y0, y1);
+                                const bool far0 = !(fabsf(y0) <= 1.f), far1 = !(fabsf(y1) <= 1.f);
+                                if constexpr (kCap == 2) unpair(near(v[i]), near0, near1);
                                 y0 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(min_nan(y0 * (2.f * kAttnLog2e), 80.f)));
                                 y1 = (a.cap_log2 - base) - __fdividef(2.f * a.cap_log2, 1.f + fast_exp2(min_nan(y1 * (2.f * kAttnLog2e), 80.f)));
-                                v[i] = pair(y0, y1);
+                                v[i] = kCap == 1 ? pair(y0, y1) : pair(far0 ? y0 : near0, far1 ? y1 : near1);
                             }
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const uint64_t u = mul_pair(v[i], v[i]);
-                                uint64_t t = pair(a.cap_poly[6], a.cap_poly[6]);
-#pragma unroll
-                                for (int c = 5; c >= 0; --c) t = fma_pair(t, u, pair(a.cap_poly[c], a.cap_poly[c]));
-                                v[i] = fma_pair(v[i], t, low);
-                            }
+                            for (int i = 0; i < 32; ++i) v[i] = near(v[i]);
                         }
                     } else {
 #pragma unroll
@@ -876,7 +884,7 @@ prompt_cut_join_kernel(const PromptArgs a) {
     if (piece == 0 && a.lse) a.lse[(long long)head * a.n_q + row] = kAttnLn2 * (M + log2f(L * (1.f / kLess)));
 }
 
-template <int DH, bool kCap, bool kBias>
+template <int DH, int kCap, bool kBias>
 int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
     auto kern = prompt_attn_mma_kernel<DH, kCap, kBias>;
     METOK_ALLOW_SMEM(kern, MmaShape<DH>::kSmem);
@@ -894,8 +902,9 @@ int launch(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
 }
 template <int DH>
 int launch_dh(const PromptArgs& a, const MmaMaps& maps, cudaStream_t st) {
-    if (a.cap_log2 > 0.f) return a.slopes ? launch<DH, true, true>(a, maps, st) : launch<DH, true, false>(a, maps, st);
-    return a.slopes ? launch<DH, false, true>(a, maps, st) : launch<DH, false, false>(a, maps, st);
+    if (a.cap_log2 > kWideCap * kAttnLog2e) return a.slopes ? launch<DH, 2, true>(a, maps, st) : launch<DH, 2, false>(a, maps, st);
+    if (a.cap_log2 > 0.f) return a.slopes ? launch<DH, 1, true>(a, maps, st) : launch<DH, 1, false>(a, maps, st);
+    return a.slopes ? launch<DH, 0, true>(a, maps, st) : launch<DH, 0, false>(a, maps, st);
 }
 
 }  // namespace
