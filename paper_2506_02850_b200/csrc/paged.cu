@@ -143,9 +143,12 @@ struct EvictArgs {
 };
 
 // Whether a sequence may be touched: its length and pages are in range, no page is its own twice or another's.  A bit per page in
-// shared memory marks the sequence's own; then every other sequence's pages are looked up.  Beyond so many pages (32 KB of bits) or
-// sequences a kernel before it claims the pages (6 us with its clearing; this costs next to nothing for few).
-constexpr int kEvictBitPages = 1 << 18, kEvictBitSeqs = 256;
+// shared memory marks the sequence's own; then every other sequence's pages are looked up, in every layer.  Beyond so many pages (32 KB of
+// bits) or sequences a kernel before it claims the pages for all layers, which with its clearing costs two launches more.  Calls in a graph, 80
+// pages a sequence, this way and by claims: 6 layers of 12 sequences 11.3 and 16.2 us, of 24 11.7 and 13.2, of 48 22.8 and 20.9, of 256 149
+// and 90; 28 layers of 12 28.7 and 30.6, of 24 46.9 and 43.7, of 256 641 and 381; one layer of 24 11.2 and 13.0, of 48 12.1 and 13.0, of 256
+// 33 and 21.
+constexpr int kEvictBitPages = 1 << 18, kEvictBitSeqs = 32;
 __device__ __forceinline__ bool evict_sound(const EvictArgs& a, int b, uint32_t* s_bits) {
     const int tid = threadIdx.x, nthr = blockDim.x, len = a.kv_len[b], page_rows = 1 << a.d.page_shift;
     if (len < 0 || len > a.d.S_cap()) return false;    // uniform
