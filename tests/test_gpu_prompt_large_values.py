@@ -48,3 +48,15 @@ def test_parts_of_cut_keys_stay_in_range(heads, n_q, n):
     dt = torch.bfloat16
     for low in ((i // 64) % 2 == 0, (i // 128) % 8 == 7):
         Q.check(queries(heads, n_q, dt), keys(n, low, 12.375, dt), values(n, Q.gen(4)), 0.125, causal=False)
+
+
+@pytest.mark.parametrize("dtype", Q.TYPES)
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n_q,n_k", [(400, 400), (7, 5000)])
+def test_outputs_of_large_logits(dtype, dh, n_q, n_k):
+    """Logits of hundreds: nearly all weight on one row, found anywhere among the keys."""
+    g = Q.gen(13)
+    q, k, v = Q.rows(g, 2, n_q, dh, dtype, 60.0), Q.rows(g, 1, n_k, dh, dtype), Q.rows(g, 1, n_k, dh, dtype)
+    Q.check(q, k, v, 1.0)
+    Q.check(q, k, v, 1.0, causal=False)
+    Q.check(q, k, v, 1.0, softcap=300.0)
