@@ -565,8 +565,8 @@ METOK_API int metok_paged_attention(int dtype, const metok_paged_cache* c, const
  *
  *   For every layer l and sequence b with more than `budget` rows, the `budget` rows that
  *   rank highest stay: first the protected ones, whose position is < n_sink or
- *   > (position of the last row) - n_recent, then by mass (a NaN ranks highest), equal
- *   ones by lower row.  new_len[b] = min(kv_len[b], budget).  Kept rows below new_len stay
+ *   > (position of the last row) - n_recent, then the others by mass (a NaN ranks highest);
+ *   of protected ones, whatever their mass, and of equal ones the lower row.  new_len[b] = min(kv_len[b], budget).  Kept rows below new_len stay
  *   where they are; the kept rows behind it, in ascending order, go to the places of the
  *   rows that leave, in ascending order: no row moves that need not.  So the rows are no
  *   longer in the order of their positions, which is why positions are wanted here and

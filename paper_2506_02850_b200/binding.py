@@ -461,7 +461,7 @@ def metok_paged_evict(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch
                       mass: torch.Tensor, positions: torch.Tensor, budget: int, n_sink: int, n_recent: int,
                       new_len: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
     """Sequences of more than `budget` rows keep, in every layer, those whose position is among the first `n_sink` or the newest
-    `n_recent`, and of the others those with the most `mass`; K, V, `mass` and `positions` ([L, n_seqs, max_pages * page_size]) are moved
+    `n_recent` (the lower rows, if these alone are more), and of the others those with the most `mass`; K, V, `mass` and `positions` ([L, n_seqs, max_pages * page_size]) are moved
     in place, kept rows behind the new length into the places of rows that leave.  Returns "keep_idx" (int32 [L, n_seqs, budget]: the
     row that each row now holds, -1 behind the new length), "new_len" and "status" (0, or -1 where a sequence was left as it is)."""
     res = _calls().paged_evict(k_layers, v_layers, block_table, kv_len, mass, positions, budget, n_sink, n_recent, new_len)

@@ -9,8 +9,8 @@ namespace {
 // ---- append -------------------------------------------------------------------------
 // A warp copies kAppendChunks 16-byte chunks per lane of one new row (all heads, K then V): a row of 4 heads of 128 bf16 is
 // one warp's work, one of 40 fp32 heads that of twenty, so that a step of few rows still fills the SMs.  Reads and writes are
-// contiguous pieces of dh elements; what bounds a long call is HBM (27 000 rows of 4 heads of 128: 43 us, 5.1 TB/s), a step's call its launch
-// and three round trips (the row's sequence, its length and page, the copy): 6 us.
+// contiguous pieces of dh elements; what bounds a long call is HBM (53 650 rows of 4 heads of 128: 42 us, 5.2 TB/s), a step's call its launch
+// and three round trips (the offsets and lengths, the page, the copy): 6 us.
 constexpr int kAppendWarps = 8, kAppendChunks = 4;
 
 struct AppendArgs {
@@ -128,7 +128,8 @@ paged_append_kernel(const AppendArgs a) {
 // Two kernels.  select: a CTA per (layer, sequence) checks the sequence's pages against those of all others, finds the rows that
 // stay, pairs the holes below the new length with the kept rows behind it, and moves their positions and mass.  move: K and V
 // rows of the pairs, and the call's status.  Sources lie at or beyond the new length and places below it, so no order is needed
-// between them.  28 layers of 4 sequences of 1184 to 4736 rows, 1263 kept: 14 us and 61 us, the moves of rows of 256 bytes at 5.6 TB/s.
+// between them.  28 layers of 4 sequences of 1734 to 4736 rows, 1263 kept: 85 us, in which rows of 256 bytes move at 5.6 TB/s (from cold
+// caches, one kernel after the other: 19 us and 64 us).
 struct EvictArgs {
     PagedDims d;
     int L, budget, n_sink, n_recent;
@@ -512,7 +513,7 @@ extern "C" int metok_paged_evict(int dtype, const metok_paged_cache* c, void* co
     METOK_LAUNCH_CHECK();
     // A CTA per 32 KB of the most pairs that a problem can have (the rows behind the new length, or the places below it): how many there
     // are is known on the device alone, and what has no work ends at once.  (A fixed share of the SMs per problem left them idle beside the
-    // longest: 28 layers of 4 sequences of 1184 to 4736 rows 113 us the call, 1263 kept.)
+    // longest: 28 layers of 4 sequences of 1734 to 4736 rows 113 us the call, 1263 kept.)
     const long long most = (long long)ceil_div(std::min(budget, d.S_cap() - budget), kMoveThreads / d.row_chunks) * ceil_div(2 * d.Hkv, kMoveHeads);
     const long long blocks = std::max(1LL, std::min(most, (long long)kMoveMostCtas / (std::min(L, kEvictPtrLayers) * d.n_seqs)));
     for (int l0 = 0; l0 < L; l0 += kEvictPtrLayers) {

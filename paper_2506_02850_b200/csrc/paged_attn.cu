@@ -13,7 +13,7 @@
 //   bf16: a warp takes 16 rows of a tile.  x^T = K Q^T (rows x heads) and o^T += V^T P^T by mma.sync m16n8k16: eight heads
 //     are a whole side of the product, where the tensor memory path would pad them to 128 (the products are a few per cent of
 //     either's rate).  P is split into two bf16 parts, so its rounding is 2^-17: fp32-like sums at no cost in bytes.
-//     48 sequences of up to 9001 rows, 28 / 4 heads of 128, capped: 97 us, 5.7 TB/s; one of 18 496 rows with weights 15.5 us, of which its 38 MB
+//     48 sequences of up to 9001 rows, 28 / 4 heads of 128, capped: 99.7 us, 5.6 TB/s; one of 18 496 rows with weights 17.5 us, of which its 38 MB
 //     are 5.8: two launches, filling the ring and the joins' chain of loads are the rest.
 //   fp32: eight lanes share a row, four rows at a time; the lanes' partial dot products of several heads are reduced and
 //     dealt out in one butterfly.
