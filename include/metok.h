@@ -26,7 +26,7 @@
  *     Outputs, including device-resident counts, are valid once the caller has
  *     synchronised with the stream.
  *   - Inputs are never written, except the K/V buffers of metok_kv_compact and what
- *     (6) to (8) say of a paged cache.
+ *     (6) to (8) and (10) say of a paged cache, and (9) of rows turned in place.
  *   - dtype: METOK_F32 (float) or METOK_BF16 (bfloat16).  bf16 paths accumulate
  *     in fp32; selections compare fp32 scores; ties always go to the lower index.
  *   - Ratios are doubles; every count derived from a ratio is
@@ -59,6 +59,7 @@ extern "C" {
 
 #define METOK_F32  0
 #define METOK_BF16 1
+#define METOK_Q4   4   /* a paged cache held in 4 bits: see (10) */
 
 #define METOK_SIM_FLATTEN  0   /* Frobenius inner product of the N x d frame matrices */
 #define METOK_SIM_MEANPOOL 1   /* average the N tokens first, then cosine in R^d      */
@@ -577,6 +578,7 @@ METOK_API int metok_paged_attention(int dtype, const metok_paged_cache* c, const
  *     K and V of every layer, positions and mass [L][n_seqs][S_cap] are moved;
  *     mass of the rows from new_len[b] to kv_len[b]-1 is set to 0.
  *
+ *   dtype may be METOK_Q4: pools of (10), whose rows move as they are held.
  *   k_layers, v_layers HOST arrays of L DEVICE pools, no two of them overlapping (c->k_pool
  *   and v_pool are not read); all layers have the same table and lengths.  new_len must not
  *   overlap kv_len.
@@ -591,6 +593,94 @@ METOK_API size_t metok_paged_evict_workspace_bytes(const metok_paged_cache* c, i
 METOK_API int metok_paged_evict(int dtype, const metok_paged_cache* c, void* const* k_layers, void* const* v_layers, int L,
                         int budget, int n_sink, int n_recent, int32_t* positions, float* mass,
                         int32_t* keep_idx, int32_t* new_len, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * (9) Norms and rotary positions of the heads of Q and K, in one pass: what a layer
+ *     does between its projections and (5) to (7).  Video rows have positions of several
+ *     axes (time, height, width), of which a pruned prompt's rows keep their own.
+ *
+ *   For row r and every head of q and k, with x the head's dh elements,
+ *     y = x * w / sqrt(mean(x^2) + eps)       if norm (w: q_weight or k_weight; NULL: 1), else y = x;
+ *     t_i = positions[pair_axis[i]][r] * inv_freq[i],   i = 0 .. rotary_dim/2 - 1,
+ *     (y_a, y_b) = (y_a cos t_i - y_b sin t_i,  y_b cos t_i + y_a sin t_i)
+ *   where pair i is (a, b) = (i, i + rotary_dim/2), or (2 i, 2 i + 1) if `interleaved`.  Elements
+ *   from rotary_dim on do not turn.  fp32 (the sum of squares, too: |x| below 2^60) and rounded
+ *   once; the angles are reduced in 64 bits, so positions may be as large as an int32.
+ *
+ *   q, q_out [Hq][n][dh], k, k_out [Hkv][n][dh] of `dtype` with the given strides in ELEMENTS
+ *   between heads and between rows (multiples of 16 bytes, at least dh where there are several);
+ *   DEVICE, 16-byte aligned.  q_out may be q, and k_out k, with the same strides; else outputs
+ *   overlap no input, nor each other.  Hkv = 0: no k (k and k_out are not read).
+ *   q_weight, k_weight DEVICE float [dh] or NULL; inv_freq DEVICE float [rotary_dim/2];
+ *   positions DEVICE int32 [n_axes][n] (NULL with n_axes = 1: the row's index); 4-byte aligned.
+ *   pair_axis HOST int32 [rotary_dim/2], or NULL: all pairs go by axis 0.
+ *   Errors: INVALID_ARG (null or misaligned pointers, n < 0, Hq < 1, Hkv < 0, strides, outputs that
+ *   overlap, n_axes outside 1 .. 4, pair_axis outside [0, n_axes), rotary_dim outside [0, dh] or no
+ *   multiple of 16, eps negative or not finite, no positions with n_axes > 1); UNSUPPORTED (dh other
+ *   than 64 or 128, more than 2^31 - 1 pieces of work).
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    const void* q;
+    const void* k;
+    void* q_out;
+    void* k_out;
+    int64_t q_head, q_row, k_head, k_row, qo_head, qo_row, ko_head, ko_row;
+    int Hq, Hkv, dh, n, rotary_dim, interleaved, n_axes, norm;
+    const float* q_weight;
+    const float* k_weight;
+    const float* inv_freq;
+    const int32_t* positions;
+    const int32_t* pair_axis;
+    float eps;
+} metok_rotate_params;
+
+METOK_API int metok_rotate_heads(int dtype, const metok_rotate_params* p, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * (10) A paged K/V cache held in 4 bits: what fills it, reads it back and attends over it.
+ *      metok_paged_evict shrinks it (dtype METOK_Q4).
+ *
+ *   16 neighbouring elements of a head's row share a scale S = 16 e, with e of the 8-bit type
+ *   e5m2 (5 bits of exponent, 2 of mantissa): the smallest e with max |x| <= 7.5 S, but at most 56.
+ *   An element is held as n = x / S, rounded to the nearest integer (ties to even) and held to
+ *   [-7, 7]; it stands for n * S, which bf16 holds exactly.  So blocks up to 6720 are off by half a
+ *   step at most, larger elements stand for 6272; elements of a block of at most 2^-13 stand for zeros.  A block
+ *   with a NaN or an infinity stands for NaNs.
+ *   A pool is [n_pages][Hkv][page_size / 16] pieces of 16 rows, 9 dh bytes each: codes
+ *   [16][dh/2] (n + 8, element d of a row in the low (d even) or high nibble of byte d/2), then
+ *   scales [16][dh/16].  A metok_paged_cache describes it (k_pool, v_pool: such pools); tables,
+ *   lengths, positions and mass are as in (6), and so are errors and what becomes of unsound
+ *   sequences, where nothing else is said.
+ *
+ *   metok_paged_append_q4: metok_paged_append with new rows of type new_dtype (METOK_F32 or METOK_BF16).
+ *
+ *   metok_paged_read_q4 writes what rows of the cache stand for, as out_dtype, for a prompt's
+ *   attention over them: rows first_row[b] + j (first_row NULL: j), j = 0 .. offsets[b+1] -
+ *   offsets[b] - 1, of sequence b to the rows offsets[b] + j of k_out and v_out ([Hkv][n_rows][dh],
+ *   strides in ELEMENTS, multiples of 16 bytes, rows at least dh apart and not overlapping), and, if pos_out is given,
+ *   their positions to pos_out [n_rows].  A sequence whose rows are not all there (below kv_len),
+ *   or whose offsets leave [0, n_rows], or with a bad page is reported by status = METOK_ERR_INVALID_ARG
+ *   and its rows of the outputs are unspecified; where offsets descend anywhere no row is written.
+ *   Rows of the outputs outside every sequence's are left as they were.
+ *   offsets DEVICE int32 [n_seqs+1], first_row DEVICE int32 [n_seqs] or NULL.
+ *   Errors: INVALID_ARG (as in (6); k_out and v_out that overlap, pos_out without positions).
+ *
+ *   metok_paged_attention_q4: (7) over such a cache, q and out of type `dtype` (METOK_F32 or METOK_BF16).
+ *   q takes part as one (bf16) or two (fp32) 11-bit numbers per element, relative to the head's
+ *   largest; weights in the product with V as one or two 11-bit numbers; logits, sums and accumulated weights are fp32.
+ * ------------------------------------------------------------------------- */
+METOK_API int metok_paged_append_q4(int new_dtype, const metok_paged_cache* c, const void* k_new, const void* v_new,
+                        int64_t k_head, int64_t k_row, int64_t v_head, int64_t v_row, int n_new,
+                        const int32_t* new_offsets, int32_t* positions, const int32_t* pos_new,
+                        float* mass, const float* mass_new, int32_t* new_len, int32_t* status, void* stream);
+METOK_API int metok_paged_read_q4(int out_dtype, const metok_paged_cache* c, const int32_t* offsets, const int32_t* first_row,
+                        int n_rows, void* k_out, void* v_out, int64_t k_head, int64_t k_row, int64_t v_head, int64_t v_row,
+                        const int32_t* positions, int32_t* pos_out, int32_t* status, void* stream);
+METOK_API size_t metok_paged_attention_q4_workspace_bytes(int dtype, const metok_paged_cache* c, int Hq, int with_mass);
+METOK_API int metok_paged_attention_q4(int dtype, const metok_paged_cache* c, const void* q, int64_t q_seq, int64_t q_head,
+                        int Hq, float softmax_scale, float softcap, const float* slopes, const int32_t* positions,
+                        float* mass, void* out, int64_t out_seq, int64_t out_head, float* lse, int32_t* status,
+                        void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------- *
  * helpers (host only, no CUDA work)

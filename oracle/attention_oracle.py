@@ -143,3 +143,58 @@ def evict_rows(mass, positions, n, budget, n_sink, n_recent):
     for hole, mover in zip(holes, [i for i in kept if i >= budget]):
         rows[hole] = mover
     return rows
+
+
+# ---- heads turned by their positions, and a cache held in 4 bits ------------------------------------------------------
+
+
+def rotate(x, angles, interleaved=False, eps=None, weight=None):
+    """x [H, n, dh] by angles [n, pairs]; eps: heads normed first.  Returns the values and, for each element, the sum of the absolute values of the
+    two that it is made of."""
+    y = np.array(x, np.float64)
+    if eps is not None:
+        y = y / np.sqrt((y ** 2).mean(-1, keepdims=True) + eps) * (1.0 if weight is None else np.asarray(weight, np.float64))
+    size = np.abs(y)
+    half = angles.shape[1]
+    a, b = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    u, v = y[..., a].copy(), y[..., b].copy()
+    y[..., a], y[..., b] = u * np.cos(angles) - v * np.sin(angles), v * np.cos(angles) + u * np.sin(angles)
+    size[..., a] = size[..., b] = np.abs(u) + np.abs(v)
+    return y, size
+
+
+# every number of type e5m2 from 0 to 56, in order: byte i stands for E5M2[i]
+E5M2 = np.array([m * 2.0 ** -16 for m in range(4)] + [(4 + m) * 2.0 ** (e - 17) for e in range(1, 21) for m in range(4)])
+E5M2 = E5M2[E5M2 <= 56.0]
+
+
+def q4_hold(x):
+    """Rows [..., dh] -> codes uint8 [..., dh / 2] and scales uint8 [..., dh / 16]."""
+    x = np.asarray(x, np.float64)
+    b = x.reshape(*x.shape[:-1], x.shape[-1] // 16, 16)
+    sound = np.isfinite(b).all(-1)
+    b = np.where(sound[..., None], b, 0.0)
+    e = np.minimum(np.searchsorted(120.0 * E5M2, np.abs(b).max(-1)), len(E5M2) - 1)
+    S = 16.0 * E5M2[e][..., None]
+    n = np.clip(np.rint(np.divide(b, S, out=np.zeros_like(b), where=S > 0)), -7, 7)
+    c = (n + 8).astype(np.uint8).reshape(x.shape)
+    return c[..., 0::2] | c[..., 1::2] << 4, np.where(sound, e, 0x7F).astype(np.uint8)
+
+
+def q4_values(codes, scales):
+    """What rows held as q4_hold says stand for."""
+    n = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 2 * codes.shape[-1]).astype(np.float64) - 8
+    e = np.append(E5M2, np.full(256 - len(E5M2), np.nan))[scales]
+    return n * np.repeat(16.0 * e, 16, axis=-1)
+
+
+def q4_parts(pool):
+    """Views of a pool [n_pages, Hkv, page / 16, 9 dh]: codes [n_pages, Hkv, page / 16, 16, dh / 2], scales [..., 16, dh / 16]."""
+    dh = pool.shape[-1] // 9
+    return pool[..., :8 * dh].reshape(*pool.shape[:-1], 16, dh // 2), pool[..., 8 * dh:].reshape(*pool.shape[:-1], 16, dh // 16)
+
+
+def q4_pool_values(pool):
+    """A whole pool's values, [n_pages, Hkv, page, dh]."""
+    v = q4_values(*q4_parts(pool))
+    return v.reshape(*v.shape[:2], -1, v.shape[-1])

@@ -24,7 +24,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "lib", "libmetok.so")
 CALLS_PATH = os.path.join(_PKG, "lib", "_metok_calls.so")
 
-F32, BF16 = 0, 1
+F32, BF16, Q4 = 0, 1, 4
 SIM_FLATTEN, SIM_MEANPOOL = 0, 1
 AGG_MEAN, AGG_MAX = 0, 1
 MODE_TOPK_MERGE, MODE_POOL = 0, 1
@@ -67,6 +67,13 @@ class PagedCache(_c.Structure):
                 ("dh", _i), ("n_seqs", _i), ("max_pages", _i)]
 
 
+class RotateParams(_c.Structure):
+    _fields_ = ([(n, _vp) for n in ("q", "k", "q_out", "k_out")] +
+                [(n, _i64) for n in ("q_head", "q_row", "k_head", "k_row", "qo_head", "qo_row", "ko_head", "ko_row")] +
+                [(n, _i) for n in ("Hq", "Hkv", "dh", "n", "rotary_dim", "interleaved", "n_axes", "norm")] +
+                [(n, _vp) for n in ("q_weight", "k_weight", "inv_freq", "positions")] + [("pair_axis", _c.POINTER(_c.c_int32)), ("eps", _f)])
+
+
 _SIGNATURES = {
     "metok_segment_events_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "metok_segment_events": (_i, [_vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -103,6 +110,12 @@ _SIGNATURES = {
     "metok_paged_evict_workspace_bytes": (_sz, [_c.POINTER(PagedCache), _i, _i]),
     "metok_paged_evict": (_i, [_i, _c.POINTER(PagedCache), _c.POINTER(_vp), _c.POINTER(_vp), _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp,
                                _vp, _sz, _vp]),
+    "metok_rotate_heads": (_i, [_i, _c.POINTER(RotateParams), _vp]),
+    "metok_paged_append_q4": (_i, [_i, _c.POINTER(PagedCache), _vp, _vp, _i64, _i64, _i64, _i64, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "metok_paged_read_q4": (_i, [_i, _c.POINTER(PagedCache), _vp, _vp, _i, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "metok_paged_attention_q4_workspace_bytes": (_sz, [_i, _c.POINTER(PagedCache), _i, _i]),
+    "metok_paged_attention_q4": (_i, [_i, _c.POINTER(PagedCache), _vp, _i64, _i64, _i, _f, _f, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp,
+                                      _vp, _sz, _vp]),
     "metok_profile_begin": (_i, []),
     "metok_profile_read": (_i, [_c.c_char_p, _sz]),
     "metok_profile_end": (_i, [_c.c_char_p, _sz]),
@@ -462,11 +475,72 @@ def metok_paged_evict(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch
                       new_len: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
     """Sequences of more than `budget` rows keep, in every layer, those whose position is among the first `n_sink` or the newest
     `n_recent` (the lower rows, if these alone are more), and of the others those with the most `mass`; K, V, `mass` and `positions` ([L, n_seqs, max_pages * page_size]) are moved
-    in place, kept rows behind the new length into the places of rows that leave.  Returns "keep_idx" (int32 [L, n_seqs, budget]: the
+    in place, kept rows behind the new length into the places of rows that leave; the pools may be held in 4 bits.  Returns "keep_idx" (int32 [L, n_seqs, budget]: the
     row that each row now holds, -1 behind the new length), "new_len" and "status" (0, or -1 where a sequence was left as it is)."""
     res = _calls().paged_evict(k_layers, v_layers, block_table, kv_len, mass, positions, budget, n_sink, n_recent, new_len)
     if type(res) is int:
         _check("metok_paged_evict", res)
+    return res
+
+
+def metok_rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                       pair_axis: Optional[Sequence[int]] = None, interleaved: bool = False, eps: Optional[float] = None,
+                       q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                       k_out: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Norms of the heads (where `eps` is given: each head's elements over the root of their mean square, times `q_weight` or `k_weight`, float
+    [dh]) and rotary positions of `q` [Hq, n, dh] and `k` [Hkv, n, dh] (or None), any strides between heads and rows.  Pair i of a head's
+    elements, (i, i + len(inv_freq)) or (2 i, 2 i + 1) if `interleaved`, turns by positions[pair_axis[i]] * inv_freq[i]: `positions` are
+    int32 [n] or [axes, n] (default: the row's index), `pair_axis` an axis for every pair (default: the first), `inv_freq` is float, of half as
+    many elements as turn (None: none do).  `q_out` and `k_out` may be `q` and `k`.  Returns "q" and "k"."""
+    res = _calls().rotate_heads(q, k, inv_freq, positions, pair_axis, interleaved, eps, q_weight, k_weight, q_out, k_out)
+    if type(res) is int:
+        _check("metok_rotate_heads", res)
+    return res
+
+
+def q4_pool(n_pages: int, Hkv: int, page_size: int, dh: int, device="cuda") -> torch.Tensor:
+    """A pool of a paged cache held in 4 bits, its rows not yet written: uint8 [n_pages, Hkv, page_size / 16, 9 * dh]."""
+    if page_size % 16:
+        raise ValueError(f"pages of {page_size} rows: a multiple of 16 is wanted")
+    return torch.empty((n_pages, Hkv, page_size // 16, 9 * dh), dtype=torch.uint8, device=device)
+
+
+def metok_paged_append_q4(k_new: torch.Tensor, v_new: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, block_table: torch.Tensor,
+                          kv_len: torch.Tensor, new_offsets: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                          pos_new: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None,
+                          mass_new: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """metok_paged_append into a cache held in 4 bits: pools of q4_pool, new rows in bf16 or fp32."""
+    res = _calls().paged_append_q4(k_new, v_new, k_pool, v_pool, block_table, kv_len, new_offsets, positions, pos_new, mass, mass_new,
+                                   new_len)
+    if type(res) is int:
+        _check("metok_paged_append_q4", res)
+    return res
+
+
+def metok_paged_read_q4(k_pool: torch.Tensor, v_pool: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, offsets: torch.Tensor,
+                        n_rows: int, first_row: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                        dtype: torch.dtype = torch.bfloat16, k_out: Optional[torch.Tensor] = None,
+                        v_out: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """What rows of a cache held in 4 bits stand for, packed as metok_prefill_attention takes them: rows first_row[b] (default 0) and on of
+    sequence b to rows offsets[b] .. offsets[b + 1] - 1 (int32 [n_seqs + 1]) of the `n_rows` of "k" and "v" [Hkv, n_rows, dh] (bf16, exact, or fp32;
+    `k_out` and `v_out`, any strides between heads and rows, or new); with `positions` ([n_seqs, max_pages * page_size]) those of the rows, too.  "status" is 0, or
+    -1 where a sequence's rows are not all there or have a bad page (its rows are then unspecified; where `offsets` descend none is written)."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    res = _calls().paged_read_q4(k_pool, v_pool, block_table, kv_len, offsets, n_rows, first_row, positions, dtype is torch.bfloat16, k_out, v_out)
+    if type(res) is int:
+        _check("metok_paged_read_q4", res)
+    return res
+
+
+def metok_paged_attention_q4(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                             softmax_scale: float, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                             positions: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None, with_lse: bool = False,
+                             out: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """metok_paged_attention over a cache held in 4 bits; `q` and "out" in bf16 or fp32."""
+    res = _calls().paged_attention_q4(q, k_pool, v_pool, block_table, kv_len, softmax_scale, softcap, slopes, positions, mass, with_lse, out)
+    if type(res) is int:
+        _check("metok_paged_attention_q4", res)
     return res
 
 

@@ -148,6 +148,27 @@ inline bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int dh) {
     const int64_t a = std::min(s0, s1), b = std::max(s0, s1), n = s0 <= s1 ? n0 : n1;
     return a >= dh && (b - dh) / a >= n - 1;           // all rows of the narrower dimension lie in one step of the other
 }
+// Rows [H][n] of dh elements, in bytes; a stride that is never stepped along is 0.
+struct Extent {
+    uintptr_t at;
+    int64_t H, head, n, row, dh;
+    uintptr_t size() const { return (uintptr_t)((H - 1) * head + (n - 1) * row + dh); }
+};
+inline Extent extent_of(const void* at, int H, int64_t head, int n, int64_t row, int dh, int esize) {
+    return {reinterpret_cast<uintptr_t>(at), H, H > 1 ? head * esize : 0, n, n > 1 ? row * esize : 0, (int64_t)dh * esize};
+}
+// No element of one is an element of the other: their extents are apart, or both repeat with the same period (between rows, as the
+// heads of one projection do, or between heads) and lie in different parts of it.
+inline bool apart(const Extent& a, const Extent& b) {
+    if (a.at >= b.at + b.size() || b.at >= a.at + a.size()) return true;
+    auto by = [&](int64_t pa, int64_t pb, int64_t span_a, int64_t span_b) {
+        if (pa != pb || span_a > pa || span_b > pa) return false;
+        const int64_t d = ((int64_t)(b.at - a.at) % pa + pa) % pa;
+        return d >= span_a && d + span_b <= pa;
+    };
+    return by(a.row, b.row, (a.H - 1) * a.head + a.dh, (b.H - 1) * b.head + b.dh) ||
+           by(a.head, b.head, (a.n - 1) * a.row + a.dh, (b.n - 1) * b.row + b.dh);
+}
 // A softmax's scale and cap (0: none): what the kernels make of them is finite.
 inline bool softmax_numbers(float scale, float cap) {
     constexpr float kMost = 1.0e38f;                   // times log2(e) it is still finite

@@ -37,7 +37,9 @@ namespace {
     X(metok_prefill_prune_schedule) X(metok_kv_compact_workspace_bytes) X(metok_kv_compact)               \
     X(metok_prefill_attention_workspace_bytes) X(metok_prefill_attention)                                \
     X(metok_paged_append) X(metok_paged_attention_workspace_bytes) X(metok_paged_attention)              \
-    X(metok_paged_evict_workspace_bytes) X(metok_paged_evict)
+    X(metok_paged_evict_workspace_bytes) X(metok_paged_evict) X(metok_rotate_heads)                      \
+    X(metok_paged_append_q4) X(metok_paged_read_q4)                                                      \
+    X(metok_paged_attention_q4_workspace_bytes) X(metok_paged_attention_q4)
 struct Api {
 #define X(name) decltype(&::name) name;
     METOK_HOST_CALLS(X)
@@ -71,7 +73,8 @@ struct Py {                                                   // owned reference
     X(sims) X(boundaries) X(event_offsets) X(frame_event) X(_sims) X(_boundaries) X(_offsets)            \
     X(token_score) X(token_inv_norm) X(out_feats) X(out_src) X(out_event) X(out_members) X(assign)       \
     X(frame_score) X(event_score) X(event_is_key) X(n_out) X(status) X(scores) X(keep_idx) X(S_out)      \
-    X(hidden_out) X(token_group) X(origin) X(n_vis) X(S) X(_inputs) X(keep_len) X(new_len) X(out) X(lse)
+    X(hidden_out) X(token_group) X(origin) X(n_vis) X(S) X(_inputs) X(keep_len) X(new_len) X(out) X(lse) \
+    X(q) X(k) X(v) X(positions)
 struct Names {
 #define X(name) PyObject* name;
     METOK_HOST_NAMES(X)
@@ -690,10 +693,17 @@ PyObject* prefill_attention(PyObject* const* a, Py_ssize_t n) {
     return res.p;
 }
 
-// The pools of one layer, the table and the lengths; `hold` keeps the last two.
-metok_paged_cache paged_cache(const at::Tensor& k, PyObject* v_obj, PyObject* table_obj, PyObject* len_obj, at::Tensor* hold) {
+// The pools of one layer, the table and the lengths; `hold` keeps the last two.  q4: pools held in 4 bits.
+metok_paged_cache paged_cache(const at::Tensor& k, PyObject* v_obj, PyObject* table_obj, PyObject* len_obj, at::Tensor* hold, bool q4 = false) {
     const at::Device dev = k.device();
-    if (k.dim() != 4 || !k.is_contiguous()) fail(PyExc_ValueError, "%s must be a contiguous [n_pages, Hkv, page_size, dh]", "a pool");
+    if (q4) {
+        if (k.dim() != 4 || !k.is_contiguous() || k.size(3) % 9)
+            fail(PyExc_ValueError, "%s must be a contiguous [n_pages, Hkv, page_size / 16, 9 * dh]", "a pool");
+        if (k.scalar_type() != at::kByte) fail(PyExc_TypeError, "%s must be uint8", "a pool");
+        if (k.size(2) > 0x7FFFFFF) fail(PyExc_ValueError, "%s is too large", "a pool");
+    } else if (k.dim() != 4 || !k.is_contiguous()) {
+        fail(PyExc_ValueError, "%s must be a contiguous [n_pages, Hkv, page_size, dh]", "a pool");
+    }
     const at::Tensor& v = on(v_obj, "a pool", dev);
     if (v.sizes() != k.sizes() || !v.is_contiguous() || v.scalar_type() != k.scalar_type())
         fail(PyExc_ValueError, "%s must be contiguous, of one shape and type", "the pools");
@@ -703,19 +713,20 @@ metok_paged_cache paged_cache(const at::Tensor& k, PyObject* v_obj, PyObject* ta
     hold[1] = array(len_obj, "kv_len", dev, at::kInt, table.size(0));
     if (!hold[1].defined()) fail(PyExc_TypeError, "%s must be a tensor", "kv_len");
     return {k.data_ptr(), v.data_ptr(), (const int32_t*)hold[0].data_ptr(), (const int32_t*)hold[1].data_ptr(), size_of(k, 0, "a pool"),
-            size_of(k, 1, "a pool"), size_of(k, 2, "a pool"), size_of(k, 3, "a pool"), size_of(table, 0, "block_table"),
+            size_of(k, 1, "a pool"), size_of(k, 2, "a pool") * (q4 ? 16 : 1), size_of(k, 3, "a pool") / (q4 ? 9 : 1), size_of(table, 0, "block_table"),
             size_of(table, 1, "block_table")};
 }
 
 // k_new, v_new, k_pool, v_pool, block_table, kv_len, new_offsets, positions, pos_new, mass, mass_new, new_len
+template <bool kQ4>
 PyObject* paged_append(PyObject* const* a, Py_ssize_t n) {
     want(n, 12);
     const at::Tensor& kp = first_tensor(a[2], "k_pool");
     const at::Device dev = kp.device();
     const c10::cuda::CUDAGuard guard(dev);
     at::Tensor hold[2];
-    const metok_paged_cache c = paged_cache(kp, a[3], a[4], a[5], hold);
-    const at::ScalarType dt = kp.scalar_type();
+    const metok_paged_cache c = paged_cache(kp, a[3], a[4], a[5], hold, kQ4);
+    const at::ScalarType dt = (kQ4 ? tensor(a[0], "k_new") : kp).scalar_type();
     const at::Tensor &kn = rows3(a[0], "k_new", dev, dt), &vn = rows3(a[1], "v_new", dev, dt);
     if (kn.sizes() != vn.sizes() || kn.size(0) != c.Hkv || kn.size(2) != c.dh) fail(PyExc_ValueError, "%s must be [Hkv, n_new, dh]", "k_new, v_new");
     const int n_new = size_of(kn, 1, "k_new");
@@ -726,7 +737,7 @@ PyObject* paged_append(PyObject* const* a, Py_ssize_t n) {
     at::Tensor new_len = array(a[11], "new_len", dev, at::kInt, c.n_seqs);
     if (!new_len.defined()) new_len = empty_i32(c.n_seqs, dev);
     const at::Tensor status = empty_i32(1, dev);
-    const int st = api.metok_paged_append(dtype_code(kp), &c, kn.data_ptr(), vn.data_ptr(), step(kn, 0, 0), step(kn, 1, c.dh), step(vn, 0, 0),
+    const int st = (kQ4 ? api.metok_paged_append_q4 : api.metok_paged_append)(dtype_code(kn), &c, kn.data_ptr(), vn.data_ptr(), step(kn, 0, 0), step(kn, 1, c.dh), step(vn, 0, 0),
                                           step(vn, 1, c.dh), n_new, ptr_or_null<const int32_t>(off), ptr_or_null<int32_t>(pos),
                                           ptr_or_null<const int32_t>(pos_new), ptr_or_null<float>(mass), ptr_or_null<const float>(mass_new),
                                           (int32_t*)new_len.data_ptr(), (int32_t*)status.data_ptr(), current_stream());
@@ -740,16 +751,17 @@ PyObject* paged_append(PyObject* const* a, Py_ssize_t n) {
 }
 
 // q, k_pool, v_pool, block_table, kv_len, softmax_scale, softcap, slopes, positions, mass, with_lse, out
+template <bool kQ4>
 PyObject* paged_attention(PyObject* const* a, Py_ssize_t n) {
     want(n, 12);
     const at::Tensor& kp = first_tensor(a[1], "k_pool");
     const at::Device dev = kp.device();
     const c10::cuda::CUDAGuard guard(dev);
     at::Tensor hold[2];
-    const metok_paged_cache c = paged_cache(kp, a[2], a[3], a[4], hold);
-    const at::Tensor& q = rows3(a[0], "q", dev, kp.scalar_type());
+    const metok_paged_cache c = paged_cache(kp, a[2], a[3], a[4], hold, kQ4);
+    const at::Tensor& q = rows3(a[0], "q", dev, (kQ4 ? tensor(a[0], "q") : kp).scalar_type());
     if (q.size(0) != c.n_seqs || q.size(2) != c.dh) fail(PyExc_ValueError, "%s must be [n_seqs, Hq, dh]", "q");
-    const int Hq = size_of(q, 1, "q"), dt = dtype_code(kp);
+    const int Hq = size_of(q, 1, "q"), dt = dtype_code(q);
     const int64_t S_cap = (int64_t)c.max_pages * c.page_size;
     const at::Tensor slopes = array(a[7], "slopes", dev, at::kFloat, Hq), pos = array(a[8], "positions", dev, at::kInt, c.n_seqs * S_cap),
                      mass = array(a[9], "mass", dev, at::kFloat, c.n_seqs * S_cap);
@@ -760,9 +772,9 @@ PyObject* paged_attention(PyObject* const* a, Py_ssize_t n) {
     at::Tensor lse;
     if (with_lse) lse = empty({c.n_seqs, Hq}, at::kFloat, dev);
     const at::Tensor status = empty_i32(1, dev);
-    const size_t need = api.metok_paged_attention_workspace_bytes(dt, &c, Hq, mass.defined());
+    const size_t need = (kQ4 ? api.metok_paged_attention_q4_workspace_bytes : api.metok_paged_attention_workspace_bytes)(dt, &c, Hq, mass.defined());
     const at::Tensor ws = empty({(int64_t)need}, at::kByte, dev);
-    const int st = api.metok_paged_attention(
+    const int st = (kQ4 ? api.metok_paged_attention_q4 : api.metok_paged_attention)(
         dt, &c, q.data_ptr(), step(q, 0, 0), step(q, 1, c.dh), Hq, (float)number(a[5]), (float)number(a[6]), ptr_or_null<const float>(slopes),
         ptr_or_null<const int32_t>(pos), ptr_or_null<float>(mass), out.data_ptr(), step(out, 0, 0), step(out, 1, c.dh), ptr_or_null<float>(lse),
         (int32_t*)status.data_ptr(), ws.data_ptr(), need, current_stream());
@@ -786,7 +798,8 @@ PyObject* paged_evict(PyObject* const* a, Py_ssize_t n) {
     const at::Device dev = k0.device();
     const c10::cuda::CUDAGuard guard(dev);
     at::Tensor hold[2];
-    const metok_paged_cache c = paged_cache(k0, vs.items[0], a[2], a[3], hold);
+    const bool q4 = k0.scalar_type() == at::kByte;
+    const metok_paged_cache c = paged_cache(k0, vs.items[0], a[2], a[3], hold, q4);
     if (ks.n > 1024) return PyLong_FromLong(METOK_ERR_UNSUPPORTED);
     const int L = (int)ks.n;
     std::vector<void*> kp(L), vp(L);
@@ -809,7 +822,7 @@ PyObject* paged_evict(PyObject* const* a, Py_ssize_t n) {
     const at::Tensor keep = empty({L, c.n_seqs, budget}, at::kInt, dev), status = empty_i32(1, dev);
     const size_t need = api.metok_paged_evict_workspace_bytes(&c, L, (int)budget);
     const at::Tensor ws = empty({(int64_t)need}, at::kByte, dev);
-    const int st = api.metok_paged_evict(dtype_code(k0), &c, kp.data(), vp.data(), L, (int)budget, n_sink, n_recent, ptr_or_null<int32_t>(pos),
+    const int st = api.metok_paged_evict(q4 ? METOK_Q4 : dtype_code(k0), &c, kp.data(), vp.data(), L, (int)budget, n_sink, n_recent, ptr_or_null<int32_t>(pos),
                                          ptr_or_null<float>(mass), (int32_t*)keep.data_ptr(), (int32_t*)new_len.data_ptr(),
                                          (int32_t*)status.data_ptr(), ws.data_ptr(), need, current_stream());
     if (st != METOK_OK) return PyLong_FromLong(st);
@@ -818,6 +831,115 @@ PyObject* paged_evict(PyObject* const* a, Py_ssize_t n) {
     put(res.p, names.keep_idx, keep);
     put(res.p, names.new_len, new_len);
     put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
+// k_pool, v_pool, block_table, kv_len, offsets, n_rows, first_row, positions, dtype, k_out, v_out
+PyObject* paged_read_q4(PyObject* const* a, Py_ssize_t n) {
+    want(n, 11);
+    const at::Tensor& kp = first_tensor(a[0], "k_pool");
+    const at::Device dev = kp.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor hold[2];
+    const metok_paged_cache c = paged_cache(kp, a[1], a[2], a[3], hold, true);
+    const long rows = integer(a[5]);
+    if (rows < 0 || rows > 0x7FFFFFFF) fail(PyExc_ValueError, "%s is out of range", "n_rows");
+    const int64_t S_cap = (int64_t)c.max_pages * c.page_size;
+    const at::Tensor off = array(a[4], "offsets", dev, at::kInt, (int64_t)c.n_seqs + 1), first = array(a[6], "first_row", dev, at::kInt, c.n_seqs),
+                     pos = array(a[7], "positions", dev, at::kInt, c.n_seqs * S_cap);
+    if (!off.defined()) fail(PyExc_TypeError, "%s must be a tensor", "offsets");
+    const bool bf16 = PyObject_IsTrue(a[8]);           // the wrapper's answer
+    const at::ScalarType dt = bf16 ? at::kBFloat16 : at::kFloat;
+    const at::Tensor k = a[9] == Py_None ? empty({c.Hkv, rows, c.dh}, dt, dev) : rows3(a[9], "k_out", dev, dt),
+                     v = a[10] == Py_None ? empty({c.Hkv, rows, c.dh}, dt, dev) : rows3(a[10], "v_out", dev, dt);
+    if (k.sizes() != v.sizes() || k.size(0) != c.Hkv || k.size(1) != rows || k.size(2) != c.dh)
+        fail(PyExc_ValueError, "%s must be [Hkv, n_rows, dh]", "k_out, v_out");
+    at::Tensor pos_out;
+    if (pos.defined()) pos_out = empty({rows}, at::kInt, dev);
+    const at::Tensor status = empty_i32(1, dev);
+    const int st = api.metok_paged_read_q4(bf16 ? METOK_BF16 : METOK_F32, &c, (const int32_t*)off.data_ptr(), ptr_or_null<const int32_t>(first), (int)rows,
+                                           k.data_ptr(), v.data_ptr(), step(k, 0, 0), step(k, 1, c.dh), step(v, 0, 0), step(v, 1, c.dh),
+                                           ptr_or_null<const int32_t>(pos), ptr_or_null<int32_t>(pos_out), (int32_t*)status.data_ptr(), current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.k, k);
+    put(res.p, names.v, v);
+    if (pos_out.defined()) put(res.p, names.positions, pos_out);
+    put(res.p, names.status, status);
+    Py_INCREF(res.p);
+    return res.p;
+}
+
+// q, k, inv_freq, positions, pair_axis, interleaved, eps, q_weight, k_weight, q_out, k_out
+PyObject* rotate_heads(PyObject* const* a, Py_ssize_t n) {
+    want(n, 11);
+    const at::Tensor& q = first_tensor(a[0], "q");
+    const at::Device dev = q.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    const at::ScalarType dt = q.scalar_type();
+    const int code = dtype_code(q);
+    rows3(a[0], "q", dev, dt);
+    const bool with_k = a[1] != Py_None;
+    at::Tensor k;
+    if (with_k) {
+        k = rows3(a[1], "k", dev, dt);
+        if (k.size(1) != q.size(1) || k.size(2) != q.size(2)) fail(PyExc_ValueError, "%s must be [Hkv, n, dh], q [Hq, n, dh]", "k");
+    }
+    metok_rotate_params p = {};
+    p.Hq = size_of(q, 0, "q"); p.n = size_of(q, 1, "q"); p.dh = size_of(q, 2, "q");
+    p.Hkv = with_k ? size_of(k, 0, "k") : 0;
+    if (with_k && p.Hkv < 1) fail(PyExc_ValueError, "%s has no heads", "k");
+    const at::Tensor freq = array(a[2], "inv_freq", dev, at::kFloat, -1);
+    if (freq.defined() && freq.numel() > 1 << 20) fail(PyExc_ValueError, "%s is too large", "inv_freq");
+    p.rotary_dim = freq.defined() ? 2 * (int)freq.numel() : 0;
+    p.inv_freq = ptr_or_null<const float>(freq);
+    p.n_axes = 1;
+    at::Tensor pos;
+    if (a[3] != Py_None) {
+        pos = array(a[3], "positions", dev, at::kInt, -1);
+        if ((pos.dim() != 1 && pos.dim() != 2) || pos.size(-1) != p.n) fail(PyExc_ValueError, "%s must be [n] or [axes, n]", "positions");
+        if (pos.dim() == 2) p.n_axes = size_of(pos, 0, "positions");
+    }
+    p.positions = ptr_or_null<const int32_t>(pos);
+    int32_t axis[64];
+    if (a[4] != Py_None) {
+        Seq s(a[4]);
+        if (s.n != p.rotary_dim / 2) fail(PyExc_ValueError, "%s must hold an axis for every pair", "pair_axis");
+        if (s.n > 64) return PyLong_FromLong(METOK_ERR_INVALID_ARG);
+        for (Py_ssize_t i = 0; i < s.n; ++i) {
+            const long v = integer(s.items[i]);
+            axis[i] = v < 0 || v > 127 ? -1 : (int32_t)v;
+        }
+        p.pair_axis = axis;
+    }
+    const int interleaved = PyObject_IsTrue(a[5]);
+    if (interleaved < 0) throw PyError();
+    p.interleaved = interleaved;
+    p.norm = a[6] != Py_None;
+    p.eps = p.norm ? (float)number(a[6]) : 0.f;
+    const at::Tensor qw = array(a[7], "q_weight", dev, at::kFloat, p.dh), kw = array(a[8], "k_weight", dev, at::kFloat, p.dh);
+    if (!p.norm && (qw.defined() || kw.defined())) fail(PyExc_ValueError, "%s: weights want eps", "q_weight, k_weight");
+    p.q_weight = ptr_or_null<const float>(qw);
+    p.k_weight = ptr_or_null<const float>(kw);
+    const at::Tensor qo = a[9] == Py_None ? empty(q.sizes(), dt, dev) : rows3(a[9], "q_out", dev, dt);
+    if (qo.sizes() != q.sizes()) fail(PyExc_ValueError, "%s must have the shape of q", "q_out");
+    at::Tensor ko;
+    if (with_k) {
+        ko = a[10] == Py_None ? empty(k.sizes(), dt, dev) : rows3(a[10], "k_out", dev, dt);
+        if (ko.sizes() != k.sizes()) fail(PyExc_ValueError, "%s must have the shape of k", "k_out");
+        p.k = k.data_ptr(); p.k_out = ko.data_ptr();
+        p.k_head = step(k, 0, 0); p.k_row = step(k, 1, 0); p.ko_head = step(ko, 0, 0); p.ko_row = step(ko, 1, 0);
+    }
+    p.q = q.data_ptr(); p.q_out = qo.data_ptr();
+    p.q_head = step(q, 0, 0); p.q_row = step(q, 1, 0); p.qo_head = step(qo, 0, 0); p.qo_row = step(qo, 1, 0);
+    const int st = api.metok_rotate_heads(code, &p, current_stream());
+    if (st != METOK_OK) return PyLong_FromLong(st);
+    Py res(PyDict_New());
+    if (!res.p) throw PyError();
+    put(res.p, names.q, qo);
+    if (with_k) put(res.p, names.k, ko);
     Py_INCREF(res.p);
     return res.p;
 }
@@ -846,9 +968,13 @@ PyMethodDef methods[] = {
     FAST("prefill_prune_schedule", prefill_prune_schedule),
     FAST("kv_compact", kv_compact),
     FAST("prefill_attention", prefill_attention),
-    FAST("paged_append", paged_append),
-    FAST("paged_attention", paged_attention),
+    FAST("paged_append", paged_append<false>),
+    FAST("paged_attention", paged_attention<false>),
     FAST("paged_evict", paged_evict),
+    FAST("rotate_heads", rotate_heads),
+    FAST("paged_append_q4", paged_append<true>),
+    FAST("paged_read_q4", paged_read_q4),
+    FAST("paged_attention_q4", paged_attention<true>),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_metok_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

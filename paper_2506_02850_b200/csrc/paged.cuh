@@ -29,6 +29,14 @@ inline int paged_dims(int dtype, const metok_paged_cache* c, PagedDims* d) {
     *d = {c->n_pages, c->Hkv, shift, c->dh, c->n_seqs, c->max_pages, c->dh * esize / 16};
     return METOK_OK;
 }
+// The same for a cache held in 4 bits: its rows lie in pieces of 16, a row_chunks of its own has no meaning.
+constexpr int kQ4Rows = 16;                            // rows of a piece
+__host__ __device__ constexpr int q4_piece(int dh) { return 9 * dh; }    // bytes of a piece: codes [16][dh / 2], scales [16][dh / 16]
+inline int paged_dims_q4(const metok_paged_cache* c, PagedDims* d) {
+    const int rc = paged_dims(METOK_BF16, c, d);
+    d->row_chunks = 0;
+    return rc;
+}
 // [a, a + an) and [b, b + bn) share an element
 inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -40,6 +48,10 @@ inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
 __device__ __forceinline__ size_t paged_chunk(const PagedDims& d, int page, int h, int r) {
     const size_t row = (((size_t)page * d.Hkv + h) << d.page_shift) + (r & ((1 << d.page_shift) - 1));
     return row * d.row_chunks;
+}
+// The piece that has row `r` of head `h` in the page `page` of a cache held in 4 bits, and the row's place in it: r % 16.
+__device__ __forceinline__ size_t q4_piece_of(const PagedDims& d, int page, int h, int r) {
+    return (((size_t)page * d.Hkv + h) << (d.page_shift - 4)) + ((r & ((1 << d.page_shift) - 1)) >> 4);
 }
 #endif
 

@@ -17,103 +17,13 @@
 //     are 5.8: two launches, filling the ring and the joins' chain of loads are the rest.
 //   fp32: eight lanes share a row, four rows at a time; the lanes' partial dot products of several heads are reduced and
 //     dealt out in one butterfly.
-#include <algorithm>
-
-#include "launchers.h"
-#include "paged.cuh"
-#include "sm100.cuh"
+#include "paged_attn.cuh"
 
 namespace metok {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLow = -3.0e38f;                       // below every logit: keeps differences free of inf - inf
 constexpr int kWarps = 4, kThreads = (kWarps + 1) * 32;
-
-struct PagedAttnArgs {
-    PagedDims d;
-    int Hq, G, NC, heads;                              // heads per K/V head, units per (sequence, K/V head), heads of a unit at most
-    int grid, tile_shift;                              // CTAs of the first kernel; rows of a tile
-    const void* q;
-    long long q_seq, q_head, out_seq, out_head;
-    const int32_t *block_table, *kv_len, *positions;
-    const float* slopes;
-    float scale_log2, cap_scale, cap_log2;             // softcap > 0: x = cap_log2 * tanh(dot * cap_scale); else cap_log2 is 0
-    float* mass;
-    void* out;
-    float *lse, *part_o, *part_ml, *logits;
-    long long* line;                                   // [n_seqs + 1]: tiles of the sequences before each, per unit; then of all
-    int32_t* status;
-    int withhold;                                      // debug builds: the copies to leave out
-};
-
-// Tiles of sequence b's one unit (0 for a length out of range, which the second kernel reports).
-__device__ __forceinline__ int unit_tiles(const PagedAttnArgs& a, int b) {
-    const int len = a.kv_len[b];
-    return len > 0 && len <= a.d.S_cap() ? (len + (1 << a.tile_shift) - 1) >> a.tile_shift : 0;
-}
-
-// Tiles of all sequences, per unit; whole CTA.  Up to 32 sequences every warp finds out by itself: no barrier.
-__device__ __forceinline__ long long line_tiles(const PagedAttnArgs& a, long long* s_sum) {
-    if (a.d.n_seqs <= 32) {
-        const int lane = threadIdx.x & 31;
-        return (long long)__reduce_add_sync(0xFFFFFFFFu, lane < a.d.n_seqs ? unit_tiles(a, lane) : 0);
-    }
-    long long all = 0;
-    for (int i = threadIdx.x; i < a.d.n_seqs; i += blockDim.x) all += unit_tiles(a, i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = all;
-    __syncthreads();
-    all = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) all += s_sum[w];
-    return all;
-}
-
-// The line for the second kernel: one warp, 32 sequences at a time.
-__device__ __forceinline__ void write_line(const PagedAttnArgs& a) {
-    const int lane = threadIdx.x & 31;
-    long long before = 0;
-    for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
-        const int b = b0 + lane, mine = b < a.d.n_seqs ? unit_tiles(a, b) : 0;
-        int incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += x;
-        }
-        if (b < a.d.n_seqs) a.line[b] = before + incl - mine;
-        before += __shfl_sync(0xFFFFFFFFu, incl, 31);
-    }
-    if (lane == 0) a.line[a.d.n_seqs] = before;
-}
-
-// CTAs that have tiles: each of them at least one.
-__device__ __forceinline__ long long busy_ctas(const PagedAttnArgs& a, long long tiles) { return min((long long)a.grid, tiles); }
-
-// Where a CTA is in the line: the unit, its tiles, and the tile.
-struct Place {
-    int b, sub, nt, t;                                 // sub: (K/V head, head chunk) of sequence b
-    long long left;                                    // tiles still to do
-};
-__device__ __forceinline__ void next_tile(const PagedAttnArgs& a, Place& p, int subs) {
-    --p.left;
-    if (++p.t < p.nt) return;
-    p.t = 0;
-    if (++p.sub < subs) return;
-    p.sub = 0;
-    if (p.left > 0) {
-        do { ++p.b; p.nt = unit_tiles(a, p.b); } while (p.nt == 0 && p.b + 1 < a.d.n_seqs);   // tiles are left: it finds them
-    }
-}
-
-// Logit in log2 units of a raw product: scaled, capped, less the distance's share.
-__device__ __forceinline__ float logit2(const PagedAttnArgs& a, float dot, float slope2, float far) {
-    if (a.cap_log2 > 0.f) dot = a.cap_log2 * tanhf(dot * a.cap_scale);
-    else dot *= a.scale_log2;
-    return fmaf(-slope2, far, dot);
-}
 
 template <typename T, int DH>
 struct PagedShape {
@@ -531,44 +441,7 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     const long long T_all = line_tiles(a, s_sum) * subs, ctas = busy_ctas(a, T_all);
     if (blockIdx.x >= ctas) return;                    // uniform
     const long long t_lo = T_all * blockIdx.x / ctas, t_hi = T_all * (blockIdx.x + 1) / ctas;
-    // the sequence that holds tile t_lo, 32 at a time: by every warp for itself where there are no more
-    Place p;
-    long long start = 0;
-    p.b = 0;
-    if (warp == 0 || a.d.n_seqs <= 32) {
-        long long at = 0;                              // tiles before sequence b0
-        for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
-            const int b = b0 + lane;
-            long long mine = b < a.d.n_seqs ? (long long)unit_tiles(a, b) * subs : 0, incl = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            const uint32_t any = __ballot_sync(0xFFFFFFFFu, at + incl > t_lo);
-            if (any) {
-                const int l = __ffs(any) - 1;
-                p.b = b0 + l;
-                start = at + __shfl_sync(0xFFFFFFFFu, incl - mine, l);
-                break;
-            }
-            at += __shfl_sync(0xFFFFFFFFu, incl, 31);
-        }
-    }
-    if (a.d.n_seqs > 32 && threadIdx.x == 0) {
-        s_b = p.b;
-        s_start = start;
-    }
-    __syncthreads();
-    if (a.d.n_seqs > 32) {
-        p.b = s_b;
-        start = s_start;
-    }
-    p.nt = unit_tiles(a, p.b);
-    const long long in = t_lo - start;
-    p.sub = (int)(in / p.nt);
-    p.t = (int)(in - (long long)p.sub * p.nt);
-    p.left = t_hi - t_lo;
+    Place p = find_place(a, subs, t_lo, t_hi, &s_b, &s_start);
     volatile int* abort_flag = &s_abort;
 
     if (warp == kWarps) {                              // brings the tiles
@@ -695,217 +568,11 @@ paged_attn_kernel(const PagedAttnArgs a, const __grid_constant__ CUtensorMap tm_
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
-// The partials of a unit: CTAs c0 .. c1, of which CTA c's lies at slot unit + c.
-struct Slots { long long first; int n; };
-__device__ __forceinline__ Slots unit_slots(const PagedAttnArgs& a, long long all, long long unit, long long f0, int nt) {
-    // the CTA that has tile f is the last one with floor(all * c / ctas) <= f
-    const long long ctas = busy_ctas(a, all), c0 = ((f0 + 1) * ctas - 1) / all, c1 = ((f0 + nt) * ctas - 1) / all;
-    return {unit + c0, (int)(c1 - c0) + 1};
-}
-
-// Joins the partials.  CTAs [0, n_seqs * Hq): one head's output and lse; the others: the weights of kMassRows rows of a sequence.
-constexpr int kJoinThreads = 128, kMassRows = 128;
-template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinThreads)
-paged_join_kernel(const PagedAttnArgs a) {
-    // Up to the wait: what needs only the call's inputs, which were complete when the first kernel was let go.
-    __shared__ __align__(16) float s_acc[kJoinThreads][4];
-    __shared__ float2 s_ml[kJoinThreads];
-    extern __shared__ __align__(16) uint8_t s_dyn[];
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int outs = a.d.n_seqs * a.Hq;
-    const bool weights = (int)blockIdx.x >= outs;
-    const int chunks = (a.d.S_cap() + kMassRows - 1) / kMassRows;
-    const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / a.Hq;
-    const int len = a.kv_len[b], subs = a.d.Hkv * a.NC;
-    const int row0 = weights ? (((int)blockIdx.x - outs) - b * chunks) * kMassRows : 0;
-    // the sequence is sound: only then anything is written for it
-    bool ok = len >= 0 && len <= a.d.S_cap();
-    if (ok) {
-        const int used = (len + (1 << a.d.page_shift) - 1) >> a.d.page_shift;
-        bool there = true;
-        for (int p = tid; p < used; p += kJoinThreads) {
-            const int page = a.block_table[(size_t)b * a.d.max_pages + p];
-            there &= page >= 0 && page < a.d.n_pages;
-        }
-        ok = __syncthreads_and(there);
-    }
-    const int nt = unit_tiles(a, b);
-    long long all = 0, base = 0;                       // tiles of the line, and of the sequences before b
-    const bool few = a.d.n_seqs <= 32;                 // one look at all lengths; else the line that the first kernel wrote
-    if (few) {
-        const int mine = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
-        all = (long long)__reduce_add_sync(0xFFFFFFFFu, mine) * subs;
-        base = (long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? mine : 0) * subs;
-    } else {
-        grid_dep_wait();
-        all = a.line[a.d.n_seqs] * subs;
-        base = a.line[b] * subs;
-    }
-
-    const auto sound = [&] {
-        if (few) grid_dep_wait();
-        if (!ok && tid == 0) *a.status = METOK_ERR_INVALID_ARG;
-        return ok;
-    };
-
-    if (!weights) {
-        const int h = (int)blockIdx.x - b * a.Hq, hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads;
-        T* out = reinterpret_cast<T*>(a.out) + b * a.out_seq + h * a.out_head;
-        const int sub = hk * a.NC + ch;
-        const Slots sl = nt ? unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt) : Slots{0, 0};
-        if (!sound()) return;
-        if (nt == 0) {
-            for (int i = tid; i < DH; i += kJoinThreads) from_float(out[i], 0.f);
-            if (tid == 0 && a.lse) a.lse[(size_t)b * a.Hq + h] = __int_as_float(0xFF800000);
-            return;
-        }
-        // DH / 4 threads side by side, kRuns slots at a time, each run with a maximum of its own
-        constexpr int kLanes = DH / 4, kRuns = kJoinThreads / kLanes;
-        const int col = tid % kLanes, run = tid / kLanes;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float M = kLow, L = 0.f;
-        constexpr int kAhead = 6;                      // slots whose loads are on their way
-        for (int i0 = run; i0 < sl.n; i0 += kRuns * kAhead) {
-            float2 ml[kAhead];
-            float4 o[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const size_t at = (size_t)(sl.first + i0 + u * kRuns) * a.heads + hl;
-                const bool in = i0 + u * kRuns < sl.n;
-                ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + at * 2) : make_float2(kLow, 0.f);
-                o[u] = in ? reinterpret_cast<const float4*>(a.part_o + at * DH)[col] : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            float top = M;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) top = fmaxf(top, ml[u].x);
-            const float less = sm100::fast_exp2(M - top);
-            M = top;
-            L *= less;
-            acc.x *= less; acc.y *= less; acc.z *= less; acc.w *= less;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const float f = sm100::fast_exp2(ml[u].x - M);
-                L += f * ml[u].y;
-                acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
-            }
-        }
-        *reinterpret_cast<float4*>(s_acc[tid]) = acc;
-        s_ml[tid] = make_float2(M, L);
-        __syncthreads();
-        if (run == 0) {
-#pragma unroll
-            for (int r = 1; r < kRuns; ++r) M = fmaxf(M, s_ml[r * kLanes + col].x);
-            L = 0.f;
-            acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int r = 0; r < kRuns; ++r) {
-                const float4 o = *reinterpret_cast<const float4*>(s_acc[r * kLanes + col]);
-                const float2 ml = s_ml[r * kLanes + col];
-                const float f = sm100::fast_exp2(ml.x - M);
-                acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
-                L += f * ml.y;
-            }
-            const float inv = L == 0.f ? 0.f : 1.f / L;                  // 0: every logit is -infinity
-            from_float(out[col * 4], acc.x * inv);
-            from_float(out[col * 4 + 1], acc.y * inv);
-            from_float(out[col * 4 + 2], acc.z * inv);
-            from_float(out[col * 4 + 3], acc.w * inv);
-            if (col == 0 && a.lse) a.lse[(size_t)b * a.Hq + h] = kLn2 * (M + log2f(L));
-        }
-        return;
-    }
-
-    // weights: where every unit's partials and every head's logits lie, then the heads' normalisers: eight threads per head, a running
-    // (maximum, sum) each with kAhead loads on their way; the first heads' logits come meanwhile
-    long long* s_first = reinterpret_cast<long long*>(s_dyn);            // [subs]
-    int* s_n = reinterpret_cast<int*>(s_first + subs);                   // [subs]
-    float* s_lse = reinterpret_cast<float*>(s_n + subs);                 // [Hq]: log2 of the sum
-    long long* s_off = reinterpret_cast<long long*>(s_dyn + ((size_t)subs * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8);   // [Hq]: the head's logits of the sequence
-    for (int sub = tid; sub < subs && nt; sub += kJoinThreads) {
-        const Slots sl = unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt);
-        s_first[sub] = sl.first;
-        s_n[sub] = sl.n;
-    }
-    for (int h = tid; h < a.Hq; h += kJoinThreads) {
-        const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads;
-        s_off[h] = ((long long)(hk * a.NC + ch) * nt * a.heads + (g - ch * a.heads)) << a.tile_shift;
-    }
-    __syncthreads();
-    if (!sound() || row0 >= len) return;
-    const int row = min(row0 + tid, len - 1), tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
-    const float* x = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
-    constexpr int kHeads = 16, kAhead = 10;
-    float v[kHeads];
-    auto logits_of = [&](int h0) {
-#pragma unroll
-        for (int u = 0; u < kHeads; ++u) v[u] = h0 + u < a.Hq ? x[s_off[h0 + u]] : kLow;
-    };
-    logits_of(0);
-    for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
-        const int h = h0 + (tid >> 3), part = tid & 7;
-        float M = kLow, L = 0.f;
-        if (h < a.Hq) {
-            const int hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads, sub = hk * a.NC + ch;
-            const Slots sl = {s_first[sub], s_n[sub]};
-            const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + sl.first * a.heads + hl;
-            for (int i0 = part; i0 < sl.n; i0 += 8 * kAhead) {
-                float2 p[kAhead];
-                float top = M;
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) p[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) top = fmaxf(top, p[u].x);
-                L *= sm100::fast_exp2(M - top);
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) L += sm100::fast_exp2(p[u].x - top) * p[u].y;
-                M = top;
-            }
-        }
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, o), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, o), top = fmaxf(M, m2);
-            L = L * sm100::fast_exp2(M - top) + l2 * sm100::fast_exp2(m2 - top);
-            M = top;
-        }
-        if (h < a.Hq && part == 0) s_lse[h] = L == 0.f ? 0.f : M + log2f(L);       // (every logit -infinity: weights of 0)
-    }
-    __syncthreads();
-    if (row0 + tid >= len) return;
-    float sum = 0.f;
-    for (int h = 0; h < a.Hq; h += kHeads) {           // kHeads loads on their way (a loop of single ones would wait for each)
-        if (h) logits_of(h);
-#pragma unroll
-        for (int u = 0; u < kHeads; ++u) sum += h + u < a.Hq ? sm100::fast_exp2(v[u] - s_lse[h + u]) : 0.f;
-    }
-    a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
-}
-
-// How the heads of a K/V head are dealt to units, and the line to CTAs.
-struct PagedPlan {
-    int G, heads, NC, grid, tile_shift;
-    size_t slots, tiles;
-};
 PagedPlan paged_plan(int dtype, const PagedDims& d, int Hq) {
-    PagedPlan p;
-    p.G = Hq / d.Hkv;
-    const int most = dtype == METOK_BF16 ? 16 : 8;     // heads of a unit
-    const int per = ceil_div(p.G, ceil_div(p.G, most));
-    if (dtype == METOK_BF16) p.heads = per <= 8 ? 8 : 16;
-    else p.heads = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 ? 4 : 8;
-    p.NC = ceil_div(p.G, p.heads);
-    p.tile_shift = dtype == METOK_BF16 ? 6 : 5;
-    const size_t units = (size_t)d.n_seqs * d.Hkv * p.NC;
-    p.tiles = units * (size_t)((d.S_cap() + (1 << p.tile_shift) - 1) >> p.tile_shift);
-    p.grid = (int)std::min<size_t>(p.tiles, 2 * kNumSMs);
-    p.slots = units + p.grid;
-    return p;
-}
-void paged_carve(Carver& cv, const PagedPlan& p, const PagedDims& d, bool mass, PagedAttnArgs* a) {
-    a->part_o = cv.take<float>(p.slots * p.heads * d.dh);
-    a->part_ml = cv.take<float>(p.slots * p.heads * 2);
-    a->line = cv.take<long long>((size_t)d.n_seqs + 1);
-    a->logits = mass ? cv.take<float>(p.tiles * p.heads << p.tile_shift) : nullptr;
+    const int G = Hq / d.Hkv, most = dtype == METOK_BF16 ? 16 : 8;       // heads of a unit
+    const int per = ceil_div(G, ceil_div(G, most));
+    const int heads = dtype == METOK_BF16 ? (per <= 8 ? 8 : 16) : per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 ? 4 : 8;
+    return paged_plan_of(d, Hq, heads, dtype == METOK_BF16 ? 6 : 5, 2 * kNumSMs);
 }
 
 template <typename T, int DH, int HX, int kUnitHeads>
@@ -918,15 +585,7 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
         launch_chained(kern, dim3(a.grid + 1), dim3(kThreads), S::kRing, st, a, tk, tv);
     }
     METOK_LAUNCH_CHECK();
-    {
-        METOK_TIMED("paged_join", st);
-        const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-        const size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
-        METOK_ALLOW_SMEM((paged_join_kernel<T, DH>), smem);
-        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), smem, st, a);
-    }
-    METOK_LAUNCH_CHECK();
-    return METOK_OK;
+    return launch_paged_join<T, DH>(a, st);
 }
 template <int DH>
 int launch_paged_dh(int dtype, const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
@@ -961,31 +620,14 @@ extern "C" int metok_paged_attention(int dtype, const metok_paged_cache* c, cons
     PagedDims d;
     int rc = paged_dims(dtype, c, &d);
     if (rc != METOK_OK) return rc;
-    if (!c->k_pool || !c->v_pool || !c->block_table || !c->kv_len || !q || !out || !status) return METOK_ERR_INVALID_ARG;
-    if (Hq < 1 || Hq % d.Hkv) return METOK_ERR_INVALID_ARG;
-    if (Hq > 2048) return METOK_ERR_UNSUPPORTED;
-    if (!aligned16(c->k_pool) || !aligned16(c->v_pool) || !aligned16(q) || !aligned16(out)) return METOK_ERR_INVALID_ARG;
-    if (!aligned4(c->block_table) || !aligned4(c->kv_len) || !aligned4(slopes) || !aligned4(positions) || !aligned4(mass) ||
-        !aligned4(lse) || !aligned4(status))
-        return METOK_ERR_INVALID_ARG;
-    const int per = 16 / (dtype == METOK_F32 ? 4 : 2);
-    if (q_seq < 0 || q_head < 0 || out_seq < 0 || out_head < 0 || (q_seq | q_head | out_seq | out_head) % per) return METOK_ERR_INVALID_ARG;
-    // outputs of different heads and sequences do not overlap
-    if (!rows_apart(d.n_seqs, out_seq, Hq, out_head, d.dh) || !softmax_numbers(softmax_scale, softcap)) return METOK_ERR_INVALID_ARG;
+    rc = paged_attention_heads(d, c, q, out, status, Hq);
+    if (rc != METOK_OK) return rc;
     const PagedPlan p = paged_plan(dtype, d, Hq);
-    const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-    if (join > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
-    if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     PagedAttnArgs a;
-    a.d = d;
-    a.Hq = Hq; a.G = p.G; a.NC = p.NC; a.heads = p.heads; a.grid = p.grid; a.tile_shift = p.tile_shift;
-    a.q = q; a.q_seq = q_seq; a.q_head = q_head; a.out = out; a.out_seq = out_seq; a.out_head = out_head;
-    a.block_table = c->block_table; a.kv_len = c->kv_len; a.positions = positions; a.slopes = slopes;
-    a.scale_log2 = softmax_scale * kLog2e;
-    a.cap_scale = softcap > 0.f ? softmax_scale / softcap : 0.f;
-    a.cap_log2 = softcap * kLog2e;
-    a.mass = mass; a.lse = lse; a.status = status;
-    a.withhold = debug_withheld();
+    rc = paged_attention_args(dtype, d, c, p, q, q_seq, q_head, Hq, softmax_scale, softcap, slopes, positions, mass, out, out_seq, out_head, lse,
+                              status, &a);
+    if (rc != METOK_OK) return rc;
+    if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     Carver cv(ws);
     paged_carve(cv, p, d, mass != nullptr, &a);
     const uint64_t rows = (uint64_t)d.n_pages * d.Hkv << d.page_shift;
