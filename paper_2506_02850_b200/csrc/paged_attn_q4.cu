@@ -24,16 +24,19 @@ namespace metok {
 namespace {
 
 constexpr int kWarps = 4, kThreads = (kWarps + 1) * 32;
-constexpr float kLift = 14.f;                          // weights are relative to 2^-14 of the largest
+// A head's weights are exp2(x - m) with a reference m that was 2^12 below the largest when it was taken; it is taken anew where a weight passes 2^15.5
+// (fp16 ends at 2^16).
+constexpr float kLift = 12.f, kMostWeight = 15.5f;
 
-template <int DH>
+// RP: pieces of a tile that are one warp's.
+template <int DH, int NG, int RP>
 struct Q4Shape {
-    static constexpr int kTile = kQ4Rows * kWarps;
-    static constexpr uint32_t kPiece = q4_piece(DH), kHalf = kWarps * kPiece, kStage = 2 * kHalf;      // K, then V
-    static constexpr int kStages = DH == 128 ? 6 : 12;
+    static constexpr int kPieces = kWarps * RP, kTile = kQ4Rows * kPieces;
+    static constexpr uint32_t kPiece = q4_piece(DH), kHalf = kPieces * kPiece, kStage = 2 * kHalf;     // K, then V
+    static constexpr int kCtas = NG == 1 ? 3 : 2;      // of an SM
+    static constexpr int kStages = 55296 / kStage;
     static constexpr size_t kRing = (size_t)kStages * kStage + 128;
 };
-constexpr int q4_ctas(int groups) { return groups == 1 ? 3 : 2; }        // CTAs of an SM
 
 __device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ __half2 as_half2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
@@ -44,9 +47,16 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     return r;
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The first product of a sum.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // The constants of two scales (as fp16: their bytes in the upper halves).
@@ -58,14 +68,19 @@ struct Q4Block {
         c0 = __hmul2(e, __float2half2_rn(-1032.f));
         c1 = __hmul2(e, __float2half2_rn(-72.f));
     }
-    // Nibbles j and j + 4 of `w`, j = 0 .. 3.
+    // Nibbles j and j + 4 of `w`, j = 0 .. 3.  (One operation masks and sets the exponents only where one of the constants is in a register.)
     __device__ __forceinline__ void pairs(uint32_t w, uint32_t (&r)[4]) const {
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
-            r[j] = as_u32(__hfma2(as_half2((w & 0x000F000Fu) | 0x64006400u), e, c0));
-            r[j + 1] = as_u32(__hfma2(as_half2((w & 0x00F000F0u) | 0x64006400u), e16, c1));
+            r[j] = as_u32(__hfma2(as_half2(mask_or(w, 0x000F000Fu)), e, c0));
+            r[j + 1] = as_u32(__hfma2(as_half2(mask_or(w, 0x00F000F0u)), e16, c1));
             w >>= 8;
         }
+    }
+    static __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask) {
+        uint32_t r;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(0x64006400u));
+        return r;
     }
 };
 
@@ -74,7 +89,7 @@ struct Q4Block {
 template <int DH, int NG, int QP>
 struct Q4Unit {
     uint32_t q[QP][NG][DH / 16][2];
-    float m[NG][2], l[NG][2], o[NG][DH / 16][4], slope[NG][2], lift[NG][2];      // lift: what the head's q was divided by, and the scales' unit
+    float m[NG][2], l[NG][2], o[NG][DH / 16][4], slope[NG][2], scale[NG][2];     // scale: from products to logits (to logits / cap)
 
     template <typename T>
     __device__ __forceinline__ void start(const PagedAttnArgs& a, int b, int h0, int nh) {
@@ -114,7 +129,7 @@ struct Q4Unit {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int hc = n * 8 + 2 * t + e;
-                lift[n][e] = __shfl_sync(0xFFFFFFFFu, up, (2 * t + e) * 4);
+                scale[n][e] = fmaxf(__shfl_sync(0xFFFFFFFFu, up, (2 * t + e) * 4) * (a.cap_log2 > 0.f ? a.cap_scale : a.scale_log2), 1.2e-38f);   // (never 0)
                 m[n][e] = kLow;
                 l[n][e] = 0.f;
                 slope[n][e] = a.slopes && hc < nh ? a.slopes[h0 + hc] * kLog2e : 0.f;
@@ -129,31 +144,46 @@ struct Q4Unit {
 
 __device__ __forceinline__ int row_at(int r) { return r ^ (r >> 2 & 1); }          // pi: the row at place r of eight
 
-// The warp's piece of a tile, of whose rows `rows` are there (<= 0: none); `far`: distances of the lane's two rows; `logits`: those of the
-// piece's rows, [head][kTile], or null.
-template <int DH, int NG, int QP>
+// tanh(y) of logits in units of the cap, |y| <= 1: y P(y^2), P the polynomial of degree 6 of least largest relative error (5e-8; 1.6e-7 in fp32).
+__device__ __forceinline__ float tanh_near(float y) {
+    const float u = y * y;
+    float t = 0.0010410226f;
+    t = fmaf(t, u, -0.00620337902f);
+    t = fmaf(t, u, 0.0202899799f);
+    t = fmaf(t, u, -0.0534570292f);
+    t = fmaf(t, u, 0.13325204f);
+    t = fmaf(t, u, -0.333328396f);
+    t = fmaf(t, u, 0.99999994f);
+    return y * t;
+}
+
+// The warp's RP pieces of a tile, of whose rows `rows` are there (kPart: not all; >= 1).  kBent: logits are capped or biased; `pos`: positions of the
+// lane's rows, for the bias.  kMass: `logits` of the warp's rows, [head][kTile], are left for the second kernel.
+template <int DH, int NG, int QP, int RP, bool kBent, bool kMass, bool kPart>
 __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnArgs& a, const uint8_t* kp, const uint8_t* vp, int rows,
-                                        const float (&far)[2], float* logits, int nh) {
-    using S = Q4Shape<DH>;
+                                        float newest, const int (&pos)[2 * RP], float* logits, int nh) {
+    using S = Q4Shape<DH, NG, RP>;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r0 = row_at(g);
-    float x[NG][4], y[NG][4];                          // two chains of products
+    float x[RP][NG][4];                                // products, or logits (kBent, kMass)
+    auto less = [&](int r, int n, int e) {             // the logit less its reference
+        return kBent || kMass ? x[r][n][e] - u.m[n][e & 1] : fmaf(x[r][n][e], u.scale[n][e & 1], -u.m[n][e & 1]);
+    };
 #pragma unroll
-    for (int n = 0; n < NG; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = y[n][e] = 0.f;
-    {
+    for (int r = 0; r < RP; ++r) {
+        const uint8_t* const piece = kp + r * S::kPiece;
+        float y[NG][4];                                // two chains of products
         uint32_t w[2][DH / 32], sc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int row = r0 + 8 * i;
             if constexpr (DH == 128) {
-                const uint4 v = *reinterpret_cast<const uint4*>(kp + row * 64 + t * 16);
+                const uint4 v = *reinterpret_cast<const uint4*>(piece + row * 64 + t * 16);
                 w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
-                sc[i] = *reinterpret_cast<const uint16_t*>(kp + 8 * DH + row * 8 + 2 * t);
+                sc[i] = *reinterpret_cast<const uint16_t*>(piece + 8 * DH + row * 8 + 2 * t);
             } else {
-                const uint2 v = *reinterpret_cast<const uint2*>(kp + row * 32 + t * 8);
+                const uint2 v = *reinterpret_cast<const uint2*>(piece + row * 32 + t * 8);
                 w[i][0] = v.x; w[i][1] = v.y;
-                sc[i] = kp[8 * DH + row * 4 + t];
+                sc[i] = piece[8 * DH + row * 4 + t];
             }
         }
 #pragma unroll
@@ -169,60 +199,123 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
                 for (int n = 0; n < NG; ++n)
 #pragma unroll
                     for (int z = 0; z < QP; ++z) {
-                        mma_f16(x[n], f0[0], f1[0], f0[1], f1[1], u.q[z][n][2 * i][0], u.q[z][n][2 * i][1]);
-                        mma_f16(y[n], f0[2], f1[2], f0[3], f1[3], u.q[z][n][2 * i + 1][0], u.q[z][n][2 * i + 1][1]);
+                        if (i == 0 && z == 0) {
+                            mma_f16_first(x[r][n], f0[0], f1[0], f0[1], f1[1], u.q[z][n][2 * i][0], u.q[z][n][2 * i][1]);
+                            mma_f16_first(y[n], f0[2], f1[2], f0[3], f1[3], u.q[z][n][2 * i + 1][0], u.q[z][n][2 * i + 1][1]);
+                        } else {
+                            mma_f16(x[r][n], f0[0], f1[0], f0[1], f1[1], u.q[z][n][2 * i][0], u.q[z][n][2 * i][1]);
+                            mma_f16(y[n], f0[2], f1[2], f0[3], f1[3], u.q[z][n][2 * i + 1][0], u.q[z][n][2 * i + 1][1]);
+                        }
                     }
             }
         }
-    }
-    const bool in0 = r0 < rows, in1 = r0 + 8 < rows;
-    uint32_t p16[QP][NG][2];
 #pragma unroll
-    for (int n = 0; n < NG; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = logit2(a, (x[n][e] + y[n][e]) * u.lift[n][e & 1], u.slope[n][e & 1], far[e >> 1]);
-        if (logits) {
+        for (int n = 0; n < NG; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int h = n * 8 + 2 * t + (e & 1);
-                if (h < nh && (e < 2 ? in0 : in1)) logits[h * S::kTile + r0 + (e >> 1) * 8] = x[n][e];
+                x[r][n][e] += y[n][e];
+                if constexpr (kBent || kMass) x[r][n][e] *= u.scale[n][e & 1];
+            }
+    }
+    if constexpr (kBent) {
+        if (a.cap_log2 > 0.f) {
+            float most = 0.f;
+#pragma unroll
+            for (int r = 0; r < RP; ++r)
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(x[r][n][e]));
+            if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
+#pragma unroll
+                for (int r = 0; r < RP; ++r)
+#pragma unroll
+                    for (int n = 0; n < NG; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[r][n][e] = a.cap_log2 * tanhf(x[r][n][e]);
+            } else {                                   // (a NaN comes out as one here, too)
+#pragma unroll
+                for (int r = 0; r < RP; ++r)
+#pragma unroll
+                    for (int n = 0; n < NG; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[r][n][e] = a.cap_log2 * tanh_near(x[r][n][e]);
             }
         }
-        float top[2];
+        if (a.slopes) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            top[e] = fmaxf(in0 ? x[n][e] : kLow, in1 ? x[n][e + 2] : kLow);
+            for (int r = 0; r < RP; ++r)
 #pragma unroll
-            for (int s = 4; s < 32; s <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xFFFFFFFFu, top[e], s));
-            top[e] = fmaxf(top[e] - kLift, u.m[n][e]);
-        }
-        if (__any_sync(0xFFFFFFFFu, top[0] > u.m[n][0] || top[1] > u.m[n][1])) {
-            const float f0 = sm100::fast_exp2(u.m[n][0] - top[0]), f1 = sm100::fast_exp2(u.m[n][1] - top[1]);
-            u.l[n][0] *= f0;
-            u.l[n][1] *= f1;
+                for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int k = 0; k < DH / 16; ++k) {
-                u.o[n][k][0] *= f0;
-                u.o[n][k][1] *= f1;
-                u.o[n][k][2] *= f0;
-                u.o[n][k][3] *= f1;
-            }
-            u.m[n][0] = top[0];
-            u.m[n][1] = top[1];
-        }
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = (e < 2 ? in0 : in1) ? sm100::fast_exp2(x[n][e] - u.m[n][e & 1]) : 0.f;
-        u.l[n][0] += p[0] + p[2];
-        u.l[n][1] += p[1] + p[3];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const __half2 hi = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
-            p16[0][n][e] = transpose8x8(as_u32(hi));
-            if constexpr (QP == 2) p16[1][n][e] = transpose8x8(pack_f16(p[2 * e] - __low2float(hi), p[2 * e + 1] - __high2float(hi)));
+                    for (int e = 0; e < 4; ++e) x[r][n][e] = fmaf(-u.slope[n][e & 1], fabsf(newest - (float)pos[2 * r + (e >> 1)]), x[r][n][e]);
         }
     }
-    {
+    if constexpr (kMass) {
+#pragma unroll
+        for (int r = 0; r < RP; ++r)
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int h = n * 8 + 2 * t + (e & 1), row = r0 + 16 * r + 8 * (e >> 1);
+                    if (h < nh && (!kPart || row < rows)) logits[h * S::kTile + row] = x[r][n][e];
+                }
+    }
+    float more = kLow;
+#pragma unroll
+    for (int r = 0; r < RP; ++r)
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // rows that are not there have no weight
+                if (kPart && r0 + 16 * r + 8 * (e >> 1) >= rows) x[r][n][e] = __int_as_float(0xFF800000);
+                more = fmaxf(more, less(r, n, e));
+            }
+    if (__any_sync(0xFFFFFFFFu, more > kMostWeight)) {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float top = kLow;
+#pragma unroll
+                for (int r = 0; r < RP; ++r) top = fmaxf(top, fmaxf(x[r][n][e], x[r][n][e + 2]));
+#pragma unroll
+                for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+                if (!kBent && !kMass) top *= u.scale[n][e];              // (> 0)
+                top = fmaxf(top - kLift, u.m[n][e]);
+                f[e] = sm100::fast_exp2(u.m[n][e] - top);
+                u.l[n][e] *= f[e];
+                u.m[n][e] = top;
+            }
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u.o[n][k][e] *= f[e & 1];
+        }
+    }
+    uint32_t p16[RP][QP][NG][2];
+#pragma unroll
+    for (int r = 0; r < RP; ++r)
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = sm100::fast_exp2(less(r, n, e));
+            u.l[n][0] += p[0] + p[2];
+            u.l[n][1] += p[1] + p[3];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const __half2 hi = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
+                p16[r][0][n][e] = transpose8x8(as_u32(hi));
+                if constexpr (QP == 2) p16[r][1][n][e] = transpose8x8(pack_f16(p[2 * e] - __low2float(hi), p[2 * e + 1] - __high2float(hi)));
+            }
+        }
+#pragma unroll
+    for (int r = 0; r < RP; ++r) {
+        const uint8_t* const piece = vp + r * S::kPiece;
         // places 2 t + e + 8 f: words of both rows of a pair, interleaved; scales of rows that are not there are zeros
         uint32_t w[2][DH / 64][2], sc[2];
 #pragma unroll
@@ -230,17 +323,18 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
             const int ra = row_at(2 * t) + 8 * f, rb = row_at(2 * t + 1) + 8 * f;
             uint32_t va[DH / 64], vb[DH / 64], sa, sb;
             if constexpr (DH == 128) {
-                const uint2 x0 = *reinterpret_cast<const uint2*>(vp + ra * 64 + g * 8), x1 = *reinterpret_cast<const uint2*>(vp + rb * 64 + g * 8);
+                const uint2 x0 = *reinterpret_cast<const uint2*>(piece + ra * 64 + g * 8), x1 = *reinterpret_cast<const uint2*>(piece + rb * 64 + g * 8);
                 va[0] = x0.x; va[1] = x0.y; vb[0] = x1.x; vb[1] = x1.y;
-                sa = vp[8 * DH + ra * 8 + g];
-                sb = vp[8 * DH + rb * 8 + g];
+                sa = piece[8 * DH + ra * 8 + g];
+                sb = piece[8 * DH + rb * 8 + g];
             } else {
-                va[0] = *reinterpret_cast<const uint32_t*>(vp + ra * 32 + g * 4);
-                vb[0] = *reinterpret_cast<const uint32_t*>(vp + rb * 32 + g * 4);
-                sa = vp[8 * DH + ra * 4 + (g >> 1)];
-                sb = vp[8 * DH + rb * 4 + (g >> 1)];
+                va[0] = *reinterpret_cast<const uint32_t*>(piece + ra * 32 + g * 4);
+                vb[0] = *reinterpret_cast<const uint32_t*>(piece + rb * 32 + g * 4);
+                sa = piece[8 * DH + ra * 4 + (g >> 1)];
+                sb = piece[8 * DH + rb * 4 + (g >> 1)];
             }
-            sc[f] = (ra < rows ? sa << 8 : 0u) | (rb < rows ? sb << 24 : 0u);
+            sc[f] = __byte_perm(sa, sb, 0x4101);       // the bytes into the upper bytes of the halves
+            if (kPart) sc[f] &= (ra + 16 * r < rows ? 0xFFFFu : 0u) | (rb + 16 * r < rows ? 0xFFFF0000u : 0u);
 #pragma unroll
             for (int i = 0; i < DH / 64; ++i) {
                 w[f][i][0] = __byte_perm(va[i], vb[i], 0x5410);
@@ -260,87 +354,87 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
                 for (int n = 0; n < NG; ++n)
 #pragma unroll
                     for (int z = 0; z < QP; ++z) {
-                        mma_f16(u.o[n][k], f0[0], f0[1], f1[0], f1[1], p16[z][n][0], p16[z][n][1]);
-                        mma_f16(u.o[n][k + 1], f0[2], f0[3], f1[2], f1[3], p16[z][n][0], p16[z][n][1]);
+                        mma_f16(u.o[n][k], f0[0], f0[1], f1[0], f1[1], p16[r][z][n][0], p16[r][z][n][1]);
+                        mma_f16(u.o[n][k + 1], f0[2], f0[3], f1[2], f1[3], p16[r][z][n][0], p16[r][z][n][1]);
                     }
             }
     }
 }
 
-// A unit's warps meet in shared memory, o [head][DH], m and l [head]: close() adds up the lanes' sums, store() writes the warp's part,
-// merge() takes another warp's part in.
+// A unit's end: the warps leave o in shared memory as their lanes hold it, and m and l by head; then each warp joins a quarter of o.
+template <int DH, int NG>
+struct Q4Join {
+    float2 o[kWarps][NG][DH / 16][2][32];              // elements 2 k, 2 k + 1 of the lane's of heads 2 t, 2 t + 1
+    float2 ml[kWarps][NG * 8];
+};
 template <int DH, int NG, int QP>
-__device__ __forceinline__ void unit_close(Q4Unit<DH, NG, QP>& u) {
+__device__ __forceinline__ void unit_end(Q4Unit<DH, NG, QP>& u, Q4Join<DH, NG>& j, int nh, float* part_o, float2* part_ml) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) u.l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, u.l[n][e], s);
+            if (lane < 4) j.ml[warp][n * 8 + 2 * t + e] = make_float2(u.m[n][e], u.l[n][e]);
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) j.o[warp][n][k][e][lane] = make_float2(u.o[n][k][e], u.o[n][k][e + 2]);
+        }
+    }
+    sm100::named_bar_sync(1, kWarps * 32);
+    constexpr int kMine = DH / 16 / kWarps;            // k that are this warp's: 2 kMine elements in a row
 #pragma unroll
     for (int n = 0; n < NG; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int s = 4; s < 32; s <<= 1) u.l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, u.l[n][e], s);
-}
-template <int DH, int NG, int QP>
-__device__ __forceinline__ void unit_merge(Q4Unit<DH, NG, QP>& u, const float* s_o, const float* s_ml) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int n = 0; n < NG; ++n) {
-        const int h = n * 8 + 2 * (lane & 3);
-        float f[2], w[2];
-#pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float m = s_ml[2 * (h + e)], M = fmaxf(m, u.m[n][e]);
-            f[e] = sm100::fast_exp2(u.m[n][e] - M);
-            w[e] = sm100::fast_exp2(m - M);
-            u.l[n][e] = u.l[n][e] * f[e] + s_ml[2 * (h + e) + 1] * w[e];
-            u.m[n][e] = M;
-        }
+            const int h = n * 8 + 2 * t + e;
+            float2 ml[kWarps];
+            float M = kLow, L = 0.f;
 #pragma unroll
-        for (int k = 0; k < DH / 16; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float2 x = *reinterpret_cast<const float2*>(s_o + (h + e) * DH + DH / 8 * (lane >> 2) + 2 * k);
-                u.o[n][k][e] = u.o[n][k][e] * f[e] + x.x * w[e];
-                u.o[n][k][e + 2] = u.o[n][k][e + 2] * f[e] + x.y * w[e];
+            for (int w = 0; w < kWarps; ++w) {
+                ml[w] = j.ml[w][h];
+                M = fmaxf(M, ml[w].x);
             }
-    }
-}
-template <int DH, int NG, int QP>
-__device__ __forceinline__ void unit_store(Q4Unit<DH, NG, QP>& u, float* s_o, float* s_ml) {
-    const int lane = threadIdx.x & 31;
+            float2 o[kMine];
 #pragma unroll
-    for (int n = 0; n < NG; ++n) {
-        const int h = n * 8 + 2 * (lane & 3);
-        if (lane < 4) {
+            for (int k = 0; k < kMine; ++k) o[k] = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                s_ml[2 * (h + e)] = u.m[n][e];
-                s_ml[2 * (h + e) + 1] = u.l[n][e];
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = sm100::fast_exp2(ml[w].x - M);
+                L += f * ml[w].y;
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    const float2 x = j.o[w][n][warp * kMine + k][e][lane];
+                    o[k].x = fmaf(f * kQ4Unit, x.x, o[k].x);
+                    o[k].y = fmaf(f * kQ4Unit, x.y, o[k].y);
+                }
+            }
+            if (h < nh) {
+                float* dst = part_o + h * DH + DH / 8 * g + 2 * kMine * warp;
+                if constexpr (kMine == 2) *reinterpret_cast<float4*>(dst) = make_float4(o[0].x, o[0].y, o[1].x, o[1].y);
+                else *reinterpret_cast<float2*>(dst) = o[0];
+                if (warp == 0 && g == 0) part_ml[h] = make_float2(M, L);
             }
         }
-#pragma unroll
-        for (int k = 0; k < DH / 16; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<float2*>(s_o + (h + e) * DH + DH / 8 * (lane >> 2) + 2 * k) = make_float2(u.o[n][k][e], u.o[n][k][e + 2]);
-    }
+    sm100::named_bar_sync(1, kWarps * 32);
 }
 
-template <typename T, int DH, int NG>
-__global__ void __launch_bounds__(kThreads, q4_ctas(NG))
+template <typename T, int DH, int NG, int RP, bool kBent, bool kMass>
+__global__ void __launch_bounds__(kThreads, (Q4Shape<DH, NG, RP>::kCtas))
 paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool) {
     using namespace sm100;
-    using S = Q4Shape<DH>;
+    using S = Q4Shape<DH, NG, RP>;
     constexpr int QP = sizeof(T) == 4 ? 2 : 1;
     extern __shared__ uint8_t smem_dyn[];
     __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages];
-    __shared__ __align__(16) float s_o[2][NG * 8 * DH];
-    __shared__ float s_ml[2][NG * 16];
+    __shared__ Q4Join<DH, NG> s_join;
     __shared__ long long s_sum[kWarps + 1];
     __shared__ long long s_start;
     __shared__ int s_b;
     __shared__ int s_abort;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    uint8_t* const ring = smem_dyn + (((smem_u32(smem_dyn) + 127u) & ~127u) - smem_u32(smem_dyn));
     const int subs = a.d.Hkv * a.NC;
+    uint8_t* const ring = smem_dyn + (((smem_u32(smem_dyn) + 127u) & ~127u) - smem_u32(smem_dyn));
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), kWarps); }
         s_abort = 0;
@@ -359,7 +453,7 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
     volatile int* abort_flag = &s_abort;
 
     if (warp == kWarps) {                              // brings the tiles
-        const int per_page = 1 << (a.d.page_shift - 4), run = min(per_page, kWarps);       // pieces of a page that are a copy
+        const int per_page = 1 << (a.d.page_shift - 4), run = min(per_page, S::kPieces);   // pieces of a page that are a copy
         int it = 0;
         for (; p.left > 0; ++it) {
             const int s = it % S::kStages;
@@ -387,76 +481,66 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
             mbar_wait_warp(smem_u32(&full_bar[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u, abort_flag);
         }
     } else {
-        int it = 0, newest = 0;
-        bool ok = true, fresh = true;
+        const int mine = warp * RP * kQ4Rows;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
         Q4Unit<DH, NG, QP> u;
-        while (p.left > 0) {
+        while (p.left > 0) {                           // units
             const int hk = p.sub / a.NC, ch = p.sub - hk * a.NC, h0 = hk * a.G + ch * a.heads, nh = min(a.heads, a.G - ch * a.heads);
-            const int len = a.kv_len[p.b], r0 = p.t * S::kTile + warp * kQ4Rows, rows = len - r0;
+            const int len = a.kv_len[p.b], tiles = (int)min((long long)(p.nt - p.t), p.left);
             const int32_t* pos = a.positions ? a.positions + (size_t)p.b * a.d.S_cap() : nullptr;
-            if (fresh) {
-                u.template start<T>(a, p.b, h0, nh);
-                newest = a.slopes ? (pos ? pos[len - 1] : len - 1) : 0;
-                fresh = false;
-            }
-            const int s = it % S::kStages;
-            // distances of the rows that this lane's logits are of
-            float far[2] = {0.f, 0.f};
-            if (a.slopes) {
-                auto distance = [&](int r) { r = min(r0 + r, len - 1); return fabsf((float)newest - (float)(pos ? pos[r] : r)); };
-                far[0] = distance(row_at(lane >> 2));
-                far[1] = distance(row_at(lane >> 2) + 8);
-            }
-            float* logits = nullptr;
-            if (a.mass) logits = a.logits + (size_t)(t_hi - p.left) * a.heads * S::kTile + warp * kQ4Rows;
-            if (ok && !mbar_wait_warp(smem_u32(&full_bar[s]), (uint32_t)(it / S::kStages) & 1u, abort_flag)) ok = false;
-            if (ok) {
-                const uint8_t* k = ring + s * S::kStage + warp * S::kPiece;
-                if (rows > 0) q4_tile<DH, NG, QP>(u, a, k, k + S::kHalf, rows, far, logits, nh);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[s]));
+            const float newest = kBent && a.slopes ? (float)(pos ? pos[len - 1] : len - 1) : 0.f;
+            float* logits = kMass ? a.logits + (size_t)(t_hi - p.left) * a.heads * S::kTile + mine : nullptr;
+            u.template start<T>(a, p.b, h0, nh);
+            int first = p.t * S::kTile + mine;         // the warp's first row of the tile
+            for (int n = 0; n < tiles; ++n) {
+                // positions of the rows that this lane's logits are of: they are not wanted before the products are there
+                int at[2 * RP] = {};
+                if (kBent && a.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 2 * RP; ++i) {
+                        at[i] = min(first + row_at(lane >> 2) + 8 * i, len - 1);
+                        if (pos) at[i] = pos[at[i]];
+                    }
+                }
+                if (ok && !mbar_wait_warp(smem_u32(&full_bar[stage]), phase, abort_flag)) ok = false;
+                if (ok) {
+                    const uint8_t* k = ring + stage * S::kStage + warp * RP * S::kPiece;
+                    if (first + kQ4Rows * RP <= len) q4_tile<DH, NG, QP, RP, kBent, kMass, false>(u, a, k, k + S::kHalf, 0, newest, at, logits, nh);
+                    else if (first < len) q4_tile<DH, NG, QP, RP, kBent, kMass, true>(u, a, k, k + S::kHalf, len - first, newest, at, logits, nh);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&empty_bar[stage]));
+                }
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+                first += S::kTile;
+                if (kMass) logits += a.heads * S::kTile;
             }
             const long long unit = (long long)p.b * subs + p.sub;
-            const bool ends = p.t + 1 == p.nt || p.left == 1;
-            ++it;
+            p.t += tiles - 1;
+            p.left -= tiles - 1;
             next_tile(a, p, subs);
-            if (ends) {
-                fresh = true;
-                // warps 2 and 3 give their rows to warps 0 and 1; what those have is joined on the way out
-                unit_close(u);
-                if (warp >= 2) unit_store(u, s_o[warp - 2], s_ml[warp - 2]);
-                named_bar_sync(1, kWarps * 32);
-                if (warp < 2) unit_merge(u, s_o[warp], s_ml[warp]);
-                __syncwarp();
-                if (warp < 2) unit_store(u, s_o[warp], s_ml[warp]);
-                named_bar_sync(1, kWarps * 32);
-                const size_t slot = (size_t)(unit + blockIdx.x);
-                for (int i = threadIdx.x; i < nh * (DH / 4); i += kWarps * 32) {
-                    const int h = i / (DH / 4);
-                    const float m0 = s_ml[0][2 * h], m1 = s_ml[1][2 * h], M = fmaxf(m0, m1);
-                    const float f = fast_exp2(m0 - M), w = fast_exp2(m1 - M), L = f * s_ml[0][2 * h + 1] + w * s_ml[1][2 * h + 1];
-                    const float4 x = reinterpret_cast<const float4*>(s_o[0])[i], y = reinterpret_cast<const float4*>(s_o[1])[i];
-                    reinterpret_cast<float4*>(a.part_o + slot * a.heads * DH)[i] =
-                        make_float4(kQ4Unit * (f * x.x + w * y.x), kQ4Unit * (f * x.y + w * y.y), kQ4Unit * (f * x.z + w * y.z), kQ4Unit * (f * x.w + w * y.w));
-                    if (i % (DH / 4) == 0) reinterpret_cast<float2*>(a.part_ml + slot * a.heads * 2)[h] = make_float2(M, L);
-                }
-                named_bar_sync(1, kWarps * 32);
-            }
+            const size_t slot = (size_t)(unit + blockIdx.x) * a.heads;
+            unit_end(u, s_join, nh, a.part_o + slot * DH, reinterpret_cast<float2*>(a.part_ml) + slot);
         }
     }
     __syncthreads();
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
+constexpr int kRP = 2;
 PagedPlan q4_plan(const PagedDims& d, int Hq) {
     const int G = Hq / d.Hkv, per = ceil_div(G, ceil_div(G, 16)), heads = per <= 8 ? 8 : 16;
-    return paged_plan_of(d, Hq, heads, 6, q4_ctas(heads / 8) * kNumSMs);
+    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads == 8 ? Q4Shape<64, 1, kRP>::kCtas : Q4Shape<64, 2, kRP>::kCtas) * kNumSMs);
 }
 
-template <typename T, int DH, int NG>
+template <typename T, int DH, int NG, bool kBent, bool kMass>
 int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cudaStream_t st) {
-    using S = Q4Shape<DH>;
-    auto kern = paged_attn_q4_kernel<T, DH, NG>;
+    using S = Q4Shape<DH, NG, kRP>;
+    auto kern = paged_attn_q4_kernel<T, DH, NG, kRP, kBent, kMass>;
     METOK_ALLOW_SMEM(kern, S::kRing);
     {
         METOK_TIMED("paged_attn_q4", st);
@@ -465,10 +549,16 @@ int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cu
     METOK_LAUNCH_CHECK();
     return launch_paged_join<T, DH>(a, st);
 }
+template <typename T, int DH>
+int launch_q4_dh(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {
+    const bool bent = a.cap_log2 > 0.f || a.slopes, mass = a.mass != nullptr;
+    if (a.heads > 8) return mass ? launch_q4<T, DH, 2, true, true>(a, k, v, st) : launch_q4<T, DH, 2, true, false>(a, k, v, st);
+    if (bent) return mass ? launch_q4<T, DH, 1, true, true>(a, k, v, st) : launch_q4<T, DH, 1, true, false>(a, k, v, st);
+    return mass ? launch_q4<T, DH, 1, false, true>(a, k, v, st) : launch_q4<T, DH, 1, false, false>(a, k, v, st);
+}
 template <typename T>
 int launch_q4_type(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {
-    if (a.d.dh == 64) return a.heads == 8 ? launch_q4<T, 64, 1>(a, k, v, st) : launch_q4<T, 64, 2>(a, k, v, st);
-    return a.heads == 8 ? launch_q4<T, 128, 1>(a, k, v, st) : launch_q4<T, 128, 2>(a, k, v, st);
+    return a.d.dh == 64 ? launch_q4_dh<T, 64>(a, k, v, st) : launch_q4_dh<T, 128>(a, k, v, st);
 }
 
 }  // namespace
