@@ -30,6 +30,7 @@ struct PagedAttnArgs {
     long long* line;                                   // [n_seqs + 1]: tiles of the sequences before each, per unit; then of all
     int32_t* status;
     int withhold;                                      // debug builds: the copies to leave out
+    int marked;                                        // the first kernel marks partials that met a bad page: a sum below 0
 };
 
 // Tiles of sequence b's one unit (0 for a length out of range, which the second kernel reports).
@@ -92,47 +93,115 @@ __device__ __forceinline__ void next_tile(const PagedAttnArgs& a, Place& p, int 
     }
 }
 
-// The place of tile t_lo: the sequence that holds it is looked for 32 at a time, by every warp for itself where there are no more.  Whole CTA.
-__device__ __forceinline__ Place find_place(const PagedAttnArgs& a, int subs, long long t_lo, long long t_hi, int* s_b, long long* s_start) {
-    const int lane = threadIdx.x & 31;
-    Place p;
-    long long start = 0;
-    p.b = 0;
-    if (threadIdx.x < 32 || a.d.n_seqs <= 32) {
-        long long at = 0;                              // tiles before sequence b0
-        for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
-            const int b = b0 + lane;
-            long long mine = b < a.d.n_seqs ? (long long)unit_tiles(a, b) * subs : 0, incl = mine;
+// a / b of numbers that mostly have 32 bits.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// The tiles of up to 256 sequences, per unit, as a warp's lanes hold them: lane l those of sequences l, l + 32 and so on.
+constexpr int kHeldSeqs = 256;
+struct HeldTiles {
+    uint32_t n[kHeldSeqs / 32], all;
+    __device__ __forceinline__ void load(const PagedAttnArgs& a) {
+        const int lane = threadIdx.x & 31;
+        uint32_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < kHeldSeqs / 32; ++i) {
+            n[i] = 32 * i + lane < a.d.n_seqs ? unit_tiles(a, 32 * i + lane) : 0;
+            sum += n[i];
+        }
+        all = __reduce_add_sync(0xFFFFFFFFu, sum);     // (sequences of 2^24 rows in tiles of 32 at least)
+    }
+    // The place of tile t_lo of the line, which has less than 2^31 of them.
+    __device__ __forceinline__ Place find(int subs, uint32_t t_lo, uint32_t t_hi) const {
+        const int lane = threadIdx.x & 31;
+        Place p;
+        uint32_t at = 0;
+#pragma unroll
+        for (int i = 0; i < kHeldSeqs / 32; ++i) {
+            uint32_t incl = n[i];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
                 if (lane >= o) incl += x;
             }
-            const uint32_t any = __ballot_sync(0xFFFFFFFFu, at + incl > t_lo);
+            const uint32_t any = __ballot_sync(0xFFFFFFFFu, (at + incl) * subs > t_lo);
             if (any) {
                 const int l = __ffs(any) - 1;
-                p.b = b0 + l;
-                start = at + __shfl_sync(0xFFFFFFFFu, incl - mine, l);
-                break;
+                const uint32_t start = (at + __shfl_sync(0xFFFFFFFFu, incl - n[i], l)) * subs;
+                p.b = 32 * i + l;
+                p.nt = (int)__shfl_sync(0xFFFFFFFFu, n[i], l);
+                p.sub = (int)((t_lo - start) / p.nt);
+                p.t = (int)(t_lo - start - (uint32_t)p.sub * p.nt);
+                p.left = t_hi - t_lo;
+                return p;
             }
             at += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
+        return {0, 0, 0, 0, 0};
     }
+};
+
+// The sequence that has tile t_lo, and the tiles before it: looked for 32 sequences at a time.  Whole warp.  N: a type that holds all tiles.
+template <typename N>
+__device__ __forceinline__ int find_sequence(const PagedAttnArgs& a, int subs, N t_lo, N* start) {
+    const int lane = threadIdx.x & 31;
+    N at = 0;                                          // tiles before sequence b0
+    for (int b0 = 0; b0 < a.d.n_seqs; b0 += 32) {
+        const int b = b0 + lane;
+        N mine = b < a.d.n_seqs ? (N)unit_tiles(a, b) * subs : 0, incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const N x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        const uint32_t any = __ballot_sync(0xFFFFFFFFu, at + incl > t_lo);
+        if (any) {
+            const int l = __ffs(any) - 1;
+            *start = at + __shfl_sync(0xFFFFFFFFu, incl - mine, l);
+            return b0 + l;
+        }
+        at += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    *start = 0;
+    return 0;
+}
+__device__ __forceinline__ Place place_in(const PagedAttnArgs& a, int b, long long start, long long t_lo, long long t_hi) {
+    Place p;
+    p.b = b;
+    p.nt = unit_tiles(a, b);
+    const long long in = t_lo - start;
+    p.sub = (int)quotient(in, p.nt);
+    p.t = (int)(in - (long long)p.sub * p.nt);
+    p.left = t_hi - t_lo;
+    return p;
+}
+// The place of tile t_lo of T_all, for a warp.
+__device__ __forceinline__ Place find_tile(const PagedAttnArgs& a, int subs, long long T_all, long long t_lo, long long t_hi) {
+    if (T_all <= 0x7FFFFFFF) {
+        int start;
+        const int b = find_sequence<int>(a, subs, (int)t_lo, &start);
+        return place_in(a, b, start, t_lo, t_hi);
+    }
+    long long start;
+    const int b = find_sequence<long long>(a, subs, t_lo, &start);
+    return place_in(a, b, start, t_lo, t_hi);
+}
+// The same for a whole CTA: up to 32 sequences every warp looks for itself.
+__device__ __forceinline__ Place find_place(const PagedAttnArgs& a, int subs, long long t_lo, long long t_hi, int* s_b, long long* s_start) {
+    long long start = 0;
+    int b = 0;
+    if (threadIdx.x < 32 || a.d.n_seqs <= 32) b = find_sequence<long long>(a, subs, t_lo, &start);
     if (a.d.n_seqs > 32 && threadIdx.x == 0) {
-        *s_b = p.b;
+        *s_b = b;
         *s_start = start;
     }
     __syncthreads();
     if (a.d.n_seqs > 32) {
-        p.b = *s_b;
+        b = *s_b;
         start = *s_start;
     }
-    p.nt = unit_tiles(a, p.b);
-    const long long in = t_lo - start;
-    p.sub = (int)(in / p.nt);
-    p.t = (int)(in - (long long)p.sub * p.nt);
-    p.left = t_hi - t_lo;
-    return p;
+    return place_in(a, b, start, t_lo, t_hi);
 }
 
 // Logit in log2 units of a raw product: scaled, capped, less the distance's share.
@@ -168,7 +237,7 @@ paged_join_kernel(const PagedAttnArgs a) {
     const int row0 = weights ? (((int)blockIdx.x - outs) - b * chunks) * kMassRows : 0;
     // the sequence is sound: only then anything is written for it
     bool ok = len >= 0 && len <= a.d.S_cap();
-    if (ok) {
+    if (ok && !a.marked) {
         const int used = (len + (1 << a.d.page_shift) - 1) >> a.d.page_shift;
         bool there = true;
         for (int p = tid; p < used; p += kJoinThreads) {
@@ -179,11 +248,16 @@ paged_join_kernel(const PagedAttnArgs a) {
     }
     const int nt = unit_tiles(a, b);
     long long all = 0, base = 0;                       // tiles of the line, and of the sequences before b
-    const bool few = a.d.n_seqs <= 32;                 // one look at all lengths; else the line that the first kernel wrote
+    const bool few = a.d.n_seqs <= 256;                // a look at all lengths; else the line that the first kernel wrote
     if (few) {
-        const int mine = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
-        all = (long long)__reduce_add_sync(0xFFFFFFFFu, mine) * subs;
-        base = (long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? mine : 0) * subs;
+        uint32_t sum = 0, before = 0;
+        for (int i = lane; i < a.d.n_seqs; i += 32) {
+            const uint32_t mine = unit_tiles(a, i);
+            sum += mine;
+            before += i < b ? mine : 0;
+        }
+        all = (long long)__reduce_add_sync(0xFFFFFFFFu, sum) * subs;
+        base = (long long)__reduce_add_sync(0xFFFFFFFFu, before) * subs;
     } else {
         grid_dep_wait();
         all = a.line[a.d.n_seqs] * subs;
@@ -212,6 +286,7 @@ paged_join_kernel(const PagedAttnArgs a) {
         const int col = tid % kLanes, run = tid / kLanes;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float M = kLow, L = 0.f;
+        bool bad = false;
         constexpr int kAhead = 6;                      // slots whose loads are on their way
         for (int i0 = run; i0 < sl.n; i0 += kRuns * kAhead) {
             float2 ml[kAhead];
@@ -225,7 +300,10 @@ paged_join_kernel(const PagedAttnArgs a) {
             }
             float top = M;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) top = fmaxf(top, ml[u].x);
+            for (int u = 0; u < kAhead; ++u) {
+                top = fmaxf(top, ml[u].x);
+                bad |= ml[u].y < 0.f;
+            }
             const float less = sm100::fast_exp2(M - top);
             M = top;
             L *= less;
@@ -239,7 +317,10 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         *reinterpret_cast<float4*>(s_acc[tid]) = acc;
         s_ml[tid] = make_float2(M, L);
-        __syncthreads();
+        if (__syncthreads_or(bad)) {
+            if (tid == 0) *a.status = METOK_ERR_INVALID_ARG;
+            return;
+        }
         if (run == 0) {
 #pragma unroll
             for (int r = 1; r < kRuns; ++r) M = fmaxf(M, s_ml[r * kLanes + col].x);
@@ -289,6 +370,7 @@ paged_join_kernel(const PagedAttnArgs a) {
         for (int u = 0; u < kHeads; ++u) v[u] = h0 + u < a.Hq ? x[s_off[h0 + u]] : kLow;
     };
     logits_of(0);
+    bool bad = false;
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
         const int h = h0 + (tid >> 3), part = tid & 7;
         float M = kLow, L = 0.f;
@@ -302,7 +384,10 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) p[u] = i0 + 8 * u < sl.n ? ml[(size_t)(i0 + 8 * u) * a.heads] : make_float2(kLow, 0.f);
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) top = fmaxf(top, p[u].x);
+                for (int u = 0; u < kAhead; ++u) {
+                    top = fmaxf(top, p[u].x);
+                    bad |= p[u].y < 0.f;
+                }
                 L *= sm100::fast_exp2(M - top);
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) L += sm100::fast_exp2(p[u].x - top) * p[u].y;
@@ -317,8 +402,7 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         if (h < a.Hq && part == 0) s_lse[h] = L == 0.f ? 0.f : M + log2f(L);       // (every logit -infinity: weights of 0)
     }
-    __syncthreads();
-    if (row0 + tid >= len) return;
+    if (__syncthreads_or(bad) || row0 + tid >= len) return;              // (the outputs' part reports it)
     float sum = 0.f;
     for (int h = 0; h < a.Hq; h += kHeads) {           // kHeads loads on their way (a loop of single ones would wait for each)
         if (h) logits_of(h);
@@ -377,6 +461,7 @@ inline int paged_attention_args(int dtype, const PagedDims& d, const metok_paged
     a->cap_log2 = softcap * kLog2e;
     a->mass = mass; a->lse = lse; a->status = status;
     a->withhold = debug_withheld();
+    a->marked = 0;
     return METOK_OK;
 }
 // What has to hold before a plan can be made.
@@ -385,12 +470,18 @@ inline int paged_attention_heads(const PagedDims& d, const metok_paged_cache* c,
     if (Hq < 1 || Hq % d.Hkv) return METOK_ERR_INVALID_ARG;
     return Hq > 2048 ? METOK_ERR_UNSUPPORTED : METOK_OK;
 }
+// spread: the first kernel has whole SMs to its CTAs.  The SMs that it leaves first would take all of the second kernel's CTAs, eight or more of them,
+// so these ask for as much shared memory as lets them share the SMs evenly (120 + 120 CTAs on 30 SMs: 10.5 us instead of 6).
 template <typename T, int DH>
-int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st) {
+int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st, bool spread = false) {
     {
         METOK_TIMED("paged_join", st);
         const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
-        const size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
+        size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
+        if (spread) {
+            const long long share = 224 * 1024 / ((blocks + kNumSMs - 1) / kNumSMs) - 5 * 1024;         // (3 KB are static, 1 KB the system's)
+            smem = std::max(smem, (size_t)std::max(share, 0LL));
+        }
         METOK_ALLOW_SMEM((paged_join_kernel<T, DH>), smem);
         launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), smem, st, a);
     }

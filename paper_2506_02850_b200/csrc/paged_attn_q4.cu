@@ -23,19 +23,21 @@ namespace metok {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = (kWarps + 1) * 32;
 // A head's weights are exp2(x - m) with a reference m that was 2^12 below the largest when it was taken; it is taken anew where a weight passes 2^15.5
 // (fp16 ends at 2^16).
 constexpr float kLift = 12.f, kMostWeight = 15.5f;
 
-// RP: pieces of a tile that are one warp's.
+// A CTA has an SM to itself: kGroups groups of kWarps warps, each with a piece of the line, a ring and a warp that fills it.  (As CTAs of their
+// own the groups of an SM end at different times, since its schedulers prefer some warps to others: here no ring may be filled further ahead of
+// the others than by a tile.)  RP: pieces of 16 rows of a tile that are one warp's.
+constexpr int kWarps = 4;
 template <int DH, int NG, int RP>
 struct Q4Shape {
+    static constexpr int kGroups = NG == 1 ? 3 : 2, kThreads = kGroups * (kWarps + 1) * 32;
     static constexpr int kPieces = kWarps * RP, kTile = kQ4Rows * kPieces;
     static constexpr uint32_t kPiece = q4_piece(DH), kHalf = kPieces * kPiece, kStage = 2 * kHalf;     // K, then V
-    static constexpr int kCtas = NG == 1 ? 3 : 2;      // of an SM
     static constexpr int kStages = 55296 / kStage;
-    static constexpr size_t kRing = (size_t)kStages * kStage + 128;
+    static constexpr uint32_t kRing = kStages * kStage;
 };
 
 __device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -164,9 +166,9 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
                                         float newest, const int (&pos)[2 * RP], float* logits, int nh) {
     using S = Q4Shape<DH, NG, RP>;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r0 = row_at(g);
-    float x[RP][NG][4];                                // products, or logits (kBent, kMass)
+    float x[RP][NG][4];                                // products, or logits (kBent)
     auto less = [&](int r, int n, int e) {             // the logit less its reference
-        return kBent || kMass ? x[r][n][e] - u.m[n][e & 1] : fmaf(x[r][n][e], u.scale[n][e & 1], -u.m[n][e & 1]);
+        return kBent ? x[r][n][e] - u.m[n][e & 1] : fmaf(x[r][n][e], u.scale[n][e & 1], -u.m[n][e & 1]);
     };
 #pragma unroll
     for (int r = 0; r < RP; ++r) {
@@ -214,7 +216,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[r][n][e] += y[n][e];
-                if constexpr (kBent || kMass) x[r][n][e] *= u.scale[n][e & 1];
+                if constexpr (kBent) x[r][n][e] *= u.scale[n][e & 1];
             }
     }
     if constexpr (kBent) {
@@ -259,7 +261,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int h = n * 8 + 2 * t + (e & 1), row = r0 + 16 * r + 8 * (e >> 1);
-                    if (h < nh && (!kPart || row < rows)) logits[h * S::kTile + row] = x[r][n][e];
+                    if (h < nh && (!kPart || row < rows)) logits[h * S::kTile + row] = kBent ? x[r][n][e] : x[r][n][e] * u.scale[n][e & 1];
                 }
     }
     float more = kLow;
@@ -284,7 +286,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
                 for (int r = 0; r < RP; ++r) top = fmaxf(top, fmaxf(x[r][n][e], x[r][n][e + 2]));
 #pragma unroll
                 for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-                if (!kBent && !kMass) top *= u.scale[n][e];              // (> 0)
+                if (!kBent) top *= u.scale[n][e];              // (> 0)
                 top = fmaxf(top - kLift, u.m[n][e]);
                 f[e] = sm100::fast_exp2(u.m[n][e] - top);
                 u.l[n][e] *= f[e];
@@ -368,8 +370,8 @@ struct Q4Join {
     float2 ml[kWarps][NG * 8];
 };
 template <int DH, int NG, int QP>
-__device__ __forceinline__ void unit_end(Q4Unit<DH, NG, QP>& u, Q4Join<DH, NG>& j, int nh, float* part_o, float2* part_ml) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+__device__ __forceinline__ void unit_end(Q4Unit<DH, NG, QP>& u, Q4Join<DH, NG>& j, int group, int bad, int nh, float* part_o, float2* part_ml) {
+    const int warp = (threadIdx.x >> 5) % kWarps, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
 #pragma unroll
@@ -381,7 +383,7 @@ __device__ __forceinline__ void unit_end(Q4Unit<DH, NG, QP>& u, Q4Join<DH, NG>& 
             for (int k = 0; k < DH / 16; ++k) j.o[warp][n][k][e][lane] = make_float2(u.o[n][k][e], u.o[n][k][e + 2]);
         }
     }
-    sm100::named_bar_sync(1, kWarps * 32);
+    sm100::named_bar_sync(1 + group, kWarps * 32);
     constexpr int kMine = DH / 16 / kWarps;            // k that are this warp's: 2 kMine elements in a row
 #pragma unroll
     for (int n = 0; n < NG; ++n)
@@ -413,75 +415,110 @@ __device__ __forceinline__ void unit_end(Q4Unit<DH, NG, QP>& u, Q4Join<DH, NG>& 
                 float* dst = part_o + h * DH + DH / 8 * g + 2 * kMine * warp;
                 if constexpr (kMine == 2) *reinterpret_cast<float4*>(dst) = make_float4(o[0].x, o[0].y, o[1].x, o[1].y);
                 else *reinterpret_cast<float2*>(dst) = o[0];
-                if (warp == 0 && g == 0) part_ml[h] = make_float2(M, L);
+                if (warp == 0 && g == 0) part_ml[h] = make_float2(M, bad ? -1.f : L);
             }
         }
-    sm100::named_bar_sync(1, kWarps * 32);
+    sm100::named_bar_sync(1 + group, kWarps * 32);
 }
 
 template <typename T, int DH, int NG, int RP, bool kBent, bool kMass>
-__global__ void __launch_bounds__(kThreads, (Q4Shape<DH, NG, RP>::kCtas))
+__global__ void __launch_bounds__((Q4Shape<DH, NG, RP>::kThreads), 1)
 paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool) {
     using namespace sm100;
     using S = Q4Shape<DH, NG, RP>;
-    constexpr int QP = sizeof(T) == 4 ? 2 : 1;
+    constexpr int QP = sizeof(T) == 4 ? 2 : 1, kGroups = S::kGroups;
     extern __shared__ uint8_t smem_dyn[];
-    __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages];
-    __shared__ Q4Join<DH, NG> s_join;
-    __shared__ long long s_sum[kWarps + 1];
-    __shared__ long long s_start;
-    __shared__ int s_b;
+    __shared__ __align__(8) uint64_t full_bar[kGroups][S::kStages], empty_bar[kGroups][S::kStages];
+    __shared__ long long s_sum[kGroups * (kWarps + 1)];
+    __shared__ volatile int s_filled[kGroups];
+    __shared__ int s_bad[kGroups][S::kStages];
     __shared__ int s_abort;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const bool fills = warp >= kGroups * kWarps;
+    const int group = fills ? warp - kGroups * kWarps : warp / kWarps;
     const int subs = a.d.Hkv * a.NC;
-    uint8_t* const ring = smem_dyn + (((smem_u32(smem_dyn) + 127u) & ~127u) - smem_u32(smem_dyn));
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), kWarps); }
+    uint8_t* const base = smem_dyn + (((smem_u32(smem_dyn) + 127u) & ~127u) - smem_u32(smem_dyn));
+    uint8_t* const ring = base + group * S::kRing;
+    if (fills && lane == 0) {
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&full_bar[group][s]), 1); mbar_init(smem_u32(&empty_bar[group][s]), kWarps); }
+        s_filled[group] = 0;
         s_abort = 0;
         mbar_fence_init();
     }
     grid_dep_wait();
-    if (blockIdx.x == a.grid) {                        // one CTA more than pieces
-        if (warp == 0) write_line(a);
-        return;
-    }
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = METOK_OK;       // a wait that gives up writes it, seconds later
-    const long long T_all = line_tiles(a, s_sum) * subs, ctas = busy_ctas(a, T_all);
-    if (blockIdx.x >= ctas) return;                    // uniform
-    const long long t_lo = T_all * blockIdx.x / ctas, t_hi = T_all * (blockIdx.x + 1) / ctas;
-    Place p = find_place(a, subs, t_lo, t_hi, &s_b, &s_start);
+    // pieces of the line go to the CTAs first, then to their groups
+    const int piece = group * gridDim.x + blockIdx.x;
+    long long t_hi = 0;
+    Place p;
+    p.left = 0;
+    const auto cut = [&](long long T_all) {            // false: the whole CTA has nothing to do
+        const long long busy = busy_ctas(a, T_all);
+        if (blockIdx.x >= busy) {
+            if (blockIdx.x == 0 && warp == 0) write_line(a);
+            return false;
+        }
+        if (piece < busy) {
+            const long long t_lo = quotient(T_all * piece, busy);
+            t_hi = quotient(T_all * (piece + 1), busy);
+            p.left = t_hi - t_lo;
+        } else if (fills && lane == 0) {
+            s_filled[group] = 0x7FFFFFFF;
+        }
+        return true;
+    };
+    if (a.d.n_seqs <= kHeldSeqs) {
+        HeldTiles held;
+        held.load(a);
+        const long long T_all = (long long)held.all * subs;
+        if (!cut(T_all)) return;
+        if (p.left > 0) p = T_all <= 0x7FFFFFFF ? held.find(subs, (uint32_t)(t_hi - p.left), (uint32_t)t_hi) : find_tile(a, subs, T_all, t_hi - p.left, t_hi);
+    } else {
+        const long long T_all = line_tiles(a, s_sum) * subs;
+        if (!cut(T_all)) return;
+        if (p.left > 0) p = find_tile(a, subs, T_all, t_hi - p.left, t_hi);
+    }
+    __syncthreads();
     volatile int* abort_flag = &s_abort;
 
-    if (warp == kWarps) {                              // brings the tiles
+    if (fills) {
         const int per_page = 1 << (a.d.page_shift - 4), run = min(per_page, S::kPieces);   // pieces of a page that are a copy
         int it = 0;
         for (; p.left > 0; ++it) {
-            const int s = it % S::kStages;
-            if (!mbar_wait_warp(smem_u32(&empty_bar[s]), ((uint32_t)(it / S::kStages) & 1u) ^ 1u, abort_flag)) break;
-            const int r0 = p.t * S::kTile, rows = min(S::kTile, a.kv_len[p.b] - r0), pieces = (rows + kQ4Rows - 1) / kQ4Rows;
-            const uint32_t fb = smem_u32(&full_bar[s]);
+            const int s = it % S::kStages, r0 = p.t * S::kTile, rows = min(S::kTile, a.kv_len[p.b] - r0), pieces = (rows + kQ4Rows - 1) / kQ4Rows;
+            const int pc = (lane >> 1) * run, n = min(run, pieces - pc), row = r0 + pc * kQ4Rows;
+            int page = n > 0 ? a.block_table[(size_t)p.b * a.d.max_pages + (row >> a.d.page_shift)] : 0;
+            if (!mbar_wait_warp(smem_u32(&empty_bar[group][s]), ((uint32_t)(it / S::kStages) & 1u) ^ 1u, abort_flag)) break;
+            uint32_t polls = 0;
+            for (int g = 0; g < kGroups; ++g)
+                while (s_filled[g] < it - 1 && polls < kWaitLimit && !((++polls & 255u) == 0 && *abort_flag)) {}
+            const uint32_t fb = smem_u32(&full_bar[group][s]);
+            // (debug builds: one copy never sent)
+            const bool bad = __any_sync(0xFFFFFFFFu, n > 0 && (page < 0 || page >= a.d.n_pages));
+            if (lane == 0) s_bad[group][s] = bad;      // the tile's partial is marked, and the second kernel drops the sequence
+            __syncwarp();
             if (lane == 0) mbar_arrive_expect_tx(fb, 2u * pieces * S::kPiece);
             __syncwarp();
-            const int pc = (lane >> 1) * run, n = min(run, pieces - pc);
-            // (debug builds: one copy never sent)
-            if (n > 0 && !(dbg_held(a.withhold, kDbgPagedAttn) && blockIdx.x == 0 && it == 0 && lane == 0)) {
-                const int row = r0 + pc * kQ4Rows;
-                int page = a.block_table[(size_t)p.b * a.d.max_pages + (row >> a.d.page_shift)];
-                if (page < 0 || page >= a.d.n_pages) page = 0;          // the second kernel drops the sequence
+            if (n > 0 && !(dbg_held(a.withhold, kDbgPagedAttn) && blockIdx.x == 0 && group == 0 && it == 0 && lane == 0)) {
+                if (bad) page = 0;
                 const size_t at = q4_piece_of(a.d, page, p.sub / a.NC, row) * S::kPiece;
                 bulk_load(smem_u32(ring) + s * S::kStage + (lane & 1) * S::kHalf + pc * S::kPiece, ((lane & 1) ? v_pool : k_pool) + at,
                           (uint32_t)n * S::kPiece, fb);
             }
             __syncwarp();
+            if (lane == 0) s_filled[group] = it + 1;
             next_tile(a, p, subs);
         }
+        if (lane == 0) s_filled[group] = 0x7FFFFFFF;
+        if (blockIdx.x == 0 && group == 0 && a.d.n_seqs > kHeldSeqs) write_line(a);
         // all copies have landed before the shared memory goes away
         for (int back = 1; back <= S::kStages && back <= it; ++back) {
             const int j = it - back;
-            mbar_wait_warp(smem_u32(&full_bar[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u, abort_flag);
+            mbar_wait_warp(smem_u32(&full_bar[group][j % S::kStages]), (uint32_t)(j / S::kStages) & 1u, abort_flag);
         }
     } else {
-        const int mine = warp * RP * kQ4Rows;
+        const int mine = warp % kWarps * RP * kQ4Rows;
+        Q4Join<DH, NG>& join = reinterpret_cast<Q4Join<DH, NG>*>(base + kGroups * S::kRing)[group];
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -493,7 +530,7 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
             const float newest = kBent && a.slopes ? (float)(pos ? pos[len - 1] : len - 1) : 0.f;
             float* logits = kMass ? a.logits + (size_t)(t_hi - p.left) * a.heads * S::kTile + mine : nullptr;
             u.template start<T>(a, p.b, h0, nh);
-            int first = p.t * S::kTile + mine;         // the warp's first row of the tile
+            int first = p.t * S::kTile + mine, bad = 0;    // the warp's first row of the tile
             for (int n = 0; n < tiles; ++n) {
                 // positions of the rows that this lane's logits are of: they are not wanted before the products are there
                 int at[2 * RP] = {};
@@ -504,13 +541,14 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
                         if (pos) at[i] = pos[at[i]];
                     }
                 }
-                if (ok && !mbar_wait_warp(smem_u32(&full_bar[stage]), phase, abort_flag)) ok = false;
+                if (ok && !mbar_wait_warp(smem_u32(&full_bar[group][stage]), phase, abort_flag)) ok = false;
                 if (ok) {
-                    const uint8_t* k = ring + stage * S::kStage + warp * RP * S::kPiece;
+                    const uint8_t* k = ring + stage * S::kStage + warp % kWarps * RP * S::kPiece;
+                    bad |= s_bad[group][stage];
                     if (first + kQ4Rows * RP <= len) q4_tile<DH, NG, QP, RP, kBent, kMass, false>(u, a, k, k + S::kHalf, 0, newest, at, logits, nh);
                     else if (first < len) q4_tile<DH, NG, QP, RP, kBent, kMass, true>(u, a, k, k + S::kHalf, len - first, newest, at, logits, nh);
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&empty_bar[stage]));
+                    if (lane == 0) mbar_arrive(smem_u32(&empty_bar[group][stage]));
                 }
                 if (++stage == S::kStages) {
                     stage = 0;
@@ -523,8 +561,8 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
             p.t += tiles - 1;
             p.left -= tiles - 1;
             next_tile(a, p, subs);
-            const size_t slot = (size_t)(unit + blockIdx.x) * a.heads;
-            unit_end(u, s_join, nh, a.part_o + slot * DH, reinterpret_cast<float2*>(a.part_ml) + slot);
+            const size_t slot = (size_t)(unit + piece) * a.heads;
+            unit_end(u, join, group, bad, nh, a.part_o + slot * DH, reinterpret_cast<float2*>(a.part_ml) + slot);
         }
     }
     __syncthreads();
@@ -534,20 +572,22 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
 constexpr int kRP = 2;
 PagedPlan q4_plan(const PagedDims& d, int Hq) {
     const int G = Hq / d.Hkv, per = ceil_div(G, ceil_div(G, 16)), heads = per <= 8 ? 8 : 16;
-    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads == 8 ? Q4Shape<64, 1, kRP>::kCtas : Q4Shape<64, 2, kRP>::kCtas) * kNumSMs);
+    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads == 8 ? Q4Shape<64, 1, kRP>::kGroups : Q4Shape<64, 2, kRP>::kGroups) * kNumSMs);
 }
 
 template <typename T, int DH, int NG, bool kBent, bool kMass>
 int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cudaStream_t st) {
     using S = Q4Shape<DH, NG, kRP>;
     auto kern = paged_attn_q4_kernel<T, DH, NG, kRP, kBent, kMass>;
-    METOK_ALLOW_SMEM(kern, S::kRing);
+    constexpr size_t smem = S::kGroups * (S::kRing + sizeof(Q4Join<DH, NG>)) + 128;
+    static_assert(smem <= 226 * 1024, "shared memory of an SM");
+    METOK_ALLOW_SMEM(kern, smem);
     {
         METOK_TIMED("paged_attn_q4", st);
-        launch_chained(kern, dim3(a.grid + 1), dim3(kThreads), S::kRing, st, a, (const uint8_t*)k_pool, (const uint8_t*)v_pool);
+        launch_chained(kern, dim3(std::min(a.grid, kNumSMs)), dim3(S::kThreads), smem, st, a, (const uint8_t*)k_pool, (const uint8_t*)v_pool);
     }
     METOK_LAUNCH_CHECK();
-    return launch_paged_join<T, DH>(a, st);
+    return launch_paged_join<T, DH>(a, st, a.grid >= kNumSMs);
 }
 template <typename T, int DH>
 int launch_q4_dh(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {
@@ -589,6 +629,7 @@ extern "C" int metok_paged_attention_q4(int dtype, const metok_paged_cache* c, c
     rc = paged_attention_args(dtype, d, c, p, q, q_seq, q_head, Hq, softmax_scale, softcap, slopes, positions, mass, out, out_seq, out_head, lse,
                               status, &a);
     if (rc != METOK_OK) return rc;
+    a.marked = 1;
     if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_q4_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     Carver cv(ws);
     paged_carve(cv, p, d, mass != nullptr, &a);
