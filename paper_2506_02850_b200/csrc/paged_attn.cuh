@@ -219,20 +219,21 @@ __device__ __forceinline__ Slots unit_slots(const PagedAttnArgs& a, long long al
     return {unit + c0, (int)(c1 - c0) + 1};
 }
 
-// Joins the partials.  CTAs [0, n_seqs * Hq): one head's output and lse; the others: the weights of kMassRows rows of a sequence.
-constexpr int kJoinThreads = 128, kMassRows = 128;
-template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinThreads)
+// Joins the partials.  The first CTAs: one head's output and lse each, or (kUnits: few partials) those of a unit; the others: the weights of NT rows
+// of a sequence.  NT: threads.
+template <typename T, int DH, int NT, bool kUnits>
+__global__ void __launch_bounds__(NT)
 paged_join_kernel(const PagedAttnArgs a) {
+    constexpr int kJoinThreads = NT, kMassRows = NT;
     // Up to the wait: what needs only the call's inputs, which were complete when the first kernel was let go.
     __shared__ __align__(16) float s_acc[kJoinThreads][4];
     __shared__ float2 s_ml[kJoinThreads];
     extern __shared__ __align__(16) uint8_t s_dyn[];
     const int tid = threadIdx.x, lane = tid & 31;
-    const int outs = a.d.n_seqs * a.Hq;
+    const int outs = a.d.n_seqs * (kUnits ? a.d.Hkv * a.NC : a.Hq);
     const bool weights = (int)blockIdx.x >= outs;
     const int chunks = (a.d.S_cap() + kMassRows - 1) / kMassRows;
-    const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / a.Hq;
+    const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / (outs / a.d.n_seqs);
     const int len = a.kv_len[b], subs = a.d.Hkv * a.NC;
     const int row0 = weights ? (((int)blockIdx.x - outs) - b * chunks) * kMassRows : 0;
     // the sequence is sound: only then anything is written for it
@@ -270,7 +271,61 @@ paged_join_kernel(const PagedAttnArgs a) {
         return ok;
     };
 
-    if (!weights) {
+    if constexpr (kUnits) {
+        if (!weights) {
+            // a thread has four elements of a head, of all partials
+            constexpr int kLanes = DH / 4, kAhead = 6;
+            const int sub = (int)blockIdx.x - b * subs, hk = sub / a.NC, ch = sub - hk * a.NC, nh = min(a.heads, a.G - ch * a.heads);
+            const Slots sl = nt ? unit_slots(a, all, (long long)b * subs + sub, base + (long long)sub * nt, nt) : Slots{0, 0};
+            if (!sound()) return;
+            const int col = tid % kLanes;
+            for (int hl = tid / kLanes; hl < nh; hl += NT / kLanes) {
+                const int h = hk * a.G + ch * a.heads + hl;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float M = kLow, L = 0.f;
+                bool bad = false;
+                for (int i0 = 0; i0 < sl.n; i0 += kAhead) {
+                    float2 ml[kAhead];
+                    float4 o[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const size_t at = (size_t)(sl.first + i0 + u) * a.heads + hl;
+                        const bool in = i0 + u < sl.n;
+                        ml[u] = in ? *reinterpret_cast<const float2*>(a.part_ml + at * 2) : make_float2(kLow, 0.f);
+                        o[u] = in ? reinterpret_cast<const float4*>(a.part_o + at * DH)[col] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    float top = M;
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        top = fmaxf(top, ml[u].x);
+                        bad |= ml[u].y < 0.f;
+                    }
+                    const float less = sm100::fast_exp2(M - top);
+                    M = top;
+                    L *= less;
+                    acc.x *= less; acc.y *= less; acc.z *= less; acc.w *= less;
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const float f = sm100::fast_exp2(ml[u].x - M);
+                        L += f * ml[u].y;
+                        acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
+                    }
+                }
+                if (bad) {
+                    *a.status = METOK_ERR_INVALID_ARG;
+                    continue;
+                }
+                T* out = reinterpret_cast<T*>(a.out) + b * a.out_seq + h * a.out_head + col * 4;
+                const float inv = L == 0.f ? 0.f : 1.f / L;              // 0: no rows, or every logit is -infinity
+                from_float(out[0], acc.x * inv);
+                from_float(out[1], acc.y * inv);
+                from_float(out[2], acc.z * inv);
+                from_float(out[3], acc.w * inv);
+                if (col == 0 && a.lse) a.lse[(size_t)b * a.Hq + h] = nt ? kLn2 * (M + log2f(L)) : __int_as_float(0xFF800000);
+            }
+            return;
+        }
+    } else if (!weights) {
         const int h = (int)blockIdx.x - b * a.Hq, hk = h / a.G, g = h - hk * a.G, ch = g / a.heads, hl = g - ch * a.heads;
         T* out = reinterpret_cast<T*>(a.out) + b * a.out_seq + h * a.out_head;
         const int sub = hk * a.NC + ch;
@@ -412,6 +467,8 @@ paged_join_kernel(const PagedAttnArgs a) {
     a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
 }
 
+constexpr int kLeastMassRows = 128;                    // rows of a CTA of the second kernel
+
 // How the heads of a K/V head are dealt to units, and the line to CTAs.
 struct PagedPlan {
     int G, heads, NC, grid, tile_shift;
@@ -450,7 +507,7 @@ inline int paged_attention_args(int dtype, const PagedDims& d, const metok_paged
     if (q_seq < 0 || q_head < 0 || out_seq < 0 || out_head < 0 || (q_seq | q_head | out_seq | out_head) % per) return METOK_ERR_INVALID_ARG;
     // outputs of different heads and sequences do not overlap
     if (!rows_apart(d.n_seqs, out_seq, Hq, out_head, d.dh) || !softmax_numbers(softmax_scale, softcap)) return METOK_ERR_INVALID_ARG;
-    const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kMassRows - 1) / kMassRows) : 0);
+    const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kLeastMassRows - 1) / kLeastMassRows) : 0);
     if (join > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     a->d = d;
     a->Hq = Hq; a->G = p.G; a->NC = p.NC; a->heads = p.heads; a->grid = p.grid; a->tile_shift = p.tile_shift;
@@ -472,18 +529,18 @@ inline int paged_attention_heads(const PagedDims& d, const metok_paged_cache* c,
 }
 // spread: the first kernel has whole SMs to its CTAs.  The SMs that it leaves first would take all of the second kernel's CTAs, eight or more of them,
 // so these ask for as much shared memory as lets them share the SMs evenly (120 + 120 CTAs on 30 SMs: 10.5 us instead of 6).
-template <typename T, int DH>
+template <typename T, int DH, int NT, bool kUnits>
 int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st, bool spread = false) {
     {
         METOK_TIMED("paged_join", st);
-        const long long blocks = (long long)a.d.n_seqs * a.Hq + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
+        const long long blocks = (long long)a.d.n_seqs * (kUnits ? a.d.Hkv * a.NC : a.Hq) + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + NT - 1) / NT) : 0);
         size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
         if (spread) {
-            const long long share = 224 * 1024 / ((blocks + kNumSMs - 1) / kNumSMs) - 5 * 1024;         // (3 KB are static, 1 KB the system's)
+            const long long share = 224 * 1024 / ((blocks + kNumSMs - 1) / kNumSMs) - 8 * 1024;         // (6 KB are static, 1 KB the system's)
             smem = std::max(smem, (size_t)std::max(share, 0LL));
         }
-        METOK_ALLOW_SMEM((paged_join_kernel<T, DH>), smem);
-        launch_chained(paged_join_kernel<T, DH>, dim3((unsigned)blocks), dim3(kJoinThreads), smem, st, a);
+        METOK_ALLOW_SMEM((paged_join_kernel<T, DH, NT, kUnits>), smem);
+        launch_chained(paged_join_kernel<T, DH, NT, kUnits>, dim3((unsigned)blocks), dim3(NT), smem, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;

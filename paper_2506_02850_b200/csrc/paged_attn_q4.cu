@@ -147,16 +147,18 @@ struct Q4Unit {
 __device__ __forceinline__ int row_at(int r) { return r ^ (r >> 2 & 1); }          // pi: the row at place r of eight
 
 // tanh(y) of logits in units of the cap, |y| <= 1: y P(y^2), P the polynomial of degree 6 of least largest relative error (5e-8; 1.6e-7 in fp32).
-__device__ __forceinline__ float tanh_near(float y) {
-    const float u = y * y;
-    float t = 0.0010410226f;
-    t = fmaf(t, u, -0.00620337902f);
-    t = fmaf(t, u, 0.0202899799f);
-    t = fmaf(t, u, -0.0534570292f);
-    t = fmaf(t, u, 0.13325204f);
-    t = fmaf(t, u, -0.333328396f);
-    t = fmaf(t, u, 0.99999994f);
-    return y * t;
+__device__ __forceinline__ uint64_t tanh_near(uint64_t y) {
+    using namespace sm100;
+    const auto both = [](float c) { return pair(c, c); };
+    const uint64_t u = mul_pair(y, y);
+    uint64_t t = both(0.0010410226f);
+    t = fma_pair(t, u, both(-0.00620337902f));
+    t = fma_pair(t, u, both(0.0202899799f));
+    t = fma_pair(t, u, both(-0.0534570292f));
+    t = fma_pair(t, u, both(0.13325204f));
+    t = fma_pair(t, u, both(-0.333328396f));
+    t = fma_pair(t, u, both(0.99999994f));
+    return mul_pair(y, t);
 }
 
 // The warp's RP pieces of a tile, of whose rows `rows` are there (kPart: not all; >= 1).  kBent: logits are capped or biased; `pos`: positions of the
@@ -166,9 +168,13 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
                                         float newest, const int (&pos)[2 * RP], float* logits, int nh) {
     using S = Q4Shape<DH, NG, RP>;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r0 = row_at(g);
+    using namespace sm100;
     float x[RP][NG][4];                                // products, or logits (kBent)
-    auto less = [&](int r, int n, int e) {             // the logit less its reference
-        return kBent ? x[r][n][e] - u.m[n][e & 1] : fmaf(x[r][n][e], u.scale[n][e & 1], -u.m[n][e & 1]);
+    const auto two = [](const float* v) { return pair(v[0], v[1]); };    // the lane's two heads
+    uint64_t low[NG];
+    auto less = [&](int r, int n, int i, float (&d)[2]) {                // logits of row i less their references
+        const uint64_t v = two(&x[r][n][2 * i]);
+        unpair(kBent ? add_pair(v, low[n]) : fma_pair(v, two(u.scale[n]), low[n]), d[0], d[1]);
     };
 #pragma unroll
     for (int r = 0; r < RP; ++r) {
@@ -214,9 +220,10 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
         for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[r][n][e] += y[n][e];
-                if constexpr (kBent) x[r][n][e] *= u.scale[n][e & 1];
+            for (int i = 0; i < 4; i += 2) {
+                uint64_t v = add_pair(two(&x[r][n][i]), two(&y[n][i]));
+                if constexpr (kBent) v = mul_pair(v, two(u.scale[n]));
+                unpair(v, x[r][n][i], x[r][n][i + 1]);
             }
     }
     if constexpr (kBent) {
@@ -241,7 +248,8 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
                     for (int n = 0; n < NG; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[r][n][e] = a.cap_log2 * tanh_near(x[r][n][e]);
+                        for (int i = 0; i < 4; i += 2)
+                            unpair(mul_pair(tanh_near(two(&x[r][n][i])), pair(a.cap_log2, a.cap_log2)), x[r][n][i], x[r][n][i + 1]);
             }
         }
         if (a.slopes) {
@@ -266,14 +274,18 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
     }
     float more = kLow;
 #pragma unroll
+    for (int n = 0; n < NG; ++n) low[n] = pair(-u.m[n][0], -u.m[n][1]);
+#pragma unroll
     for (int r = 0; r < RP; ++r)
 #pragma unroll
         for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int i = 0; i < 2; ++i) {
                 // rows that are not there have no weight
-                if (kPart && r0 + 16 * r + 8 * (e >> 1) >= rows) x[r][n][e] = __int_as_float(0xFF800000);
-                more = fmaxf(more, less(r, n, e));
+                if (kPart && r0 + 16 * r + 8 * i >= rows) x[r][n][2 * i] = x[r][n][2 * i + 1] = __int_as_float(0xFF800000);
+                float d[2];
+                less(r, n, i, d);
+                more = fmaxf(more, fmaxf(d[0], d[1]));
             }
     if (__any_sync(0xFFFFFFFFu, more > kMostWeight)) {
 #pragma unroll
@@ -296,6 +308,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
             for (int k = 0; k < DH / 16; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) u.o[n][k][e] *= f[e & 1];
+            low[n] = pair(-u.m[n][0], -u.m[n][1]);
         }
     }
     uint32_t p16[RP][QP][NG][2];
@@ -305,9 +318,13 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
         for (int n = 0; n < NG; ++n) {
             float p[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = sm100::fast_exp2(less(r, n, e));
-            u.l[n][0] += p[0] + p[2];
-            u.l[n][1] += p[1] + p[3];
+            for (int i = 0; i < 2; ++i) {
+                float d[2];
+                less(r, n, i, d);
+                p[2 * i] = fast_exp2(d[0]);
+                p[2 * i + 1] = fast_exp2(d[1]);
+            }
+            unpair(add_pair(two(u.l[n]), add_pair(two(p), two(p + 2))), u.l[n][0], u.l[n][1]);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const __half2 hi = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
@@ -587,7 +604,10 @@ int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cu
         launch_chained(kern, dim3(std::min(a.grid, kNumSMs)), dim3(S::kThreads), smem, st, a, (const uint8_t*)k_pool, (const uint8_t*)v_pool);
     }
     METOK_LAUNCH_CHECK();
-    return launch_paged_join<T, DH>(a, st, a.grid >= kNumSMs);
+    // a unit's partials are few where the units are many: a CTA joins all of its heads
+    if (a.grid < kNumSMs) return launch_paged_join<T, DH, 128, false>(a, st);
+    const bool few = (long long)a.d.n_seqs * a.d.Hkv * a.NC * 8 >= a.grid;
+    return few ? launch_paged_join<T, DH, 256, true>(a, st, true) : launch_paged_join<T, DH, 256, false>(a, st, true);
 }
 template <typename T, int DH>
 int launch_q4_dh(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {

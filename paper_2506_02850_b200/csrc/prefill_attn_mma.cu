@@ -101,11 +101,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // 2^x on the FMA pipe (exp2_fma_pair): arguments outside [-125, 128] are held there.  2^-125 is taken off (rounded away beside what
 // counts), so that a hidden key's weight is 0 and its V, however large, adds nothing.  At 128 the exponent's bits are those of +infinity:
 // a NaN is held there too (a minimum takes the number of the two), and a sum of weights that is not finite is a row's sign of one.

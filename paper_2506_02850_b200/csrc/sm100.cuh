@@ -257,6 +257,11 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // 2^x of both halves on the special-function unit.
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
     float a, b;
