@@ -1,8 +1,6 @@
-// metok_paged_append and metok_paged_evict: rows into a paged K/V cache, and out of it by accumulated attention weight; the same for a cache
-// held in 4 bits, and metok_paged_read_q4, which brings its rows back.
+// metok_paged_append and metok_paged_evict: rows into a paged K/V cache, and out of it by accumulated attention weight.
 #include "launchers.h"
 #include "paged.cuh"
-#include "q4.cuh"
 
 namespace metok {
 
@@ -13,7 +11,7 @@ namespace {
 // one warp's work, one of 40 fp32 heads that of twenty, so that a step of few rows still fills the SMs.  Reads and writes are
 // contiguous pieces of dh elements; what bounds a long call is HBM (53 650 rows of 4 heads of 128: 42 us, 5.2 TB/s), a step's call its launch
 // and three round trips (the offsets and lengths, the page, the copy): 6 us.
-constexpr int kAppendWarps = 8, kAppendChunks = 4, kHoldBlocks = 2;
+constexpr int kAppendWarps = 8, kAppendChunks = 4;
 
 struct AppendArgs {
     PagedDims d;
@@ -47,65 +45,6 @@ __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ offsets, 
     return lo;
 }
 
-// New row i to row `row` of a sequence, in the page `page`: a warp's part of it.
-struct CopyRows {
-    static __device__ __forceinline__ void row(const AppendArgs& a, int page, int row, int i, int part, int lane) {
-        const int cpr = a.d.row_chunks, half = a.d.Hkv * cpr;
-        uint4* to[kAppendChunks];
-        uint4 v[kAppendChunks];
-#pragma unroll
-        for (int u = 0; u < kAppendChunks; ++u) {
-            int e = part * (32 * kAppendChunks) + u * 32 + lane;
-            to[u] = nullptr;
-            if (e >= 2 * half) continue;
-            const bool is_v = e >= half;
-            if (is_v) e -= half;
-            const int h = e / cpr, c = e - h * cpr;
-            to[u] = (is_v ? a.v_pool : a.k_pool) + paged_chunk(a.d, page, h, row) + c;
-            v[u] = __ldg(is_v ? a.v_new + h * a.v_head + i * a.v_row + c : a.k_new + h * a.k_head + i * a.k_row + c);
-        }
-#pragma unroll
-        for (int u = 0; u < kAppendChunks; ++u)
-            if (to[u]) *to[u] = v[u];
-    }
-};
-// The same into a cache held in 4 bits: a lane takes blocks of 16 elements.
-template <typename T>
-struct HoldRows {
-    static __device__ __forceinline__ void row(const AppendArgs& a, int page, int row, int i, int part, int lane) {
-        constexpr int kChunks = sizeof(T);             // 16-byte chunks of a block
-        const int dh = a.d.dh, bpr = dh / 16, half = a.d.Hkv * bpr, at = row & 15;
-        uint4 v[kHoldBlocks][kChunks];
-        uint8_t* to[kHoldBlocks];
-        int blk[kHoldBlocks];
-#pragma unroll
-        for (int u = 0; u < kHoldBlocks; ++u) {
-            int e = part * (32 * kHoldBlocks) + u * 32 + lane;
-            to[u] = nullptr;
-            if (e >= 2 * half) continue;
-            const bool is_v = e >= half;
-            if (is_v) e -= half;
-            const int h = e / bpr;
-            blk[u] = e - h * bpr;
-            to[u] = reinterpret_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + q4_piece_of(a.d, page, h, row) * q4_piece(dh);
-            const uint4* from = (is_v ? a.v_new + h * a.v_head + i * a.v_row : a.k_new + h * a.k_head + i * a.k_row) + blk[u] * kChunks;
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) v[u][j] = __ldg(from + j);
-        }
-#pragma unroll
-        for (int u = 0; u < kHoldBlocks; ++u) {
-            if (!to[u]) continue;
-            float x[16];
-            q4_widen<T>(v[u], x);
-            uint32_t code[2];
-            const uint32_t scale = q4_hold(x, code);
-            *reinterpret_cast<uint2*>(to[u] + at * (dh / 2) + blk[u] * 8) = make_uint2(code[0], code[1]);
-            to[u][8 * dh + at * bpr + blk[u]] = (uint8_t)scale;
-        }
-    }
-};
-
-template <typename Copy>
 __global__ void __launch_bounds__(kAppendWarps * 32)
 paged_append_kernel(const AppendArgs a) {
     grid_dep_wait();
@@ -159,114 +98,29 @@ paged_append_kernel(const AppendArgs a) {
     const int row = len + (i - lo);
     const int page = a.block_table[(size_t)b * a.d.max_pages + (row >> a.d.page_shift)];
     if (page < 0 || page >= a.d.n_pages) return;
-    Copy::row(a, page, row, i, part, lane);
+    const int cpr = a.d.row_chunks, half = a.d.Hkv * cpr;
+    uint4* to[kAppendChunks];
+    uint4 v[kAppendChunks];
+#pragma unroll
+    for (int u = 0; u < kAppendChunks; ++u) {
+        int e = part * (32 * kAppendChunks) + u * 32 + lane;
+        to[u] = nullptr;
+        if (e >= 2 * half) continue;
+        const bool is_v = e >= half;
+        if (is_v) e -= half;
+        const int h = e / cpr, c = e - h * cpr;
+        to[u] = (is_v ? a.v_pool : a.k_pool) + paged_chunk(a.d, page, h, row) + c;
+        v[u] = __ldg(is_v ? a.v_new + h * a.v_head + i * a.v_row + c : a.k_new + h * a.k_head + i * a.k_row + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendChunks; ++u)
+        if (to[u]) *to[u] = v[u];
     if (part == 0 && lane == 0) {
         if (a.positions) {
             int32_t* pos = a.positions + (size_t)b * S_cap;
             pos[row] = a.pos_new ? a.pos_new[i] : (len > 0 ? pos[len - 1] + 1 : 0) + (i - lo);
         }
         if (a.mass) a.mass[(size_t)b * S_cap + row] = a.mass_new ? a.mass_new[i] : 0.f;
-    }
-}
-
-// ---- rows of a cache held in 4 bits, as they were -------------------------------------
-// A CTA takes 32 packed rows: its first warp finds where each lies, then a thread takes blocks of 16 elements, kReadBlocks on their way, a
-// head's rows after one another so that a warp's loads and stores are 256 and 1024 bytes in one piece.  What bounds it is HBM, the writes above all.
-constexpr int kReadThreads = 256, kReadRows = 32, kReadBlocks = 4;
-struct ReadArgs {
-    PagedDims d;
-    const uint8_t *k_pool, *v_pool;
-    uint4 *k_out, *v_out;
-    long long k_head, k_row, v_head, v_row;            // in 16-byte chunks
-    int n_rows;
-    const int32_t *block_table, *kv_len, *offsets, *first_row, *positions;
-    int32_t *pos_out, *status;
-};
-
-template <typename T>
-__global__ void __launch_bounds__(kReadThreads)
-paged_read_q4_kernel(const ReadArgs a) {
-    __shared__ int s_page[kReadRows], s_row[kReadRows];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, S_cap = a.d.S_cap(), n = a.d.n_seqs;
-    grid_dep_wait();
-    // offsets that descend anywhere: nothing is written
-    int down = 0;
-    for (int s = tid; s < n; s += kReadThreads) down |= a.offsets[s + 1] < a.offsets[s];
-    const bool none = __syncthreads_or(down);
-    if (blockIdx.x == 0) {                             // the first CTA checks the sequences
-        int bad = none;
-        for (int b = warp; b < n && !none; b += kReadThreads / 32) {
-            const int lo = a.offsets[b], hi = a.offsets[b + 1], first = a.first_row ? a.first_row[b] : 0, len = a.kv_len[b];
-            bool ok = lo >= 0 && hi <= a.n_rows && len >= 0 && len <= S_cap && first >= 0 && first <= len && hi - lo <= len - first;
-            if (ok && hi > lo) {
-                const int p1 = (first + hi - lo - 1) >> a.d.page_shift;
-                bool there = true;
-                for (int p = (first >> a.d.page_shift) + lane; p <= p1; p += 32) {
-                    const int page = a.block_table[(size_t)b * a.d.max_pages + p];
-                    there &= page >= 0 && page < a.d.n_pages;
-                }
-                ok = __all_sync(0xFFFFFFFFu, there);
-            }
-            bad |= !ok;
-        }
-        bad = __syncthreads_or(bad);
-        if (tid == 0) *a.status = bad ? METOK_ERR_INVALID_ARG : METOK_OK;
-        return;
-    }
-    if (none) return;
-    const int i0 = (blockIdx.x - 1) * kReadRows;
-    if (warp == 0) {
-        const int i = i0 + lane;
-        int page = -1, row = 0;
-        if (i < a.n_rows) {
-            int lo = 0, hi = n;                        // the number of offsets[1 .. n] that are <= i: the row's sequence, n for none
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (a.offsets[1 + mid] <= i) lo = mid + 1;
-                else hi = mid;
-            }
-            if (lo < n) {
-                const int o0 = a.offsets[lo], o1 = a.offsets[lo + 1], first = a.first_row ? a.first_row[lo] : 0, len = a.kv_len[lo];
-                if (i >= o0 && o0 >= 0 && o1 <= a.n_rows && len >= 0 && len <= S_cap && first >= 0 && first <= len && o1 - o0 <= len - first) {
-                    row = first + (i - o0);
-                    page = a.block_table[(size_t)lo * a.d.max_pages + (row >> a.d.page_shift)];
-                    if (page < 0 || page >= a.d.n_pages) page = -1;
-                    else if (a.pos_out) a.pos_out[i] = a.positions[(size_t)lo * S_cap + row];
-                }
-            }
-        }
-        s_page[lane] = page;
-        s_row[lane] = row;
-    }
-    __syncthreads();
-    constexpr int kChunks = sizeof(T);                 // 16-byte chunks of a block
-    const int dh = a.d.dh, shift = dh == 128 ? 3 : 2, per_head = kReadRows << shift, items = 2 * a.d.Hkv * per_head;
-    for (int e0 = tid; e0 < items; e0 += kReadThreads * kReadBlocks) {
-        uint2 code[kReadBlocks];
-        uint32_t scale[kReadBlocks];
-        uint4* to[kReadBlocks];
-#pragma unroll
-        for (int u = 0; u < kReadBlocks; ++u) {
-            const int e = e0 + u * kReadThreads, blk = e & ((1 << shift) - 1), r = (e >> shift) & (kReadRows - 1), hh = e / per_head;
-            to[u] = nullptr;
-            if (e >= items || s_page[r] < 0) continue;
-            const bool is_v = hh >= a.d.Hkv;
-            const int h = is_v ? hh - a.d.Hkv : hh, row = s_row[r], at = row & 15;
-            const uint8_t* piece = (is_v ? a.v_pool : a.k_pool) + q4_piece_of(a.d, s_page[r], h, row) * q4_piece(dh);
-            code[u] = __ldg(reinterpret_cast<const uint2*>(piece + at * (dh / 2) + blk * 8));
-            scale[u] = __ldg(piece + 8 * dh + (at << shift) + blk);
-            to[u] = (is_v ? a.v_out + h * a.v_head + (long long)(i0 + r) * a.v_row : a.k_out + h * a.k_head + (long long)(i0 + r) * a.k_row) + blk * kChunks;
-        }
-#pragma unroll
-        for (int u = 0; u < kReadBlocks; ++u) {
-            if (!to[u]) continue;
-            float x[16];
-            q4_stands_for(code[u], scale[u], x);
-            uint4 v[kChunks];
-            q4_narrow<T>(x, v);
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) to[u][j] = v[j];
-        }
     }
 }
 
@@ -605,14 +459,12 @@ evict_move_q4_kernel(const EvictArgs a, const EvictPools pools, int layer0) {
 
 using namespace metok;
 
-namespace {
-// What both appends do: dtype is that of the new rows; q4: into a cache held in 4 bits.
-int append_call(int dtype, bool q4, const metok_paged_cache* c, const void* k_new, const void* v_new, int64_t k_head, int64_t k_row, int64_t v_head,
-                int64_t v_row, int n_new, const int32_t* new_offsets, int32_t* positions, const int32_t* pos_new, float* mass,
-                const float* mass_new, int32_t* new_len, int32_t* status, void* stream) {
+extern "C" int metok_paged_append(int dtype, const metok_paged_cache* c, const void* k_new, const void* v_new, int64_t k_head,
+                                  int64_t k_row, int64_t v_head, int64_t v_row, int n_new, const int32_t* new_offsets,
+                                  int32_t* positions, const int32_t* pos_new, float* mass, const float* mass_new, int32_t* new_len,
+                                  int32_t* status, void* stream) {
     PagedDims d;
-    if (dtype != METOK_F32 && dtype != METOK_BF16) return METOK_ERR_INVALID_ARG;
-    const int rc = q4 ? paged_dims_q4(c, &d) : paged_dims(dtype, c, &d);
+    const int rc = paged_dims(dtype, c, &d);
     if (rc != METOK_OK) return rc;
     if (!c->k_pool || !c->v_pool || !c->block_table || !c->kv_len || !new_len || !status || n_new < 0) return METOK_ERR_INVALID_ARG;
     if (n_new > 0 && (!k_new || !v_new)) return METOK_ERR_INVALID_ARG;
@@ -630,71 +482,15 @@ int append_call(int dtype, bool q4, const metok_paged_cache* c, const void* k_ne
     a.k_pool = (uint4*)c->k_pool; a.v_pool = (uint4*)c->v_pool;
     a.k_head = k_head / per; a.k_row = k_row / per; a.v_head = v_head / per; a.v_row = v_row / per;
     a.n_new = n_new;
-    a.parts = q4 ? ceil_div(2 * d.Hkv * (d.dh / 16), 32 * kHoldBlocks) : ceil_div(2 * d.Hkv * d.row_chunks, 32 * kAppendChunks);
+    a.parts = ceil_div(2 * d.Hkv * d.row_chunks, 32 * kAppendChunks);
     a.block_table = c->block_table; a.kv_len = c->kv_len; a.offsets = new_offsets; a.pos_new = pos_new;
     a.positions = positions; a.mass = mass; a.mass_new = mass_new; a.new_len = new_len; a.status = status;
     const long long blocks = 1 + ((long long)n_new * a.parts + kAppendWarps - 1) / kAppendWarps;
     if (blocks > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)stream;
     {
-        METOK_TIMED(q4 ? "paged_append_q4" : "paged_append", st);
-        auto kern = !q4 ? paged_append_kernel<CopyRows> : dtype == METOK_F32 ? paged_append_kernel<HoldRows<float>> : paged_append_kernel<HoldRows<__nv_bfloat16>>;
-        launch_chained(kern, dim3((unsigned)blocks), dim3(kAppendWarps * 32), 0, st, a);
-    }
-    METOK_LAUNCH_CHECK();
-    return METOK_OK;
-}
-}  // namespace
-
-extern "C" int metok_paged_append(int dtype, const metok_paged_cache* c, const void* k_new, const void* v_new, int64_t k_head,
-                                  int64_t k_row, int64_t v_head, int64_t v_row, int n_new, const int32_t* new_offsets,
-                                  int32_t* positions, const int32_t* pos_new, float* mass, const float* mass_new, int32_t* new_len,
-                                  int32_t* status, void* stream) {
-    return append_call(dtype, false, c, k_new, v_new, k_head, k_row, v_head, v_row, n_new, new_offsets, positions, pos_new, mass, mass_new, new_len,
-                       status, stream);
-}
-extern "C" int metok_paged_append_q4(int new_dtype, const metok_paged_cache* c, const void* k_new, const void* v_new, int64_t k_head,
-                                     int64_t k_row, int64_t v_head, int64_t v_row, int n_new, const int32_t* new_offsets,
-                                     int32_t* positions, const int32_t* pos_new, float* mass, const float* mass_new, int32_t* new_len,
-                                     int32_t* status, void* stream) {
-    return append_call(new_dtype, true, c, k_new, v_new, k_head, k_row, v_head, v_row, n_new, new_offsets, positions, pos_new, mass, mass_new, new_len,
-                       status, stream);
-}
-
-extern "C" int metok_paged_read_q4(int out_dtype, const metok_paged_cache* c, const int32_t* offsets, const int32_t* first_row, int n_rows,
-                                   void* k_out, void* v_out, int64_t k_head, int64_t k_row, int64_t v_head, int64_t v_row,
-                                   const int32_t* positions, int32_t* pos_out, int32_t* status, void* stream) {
-    PagedDims d;
-    if (out_dtype != METOK_F32 && out_dtype != METOK_BF16) return METOK_ERR_INVALID_ARG;
-    const int rc = paged_dims_q4(c, &d);
-    if (rc != METOK_OK) return rc;
-    if (!c->k_pool || !c->v_pool || !c->block_table || !c->kv_len || !offsets || !status || n_rows < 0) return METOK_ERR_INVALID_ARG;
-    if (n_rows > 0 && (!k_out || !v_out)) return METOK_ERR_INVALID_ARG;
-    if (!aligned16(c->k_pool) || !aligned16(c->v_pool) || !aligned16(k_out) || !aligned16(v_out)) return METOK_ERR_INVALID_ARG;
-    if (!aligned4(c->block_table) || !aligned4(c->kv_len) || !aligned4(offsets) || !aligned4(first_row) || !aligned4(positions) ||
-        !aligned4(pos_out) || !aligned4(status))
-        return METOK_ERR_INVALID_ARG;
-    if (pos_out && !positions) return METOK_ERR_INVALID_ARG;
-    const int esize = out_dtype == METOK_F32 ? 4 : 2, per = 16 / esize;
-    if (k_head < 0 || v_head < 0 || k_row < 0 || v_row < 0 || (k_head | k_row | v_head | v_row) % per) return METOK_ERR_INVALID_ARG;
-    if (!rows_apart(d.Hkv, k_head, n_rows, k_row, d.dh) || !rows_apart(d.Hkv, v_head, n_rows, v_row, d.dh)) return METOK_ERR_INVALID_ARG;
-    if (n_rows > 0) {
-        const Extent k = extent_of(k_out, d.Hkv, k_head, n_rows, k_row, d.dh, esize), v = extent_of(v_out, d.Hkv, v_head, n_rows, v_row, d.dh, esize);
-        if (!apart(k, v)) return METOK_ERR_INVALID_ARG;
-    }
-    ReadArgs a;
-    a.d = d;
-    a.k_pool = (const uint8_t*)c->k_pool; a.v_pool = (const uint8_t*)c->v_pool;
-    a.k_out = (uint4*)k_out; a.v_out = (uint4*)v_out;
-    a.k_head = k_head / per; a.k_row = k_row / per; a.v_head = v_head / per; a.v_row = v_row / per;
-    a.n_rows = n_rows;
-    a.block_table = c->block_table; a.kv_len = c->kv_len; a.offsets = offsets; a.first_row = first_row; a.positions = positions;
-    a.pos_out = pos_out; a.status = status;
-    cudaStream_t st = (cudaStream_t)stream;
-    {
-        METOK_TIMED("paged_read_q4", st);
-        auto kern = out_dtype == METOK_F32 ? paged_read_q4_kernel<float> : paged_read_q4_kernel<__nv_bfloat16>;
-        launch_chained(kern, dim3(1 + (unsigned)(((long long)n_rows + kReadRows - 1) / kReadRows)), dim3(kReadThreads), 0, st, a);
+        METOK_TIMED("paged_append", st);
+        launch_chained(paged_append_kernel, dim3((unsigned)blocks), dim3(kAppendWarps * 32), 0, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;

@@ -10,13 +10,15 @@
 #include <math.h>
 
 #include "launchers.h"
-#include "paged.cuh"
+#include "common.cuh"
+#include "sm100.cuh"
 
 namespace metok {
 
 namespace {
 
 constexpr int kWarps = 8, kMaxAxes = 4, kMaxPairs = 64;
+constexpr int kDepth = 4;                              // turns whose elements are on their way
 
 struct RotateRows {
     const void* x;
@@ -36,151 +38,180 @@ struct RotateArgs {
 
 template <typename T> struct Raw { uint4 v[sizeof(T)]; };              // 16 elements: two chunks of eight
 
+// Elements 2 i, 2 i + 1 side by side.
 template <typename T>
-__device__ __forceinline__ void widen(const Raw<T>& r, float (&x)[16]) {
-    if constexpr (sizeof(T) == 4) {
+__device__ __forceinline__ void widen(const Raw<T>& r, uint64_t (&x)[8]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[4 * i] = __uint_as_float(r.v[i].x); x[4 * i + 1] = __uint_as_float(r.v[i].y);
-            x[4 * i + 2] = __uint_as_float(r.v[i].z); x[4 * i + 3] = __uint_as_float(r.v[i].w);
-        }
-    } else {
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+        const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+        if constexpr (sizeof(T) == 4) {
+            x[2 * i] = sm100::pair(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            x[2 * i + 1] = sm100::pair(__uint_as_float(w[2]), __uint_as_float(w[3]));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-                x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-            }
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = sm100::pair(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
         }
     }
 }
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 template <typename T>
-__device__ __forceinline__ Raw<T> narrow(const float (&x)[16]) {
+__device__ __forceinline__ Raw<T> narrow(const uint64_t (&x)[8]) {
     Raw<T> r;
-    if constexpr (sizeof(T) == 4) {
+    uint32_t w[4 * sizeof(T)];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            r.v[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            r.v[i] = make_uint4(two_bf16(x[8 * i], x[8 * i + 1]), two_bf16(x[8 * i + 2], x[8 * i + 3]), two_bf16(x[8 * i + 4], x[8 * i + 5]),
-                                two_bf16(x[8 * i + 6], x[8 * i + 7]));
+    for (int i = 0; i < 8; ++i) {
+        float lo, hi;
+        sm100::unpair(x[i], lo, hi);
+        if constexpr (sizeof(T) == 4) {
+            w[2 * i] = __float_as_uint(lo);
+            w[2 * i + 1] = __float_as_uint(hi);
+        } else {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(hi), "f"(lo));
+        }
     }
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) r.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     return r;
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
 template <typename T, int DH>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, 3)
 rotate_kernel(const RotateArgs a) {
+    using namespace sm100;
     constexpr int L = DH / 16, G = 32 / L, kMine = 8 / G;                // lanes of a head, heads at a time, angles of a lane
     constexpr int kHalf = sizeof(T) / 2;                                 // 16-byte pieces of a chunk
+    extern __shared__ uint4 s_ring[];                  // [warp][turn][piece][lane]: each lane reads what it has copied
     const int lane = threadIdx.x & 31, s = lane % L, g = lane / L;
-    const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const long long row = item / a.split;
-    const int part = (int)(item - row * a.split), passes = a.q.passes + a.k.passes;
-    grid_dep_wait();
-    if (row >= a.n) return;                            // uniform in the warp
-    const int p0 = passes * part / a.split, p1 = passes * (part + 1) / a.split;
+    const uint32_t item = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int row = (int)(item / (uint32_t)a.split), part = (int)(item - (uint32_t)row * a.split), passes = a.q.passes + a.k.passes;
     // the lane's two chunks of eight elements
     const int slots = a.rotary / 16;                   // lanes of a head whose elements turn
     const int c0 = a.interleaved || s >= slots ? 16 * s : 8 * s, c1 = a.interleaved || s >= slots ? 16 * s + 8 : a.rotary / 2 + 8 * s;
+    const int p0 = (int)((uint32_t)passes * part / (uint32_t)a.split), p1 = (int)((uint32_t)passes * (part + 1) / (uint32_t)a.split);
+    grid_dep_wait();
+    if (row >= a.n) return;                            // uniform in the warp
+    const T *q_row = reinterpret_cast<const T*>(a.q.x) + row * a.q.row, *k_row = reinterpret_cast<const T*>(a.k.x) + row * a.k.row;
+    T *q_out = reinterpret_cast<T*>(a.q.out) + row * a.q.out_row, *k_out = reinterpret_cast<T*>(a.k.out) + row * a.k.out_row;
 
-    auto fetch = [&](int p, Raw<T>& r) {
-        const RotateRows& x = p < a.q.passes ? a.q : a.k;
-        const int h = (p < a.q.passes ? p : p - a.q.passes) * G + g;
-        if (p >= p1 || h >= x.H) return;
-        const T* src = reinterpret_cast<const T*>(x.x) + h * x.head + row * x.row;
+    const uint4* const mine = s_ring + (threadIdx.x >> 5) * (kDepth * (int)sizeof(T) * 32) + lane;
+    const uint32_t mine_at = smem_u32(mine);
+    auto fetch = [&](int p) {
+        const bool is_k = p >= a.q.passes;
+        const int h = (is_k ? p - a.q.passes : p) * G + g;
+        if (p < p1 && h < (is_k ? a.k.H : a.q.H)) {
+            const T* src = is_k ? k_row + h * a.k.head : q_row + h * a.q.head;
+            const uint32_t dst = mine_at + (p - p0) % kDepth * ((int)sizeof(T) * 512);
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            r.v[i] = reinterpret_cast<const uint4*>(src + c0)[i];
-            r.v[kHalf + i] = reinterpret_cast<const uint4*>(src + c1)[i];
+            for (int i = 0; i < kHalf; ++i) {
+                copy16(dst + i * 512, reinterpret_cast<const uint4*>(src + c0) + i);
+                copy16(dst + (kHalf + i) * 512, reinterpret_cast<const uint4*>(src + c1) + i);
+            }
         }
+        copies_close();
     };
-    Raw<T> next = {};
-    fetch(p0, next);
+    for (int u = 0; u < kDepth; ++u) fetch(p0 + u);
 
-    // sines and cosines of pairs 8 s .. 8 s + 7
-    float cs[8], sn[8];
+    // sines and cosines of pairs 8 s .. 8 s + 7, side by side
+    uint64_t cs[4], sn[4];
     if (slots > 0) {
         float mc[kMine], ms[kMine];
 #pragma unroll
         for (int u = 0; u < kMine; ++u) {
-            const int pair = 8 * s + g * kMine + u;
+            const int at = 8 * s + g * kMine + u;
             float x = 0.f;
             if (s < slots) {
-                const int axis = (int)(a.axis[pair >> 5] >> (2 * (pair & 31))) & 3;
-                const int pos = a.positions ? a.positions[(long long)axis * a.n + row] : (int)row;
-                const double t = (double)pos * ((double)a.inv_freq[pair] * 0.15915494309189533577);   // turns
+                const int axis = (int)(a.axis[at >> 5] >> (2 * (at & 31))) & 3;
+                const int pos = a.positions ? a.positions[(long long)axis * a.n + row] : row;
+                const double t = (double)pos * ((double)a.inv_freq[at] * 0.15915494309189533577);     // turns
                 x = (float)(2.0 * (t - rint(t)));
             }
             sincospif(x, &ms[u], &mc[u]);
         }
+        float c[8], d[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            cs[j] = __shfl_sync(0xFFFFFFFFu, mc[j % kMine], (j / kMine) * L + s);
-            sn[j] = __shfl_sync(0xFFFFFFFFu, ms[j % kMine], (j / kMine) * L + s);
+            c[j] = __shfl_sync(0xFFFFFFFFu, mc[j % kMine], (j / kMine) * L + s);
+            d[j] = __shfl_sync(0xFFFFFFFFu, ms[j % kMine], (j / kMine) * L + s);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            cs[j] = pair(c[2 * j], c[2 * j + 1]);
+            sn[j] = pair(d[2 * j], d[2 * j + 1]);
         }
     }
 
-    float w[16];
-    bool weights_of_k = false;
+    uint64_t w[8];
     auto weights = [&](const float* src) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float* at = src + (i < 2 ? c0 + 4 * i : c1 + 4 * (i - 2));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[4 * i + j] = src ? at[j] : 1.f;
+        for (int i = 0; i < 8; ++i) {
+            const int at = i < 4 ? c0 + 2 * i : c1 + 2 * (i - 4);
+            w[i] = src ? pair(src[at], src[at + 1]) : pair(1.f, 1.f);
         }
     };
     for (int p = p0; p < p1; ++p) {
         const bool is_k = p >= a.q.passes;
-        const RotateRows& o = is_k ? a.k : a.q;
         const int h = (is_k ? p - a.q.passes : p) * G + g;
-        float x[16];
-        widen<T>(next, x);
-        fetch(p + 1, next);
-        if (a.norm) {
-            if (p == p0 || is_k != weights_of_k) {
-                weights(o.weight);
-                weights_of_k = is_k;
-            }
-            float ss = 0.f;
+        uint64_t x[8];
+        copies_wait<kDepth - 1>();
+        {
+            Raw<T> raw;
+            const uint4* from = mine + (p - p0) % kDepth * ((int)sizeof(T) * 32);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+            for (int i = 0; i < (int)sizeof(T); ++i) raw.v[i] = from[i * 32];
+            widen<T>(raw, x);
+        }
+        fetch(p + kDepth);
+        if (a.norm) {
+            if (p == p0 || p == a.q.passes) weights(is_k ? a.k.weight : a.q.weight);
+            uint64_t sum = mul_pair(x[0], x[0]);
+#pragma unroll
+            for (int i = 1; i < 8; ++i) sum = fma_pair(x[i], x[i], sum);
+            float ss, odd;
+            unpair(sum, ss, odd);
+            ss += odd;
 #pragma unroll
             for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-            const float f = 1.f / sqrtf(ss * (1.f / DH) + a.eps);
+            const float f = rsqrtf(fmaf(ss, 1.f / DH, a.eps));
+            const uint64_t f2 = pair(f, f);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= f * w[i];
+            for (int i = 0; i < 8; ++i) x[i] = mul_pair(x[i], mul_pair(f2, w[i]));
         }
         if (s < slots) {
             if (a.interleaved) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float u = x[2 * j], v = x[2 * j + 1];
-                    x[2 * j] = fmaf(u, cs[j], -v * sn[j]);
-                    x[2 * j + 1] = fmaf(v, cs[j], u * sn[j]);
+                    float u, v, c, d;
+                    unpair(x[j], u, v);
+                    if (j & 1) {
+                        float skip;
+                        unpair(cs[j / 2], skip, c);
+                        unpair(sn[j / 2], skip, d);
+                    } else {
+                        float skip;
+                        unpair(cs[j / 2], c, skip);
+                        unpair(sn[j / 2], d, skip);
+                    }
+                    x[j] = pair(fmaf(u, c, -v * d), fmaf(v, c, u * d));
                 }
             } else {
+                const uint64_t minus = pair(-1.f, -1.f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float u = x[j], v = x[8 + j];
-                    x[j] = fmaf(u, cs[j], -v * sn[j]);
-                    x[8 + j] = fmaf(v, cs[j], u * sn[j]);
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t u = x[j], v = x[4 + j];
+                    x[j] = fma_pair(u, cs[j], mul_pair(mul_pair(v, minus), sn[j]));
+                    x[4 + j] = fma_pair(v, cs[j], mul_pair(u, sn[j]));
                 }
             }
         }
-        if (h < o.H) {
+        if (h < (is_k ? a.k.H : a.q.H)) {
             const Raw<T> r = narrow<T>(x);
-            T* dst = reinterpret_cast<T*>(o.out) + h * o.out_head + row * o.out_row;
+            T* dst = is_k ? k_out + h * a.k.out_head : q_out + h * a.q.out_head;
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
                 reinterpret_cast<uint4*>(dst + c0)[i] = r.v[i];
@@ -188,13 +219,23 @@ rotate_kernel(const RotateArgs a) {
             }
         }
     }
+    copies_wait<0>();
 }
 
 template <typename T>
-void launch_rotate(int dh, const RotateArgs& a, unsigned blocks, cudaStream_t st) {
-    METOK_TIMED("rotate_heads", st);
-    if (dh == 64) launch_chained(rotate_kernel<T, 64>, dim3(blocks), dim3(kWarps * 32), 0, st, a);
-    else launch_chained(rotate_kernel<T, 128>, dim3(blocks), dim3(kWarps * 32), 0, st, a);
+int launch_rotate(int dh, const RotateArgs& a, unsigned blocks, cudaStream_t st) {
+    constexpr size_t smem = (size_t)kWarps * kDepth * sizeof(T) * 512;
+    if (dh == 64) {
+        METOK_ALLOW_SMEM((rotate_kernel<T, 64>), smem);
+        METOK_TIMED("rotate_heads", st);
+        launch_chained(rotate_kernel<T, 64>, dim3(blocks), dim3(kWarps * 32), smem, st, a);
+    } else {
+        METOK_ALLOW_SMEM((rotate_kernel<T, 128>), smem);
+        METOK_TIMED("rotate_heads", st);
+        launch_chained(rotate_kernel<T, 128>, dim3(blocks), dim3(kWarps * 32), smem, st, a);
+    }
+    METOK_LAUNCH_CHECK();
+    return METOK_OK;
 }
 
 }  // namespace
@@ -248,10 +289,7 @@ extern "C" int metok_rotate_heads(int dtype, const metok_rotate_params* p, void*
     const int passes = a.q.passes + a.k.passes;
     a.split = std::max(1, std::min(passes, (int)std::min<long long>(passes, (32LL * kNumSMs + p->n - 1) / p->n)));
     const long long blocks = ((long long)p->n * a.split + kWarps - 1) / kWarps;
-    if (blocks > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
+    if (blocks > 0x7FFFFFFFLL / kWarps) return METOK_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == METOK_F32) launch_rotate<float>(p->dh, a, (unsigned)blocks, st);
-    else launch_rotate<__nv_bfloat16>(p->dh, a, (unsigned)blocks, st);
-    METOK_LAUNCH_CHECK();
-    return METOK_OK;
+    return dtype == METOK_F32 ? launch_rotate<float>(p->dh, a, (unsigned)blocks, st) : launch_rotate<__nv_bfloat16>(p->dh, a, (unsigned)blocks, st);
 }
