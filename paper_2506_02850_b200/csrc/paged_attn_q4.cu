@@ -91,7 +91,7 @@ struct Q4Block {
 template <int DH, int NG, int QP>
 struct Q4Unit {
     uint32_t q[QP][NG][DH / 16][2];
-    float m[NG][2], l[NG][2], o[NG][DH / 16][4], slope[NG][2], scale[NG][2];     // scale: from products to logits (to logits / cap)
+    float m[NG][2], l[NG][2], o[NG][DH / 16][4], slope[NG][2], scale[NG][2];     // scale: from products to logits, or to those of whole q where they are capped
 
     template <typename T>
     __device__ __forceinline__ void start(const PagedAttnArgs& a, int b, int h0, int nh) {
@@ -131,7 +131,8 @@ struct Q4Unit {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int hc = n * 8 + 2 * t + e;
-                scale[n][e] = fmaxf(__shfl_sync(0xFFFFFFFFu, up, (2 * t + e) * 4) * (a.cap_log2 > 0.f ? a.cap_scale : a.scale_log2), 1.2e-38f);   // (never 0)
+                scale[n][e] = __shfl_sync(0xFFFFFFFFu, up, (2 * t + e) * 4);
+                if (!(a.cap_log2 > 0.f)) scale[n][e] = fmaxf(scale[n][e] * a.scale_log2, 1.2e-38f);      // (never 0: rows that are not there count as -infinity)
                 m[n][e] = kLow;
                 l[n][e] = 0.f;
                 slope[n][e] = a.slopes && hc < nh ? a.slopes[h0 + hc] * kLog2e : 0.f;
@@ -234,7 +235,10 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
                 for (int n = 0; n < NG; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(x[r][n][e]));
+                    for (int i = 0; i < 4; i += 2) {   // in units of the cap
+                        unpair(mul_pair(two(&x[r][n][i]), pair(a.cap_scale, a.cap_scale)), x[r][n][i], x[r][n][i + 1]);
+                        most = fmaxf(most, fmaxf(fabsf(x[r][n][i]), fabsf(x[r][n][i + 1])));
+                    }
             if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
 #pragma unroll
                 for (int r = 0; r < RP; ++r)

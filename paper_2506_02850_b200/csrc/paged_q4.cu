@@ -11,6 +11,7 @@ namespace metok {
 namespace {
 
 constexpr int kThreads = 256, kMostRows = 32, kFewSeqs = 32;
+static_assert(kMostRows >= 32, "whole warps find the rows");
 
 struct RowsArgs {
     PagedDims d;
@@ -130,14 +131,15 @@ __device__ __forceinline__ void find_rows(const RowsArgs& a, int i0, int (&s_pag
     __syncthreads();
 }
 
-// A thread keeps its places in the rows, blocks of 16 elements (append) or words of eight (read), and goes over the heads of K and of V with the
-// next one's on their way, an append's first ones already while its warps find out where they belong.  Where the rows are few, groups of
-// threads share the heads.
+// A thread keeps its place in the rows, a block of 16 elements (append) or words of eight (read), and goes over the heads of K and of V.  Of an
+// append the next head's elements are on their way, the first ones already while its warps find out where they belong; of a read kReadHeads heads'
+// codes at a time.  Where the rows are few, groups of threads share the heads.
+constexpr int kReadHeads = 4;
+
 template <typename T, bool kAppend>
 __global__ void __launch_bounds__(kThreads)
 paged_rows_q4_kernel(const RowsArgs a) {
     constexpr int kOf = kAppend ? 16 : 8, kChunks = kOf * (int)sizeof(T) / 16;       // elements of an item, 16-byte chunks of them
-    constexpr int kPlaces = kAppend ? 1 : 2;           // of a thread at most: kMostRows rows of dh 128
     __shared__ int s_page[kMostRows], s_row[kMostRows];
     grid_dep_wait();
     const int i0 = ((int)blockIdx.x - 1) << a.rows_shift;
@@ -145,87 +147,66 @@ paged_rows_q4_kernel(const RowsArgs a) {
     const int groups = max(1, kThreads >> place_shift), group = (int)threadIdx.x >> place_shift;          // (powers of two)
     const int kv0 = groups > 1 ? group & 1 : 0, kvs = groups > 1 ? kv0 + 1 : 2, h0 = groups > 1 ? group >> 1 : 0, h_step = groups > 1 ? groups >> 1 : 1;
     const long long head = (long long)q4_piece(dh) << (a.d.page_shift - 4);          // bytes from head to head of a page
-    const int place = threadIdx.x & ((1 << place_shift) - 1), i = place & ((1 << shift) - 1);
-    int r[kPlaces];
-#pragma unroll
-    for (int u = 0; u < kPlaces; ++u) r[u] = place + u * kThreads < 1 << place_shift ? (place + u * kThreads) >> shift : -1;
-    auto rows_at = [&](int u, int kv) {
-        return (kv ? a.v_rows + (i0 + r[u]) * a.v_row + h0 * a.v_head : a.k_rows + (i0 + r[u]) * a.k_row + h0 * a.k_head) + i * (kChunks * 16);
+    const int i = threadIdx.x & ((1 << shift) - 1);
+    auto rows_at = [&](int r, int kv) {
+        return (kv ? a.v_rows + (i0 + r) * a.v_row + h0 * a.v_head : a.k_rows + (i0 + r) * a.k_row + h0 * a.k_head) + i * (kChunks * 16);
     };
-    uint4 x[kPlaces][kAppend ? kChunks : 1];           // appends: elements; reads: codes and scale
-    if constexpr (kAppend) {
-        if (blockIdx.x && r[0] >= 0 && i0 + r[0] < a.n_rows && h0 < a.d.Hkv) {
-            const uint4* from = reinterpret_cast<const uint4*>(rows_at(0, kv0));
+    int place = threadIdx.x & ((1 << place_shift) - 1);
+    uint4 x[kChunks];                                  // of an append
+    auto fetch = [&](const char* from) {
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) x[0][j] = __ldg(from + j);
-        }
+        for (int j = 0; j < kChunks; ++j) x[j] = __ldg(reinterpret_cast<const uint4*>(from) + j);
+    };
+    if constexpr (kAppend) {
+        if (blockIdx.x && i0 + (place >> shift) < a.n_rows && h0 < a.d.Hkv) fetch(rows_at(place >> shift, kv0));
     }
     find_rows<kAppend>(a, i0, s_page, s_row);
     if (blockIdx.x == 0 || h0 >= a.d.Hkv) return;
-    size_t codes[kPlaces];                             // from the pool's beginning; scales from there
-    int scales[kPlaces];
-    bool any = false;
-#pragma unroll
-    for (int u = 0; u < kPlaces; ++u) {
-        const int page = r[u] >= 0 ? s_page[r[u]] : -1, at = page >= 0 ? s_row[r[u]] & 15 : 0;
-        if (page < 0) r[u] = -1;
-        codes[u] = page >= 0 ? q4_piece_of(a.d, page, 0, s_row[r[u]]) * q4_piece(dh) + at * (dh / 2) + i * (kOf / 2) + h0 * head : 0;
-        scales[u] = 8 * dh + at * (dh / 16) + (kAppend ? i : i >> 1) - (at * (dh / 2) + i * (kOf / 2));
-        any |= page >= 0;
-    }
-    if (!any) return;
-    for (int kv = kv0; kv < kvs; ++kv) {
-        uint8_t* pool = kv ? a.v_pool : a.k_pool;
-        char* rows[kPlaces];
-#pragma unroll
-        for (int u = 0; u < kPlaces; ++u) rows[u] = rows_at(u, kv);
-        const long long row_step = h_step * (kv ? a.v_head : a.k_head), code_step = h_step * head;
-        auto fetch = [&](long long ahead) {            // heads from the one at hand
-#pragma unroll
-            for (int u = 0; u < kPlaces; ++u) {
-                if (r[u] < 0) continue;
-                if constexpr (kAppend) {
-                    const uint4* from = reinterpret_cast<const uint4*>(rows[u] + ahead * row_step);
-#pragma unroll
-                    for (int j = 0; j < kChunks; ++j) x[u][j] = __ldg(from + j);
-                } else {
-                    const uint8_t* from = pool + codes[u] + ahead * code_step;
-                    x[u][0].x = __ldg(reinterpret_cast<const uint32_t*>(from));
-                    x[u][0].y = __ldg(from + scales[u]);
-                }
-            }
-        };
-        if (!kAppend || kv > kv0) fetch(0);
-        for (int h = h0; h < a.d.Hkv; h += h_step) {
+    for (; place < 1 << place_shift; place += kThreads) {                // (one turn of an append)
+        const int r = place >> shift, page = s_page[r], at = s_row[r] & 15;
+        if (page < 0) continue;
+        const size_t codes = q4_piece_of(a.d, page, 0, s_row[r]) * q4_piece(dh) + at * (dh / 2) + i * (kOf / 2) + h0 * head;
+        const int scale = 8 * dh + at * (dh / 16) + (kAppend ? i : i >> 1) - (at * (dh / 2) + i * (kOf / 2));
+        const long long code_step = h_step * head;
+        for (int kv = kv0; kv < kvs; ++kv) {
+            uint8_t* code = (kv ? a.v_pool : a.k_pool) + codes;
+            char* row = rows_at(r, kv);
+            const long long row_step = h_step * (kv ? a.v_head : a.k_head);
             if constexpr (kAppend) {
-                float v[16];
-                q4_widen<T>(x[0], v);
-                if (h + h_step < a.d.Hkv) fetch(1);
-                uint32_t c[2];
-                uint8_t* to = pool + codes[0];
-                to[scales[0]] = (uint8_t)q4_hold(v, c);
-                *reinterpret_cast<uint2*>(to) = make_uint2(c[0], c[1]);
-                rows[0] += row_step;
-            } else {
-                uint32_t code[kPlaces], scale[kPlaces];
-#pragma unroll
-                for (int u = 0; u < kPlaces; ++u) {
-                    code[u] = x[u][0].x;
-                    scale[u] = x[u][0].y;
+                if (kv > kv0) fetch(row);
+                for (int h = h0; h < a.d.Hkv; h += h_step) {
+                    float v[16];
+                    q4_widen<T>(x, v);
+                    row += row_step;
+                    if (h + h_step < a.d.Hkv) fetch(row);
+                    uint32_t c[2];
+                    code[scale] = (uint8_t)q4_hold(v, c);
+                    *reinterpret_cast<uint2*>(code) = make_uint2(c[0], c[1]);
+                    code += code_step;
                 }
-                if (h + h_step < a.d.Hkv) fetch(1);
+            } else {
+                for (int h = h0; h < a.d.Hkv; h += h_step * kReadHeads) {
+                    uint32_t c[kReadHeads], e[kReadHeads];
 #pragma unroll
-                for (int u = 0; u < kPlaces; ++u) {
-                    if (r[u] >= 0) {
-                        uint4 v[kChunks];
-                        q4_stands_for<T>(code[u], scale[u], v);
-#pragma unroll
-                        for (int j = 0; j < kChunks; ++j) reinterpret_cast<uint4*>(rows[u])[j] = v[j];
+                    for (int u = 0; u < kReadHeads; ++u) {
+                        if (h + u * h_step < a.d.Hkv) {
+                            c[u] = __ldg(reinterpret_cast<const uint32_t*>(code));
+                            e[u] = __ldg(code + scale);
+                        }
+                        code += code_step;
                     }
-                    rows[u] += row_step;
+#pragma unroll
+                    for (int u = 0; u < kReadHeads; ++u) {
+                        if (h + u * h_step < a.d.Hkv) {
+                            uint4 v[kChunks];
+                            q4_stands_for<T>(c[u], e[u], v);
+#pragma unroll
+                            for (int j = 0; j < kChunks; ++j) reinterpret_cast<uint4*>(row)[j] = v[j];
+                        }
+                        row += row_step;
+                    }
                 }
             }
-            pool += code_step;
         }
     }
 }

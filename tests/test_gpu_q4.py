@@ -277,6 +277,20 @@ def test_attention_of_small_and_large_numbers(dtype, size):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cap", [1e6, 1e20, 1e30, 1e38])
+def test_attention_under_a_cap_that_is_far_away(dtype, cap):
+    """A cap that no logit comes near changes next to nothing: cap tanh(x / cap) is x up to fp32's roundings.  At 1e38 the scale over the cap is 1e-39,
+    where numbers are 2^-149 apart: it is off by 7e-7 of itself, and logits (below 16 here) by 1.1e-5."""
+    c = Cache([300, 65], 2, 128, 32, seed=31)
+    q = torch.randn((2, 8, 128), generator=c.g, device="cuda").to(dtype)
+    call = lambda x: B.metok_paged_attention_q4(q, c.k[0], c.v[0], c.block_table, c.kv_len, 0.1, softcap=x, with_lse=True)
+    plain, capped = call(0.0), call(cap)
+    torch.cuda.synchronize()
+    assert torch.allclose(capped["lse"], plain["lse"], rtol=0, atol=2e-5)
+    assert torch.allclose(capped["out"].float(), plain["out"].float(), rtol=2 * HALF[dtype], atol=1e-4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_attention_equal_weights_and_large_logits(dtype):
     c = Cache([90, 130], 2, 64, 16, seed=5)
     check_attention(c, 4, dtype, q=torch.zeros((2, 4, 64), dtype=dtype, device="cuda"))
@@ -333,6 +347,27 @@ def test_attention_bad_pages_and_lengths_leave_the_sequence_alone():
     for b in (0, 2, 3):
         assert (out[b] == 3.0).all() and torch.equal(mass[b], c.mass[0, b])
     assert torch.allclose(out[1].float(), good["out"][1].float(), rtol=0.02, atol=0.02)
+
+
+@pytest.mark.parametrize("mass", [False, True])
+def test_attention_a_bad_page_among_many_sequences(mass):
+    lens = np.random.default_rng(5).integers(1, 90, 300).tolist()
+    lens[7] = 80
+    c = Cache(lens, 2, 64, 16, seed=13)
+    q = torch.randn((300, 6, 64), generator=c.g, device="cuda").to(torch.bfloat16)
+    call = lambda table, m, out: B.metok_paged_attention_q4(q, c.k[0], c.v[0], table, c.kv_len, 0.125, mass=m, out=out, with_lse=True)
+    m0, m1 = (c.mass[0].clone() if mass else None for _ in range(2))
+    good, out = torch.empty_like(q), torch.full_like(q, 3.0)
+    want = call(c.block_table, m0, good)
+    table = c.block_table.clone()
+    table[7, 4] = -5
+    got = call(table, m1, out)
+    torch.cuda.synchronize()
+    assert int(want["status"]) == 0 and int(got["status"]) == -1
+    others = [b for b in range(300) if b != 7]
+    assert (out[7] == 3).all() and torch.equal(out[others], good[others]) and torch.equal(got["lse"][others], want["lse"][others])
+    if mass:
+        assert torch.equal(m1[7], c.mass[0, 7]) and torch.equal(m1[others], m0[others])
 
 
 def test_attention_captured_with_lengths_that_change():
