@@ -2,11 +2,12 @@
 //
 // A group of dh / 16 lanes has a head of a row, 16 elements a lane that hold both halves of eight pairs; a warp has 8 (dh 64) or 4
 // (dh 128) heads at a time and goes over the heads of its row, so that the row's sines and cosines stay in registers.  Each lane works
-// out one or two of a pair's angles and the groups exchange them: t = position * inv_freq / 2 pi in 64 bits, of which the distance to
-// the nearest integer is exact enough for any int32 position, and sincospif of that in 32.  The sum of squares is the lanes' 16, added by
-// shuffles.  The next heads' elements are on their way while these are turned.
+// out one or two of the pairs' angles and the groups exchange them: t = position * inv_freq / 2 pi in 64 bits, of which the distance to
+// the nearest integer is exact enough for any int32 position, and sincospi of that in 32.  Elements are worked on two at a time.
 //
-// What bounds it is reading and writing Q and K once.
+// What bounds it is reading and writing Q and K once: the next four turns' elements are on their way to a ring in shared memory, 96 KB for
+// the 24 warps of an SM, that costs no registers (of two turns' in registers, for which there were 16 warps, 76 us).  18 496 rows of 28 + 4 heads of
+// 128: 51.6 us, 5.9 TB/s, as a copy of as many bytes; some 200 operations a turn of a warp, with pointers that are worked out for every turn 56 us.
 #include <math.h>
 
 #include "launchers.h"
@@ -96,26 +97,50 @@ rotate_kernel(const RotateArgs a) {
     const int p0 = (int)((uint32_t)passes * part / (uint32_t)a.split), p1 = (int)((uint32_t)passes * (part + 1) / (uint32_t)a.split);
     grid_dep_wait();
     if (row >= a.n) return;                            // uniform in the warp
-    const T *q_row = reinterpret_cast<const T*>(a.q.x) + row * a.q.row, *k_row = reinterpret_cast<const T*>(a.k.x) + row * a.k.row;
-    T *q_out = reinterpret_cast<T*>(a.q.out) + row * a.q.out_row, *k_out = reinterpret_cast<T*>(a.k.out) + row * a.k.out_row;
-
+    // The warp's way over the heads, to be fetched and to be turned: a lane's head, in a turn, and its first element there.
+    struct Way {
+        int p, h;
+        char* at;
+    };
+    auto set = [&](Way& w, bool out) {                 // at the first turn, and where K's begin
+        const bool is_k = w.p >= a.q.passes;
+        const RotateRows& o = is_k ? a.k : a.q;
+        w.h = (is_k ? w.p - a.q.passes : w.p) * G + g;
+        w.at = out ? reinterpret_cast<char*>(reinterpret_cast<T*>(o.out) + row * o.out_row + w.h * o.out_head)
+                   : reinterpret_cast<char*>(const_cast<T*>(reinterpret_cast<const T*>(o.x) + row * o.row + w.h * o.head));
+    };
+    auto next = [&](Way& w, bool out) {
+        if (++w.p == a.q.passes) {
+            set(w, out);
+            return;
+        }
+        const RotateRows& o = w.p >= a.q.passes ? a.k : a.q;
+        w.h += G;
+        w.at += (out ? o.out_head : o.head) * (long long)(G * sizeof(T));
+    };
     const uint4* const mine = s_ring + (threadIdx.x >> 5) * (kDepth * (int)sizeof(T) * 32) + lane;
     const uint32_t mine_at = smem_u32(mine);
-    auto fetch = [&](int p) {
-        const bool is_k = p >= a.q.passes;
-        const int h = (is_k ? p - a.q.passes : p) * G + g;
-        if (p < p1 && h < (is_k ? a.k.H : a.q.H)) {
-            const T* src = is_k ? k_row + h * a.k.head : q_row + h * a.q.head;
-            const uint32_t dst = mine_at + (p - p0) % kDepth * ((int)sizeof(T) * 512);
+    Way in = {p0, 0, nullptr}, out = {p0, 0, nullptr};
+    set(in, false);
+    set(out, true);
+    const int b0 = c0 * (int)sizeof(T), b1 = c1 * (int)sizeof(T);
+    uint32_t slot = 0;                                 // of the next to be fetched, and of the one at hand
+    auto fetch = [&]() {
+        if (in.p < p1) {
+            if (in.h < (in.p >= a.q.passes ? a.k.H : a.q.H)) {
+                const uint32_t dst = mine_at + slot;
 #pragma unroll
-            for (int i = 0; i < kHalf; ++i) {
-                copy16(dst + i * 512, reinterpret_cast<const uint4*>(src + c0) + i);
-                copy16(dst + (kHalf + i) * 512, reinterpret_cast<const uint4*>(src + c1) + i);
+                for (int i = 0; i < kHalf; ++i) {
+                    copy16(dst + i * 512, in.at + b0 + i * 16);
+                    copy16(dst + (kHalf + i) * 512, in.at + b1 + i * 16);
+                }
             }
+            next(in, false);
         }
         copies_close();
+        slot = slot + (uint32_t)sizeof(T) * 512 == kDepth * (uint32_t)sizeof(T) * 512 ? 0 : slot + (uint32_t)sizeof(T) * 512;
     };
-    for (int u = 0; u < kDepth; ++u) fetch(p0 + u);
+    for (int u = 0; u < kDepth; ++u) fetch();
 
     // sines and cosines of pairs 8 s .. 8 s + 7, side by side
     uint64_t cs[4], sn[4];
@@ -154,21 +179,20 @@ rotate_kernel(const RotateArgs a) {
             w[i] = src ? pair(src[at], src[at + 1]) : pair(1.f, 1.f);
         }
     };
-    for (int p = p0; p < p1; ++p) {
-        const bool is_k = p >= a.q.passes;
-        const int h = (is_k ? p - a.q.passes : p) * G + g;
+    for (; out.p < p1; next(out, true)) {
+        const bool is_k = out.p >= a.q.passes;
         uint64_t x[8];
         copies_wait<kDepth - 1>();
         {
             Raw<T> raw;
-            const uint4* from = mine + (p - p0) % kDepth * ((int)sizeof(T) * 32);
+            const uint4* from = mine + slot / 16;
 #pragma unroll
             for (int i = 0; i < (int)sizeof(T); ++i) raw.v[i] = from[i * 32];
             widen<T>(raw, x);
         }
-        fetch(p + kDepth);
+        fetch();
         if (a.norm) {
-            if (p == p0 || p == a.q.passes) weights(is_k ? a.k.weight : a.q.weight);
+            if (out.p == p0 || out.p == a.q.passes) weights(is_k ? a.k.weight : a.q.weight);
             uint64_t sum = mul_pair(x[0], x[0]);
 #pragma unroll
             for (int i = 1; i < 8; ++i) sum = fma_pair(x[i], x[i], sum);
@@ -209,13 +233,12 @@ rotate_kernel(const RotateArgs a) {
                 }
             }
         }
-        if (h < (is_k ? a.k.H : a.q.H)) {
+        if (out.h < (is_k ? a.k.H : a.q.H)) {
             const Raw<T> r = narrow<T>(x);
-            T* dst = is_k ? k_out + h * a.k.out_head : q_out + h * a.q.out_head;
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
-                reinterpret_cast<uint4*>(dst + c0)[i] = r.v[i];
-                reinterpret_cast<uint4*>(dst + c1)[i] = r.v[kHalf + i];
+                *reinterpret_cast<uint4*>(out.at + b0 + i * 16) = r.v[i];
+                *reinterpret_cast<uint4*>(out.at + b1 + i * 16) = r.v[kHalf + i];
             }
         }
     }
