@@ -219,12 +219,13 @@ __device__ __forceinline__ Slots unit_slots(const PagedAttnArgs& a, long long al
     return {unit + c0, (int)(c1 - c0) + 1};
 }
 
-// Joins the partials.  The first CTAs: one head's output and lse each, or (kUnits: few partials) those of a unit; the others: the weights of NT rows
-// of a sequence.  NT: threads.
+// Joins the partials.  The first CTAs: one head's output and lse each, or (kUnits: few partials) those of a unit; the others: the weights of 128
+// rows of a sequence.  NT: threads.
+constexpr int kMassRows = 128;                         // rows of a CTA of the second kernel
 template <typename T, int DH, int NT, bool kUnits>
 __global__ void __launch_bounds__(NT)
 paged_join_kernel(const PagedAttnArgs a) {
-    constexpr int kJoinThreads = NT, kMassRows = NT;
+    constexpr int kJoinThreads = NT, kShares = NT / kMassRows;           // kShares threads have a row's heads
     // Up to the wait: what needs only the call's inputs, which were complete when the first kernel was let go.
     __shared__ __align__(16) float s_acc[kJoinThreads][4];
     __shared__ float2 s_ml[kJoinThreads];
@@ -416,7 +417,7 @@ paged_join_kernel(const PagedAttnArgs a) {
     }
     __syncthreads();
     if (!sound() || row0 >= len) return;
-    const int row = min(row0 + tid, len - 1), tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
+    const int share = tid / kMassRows, row = min(row0 + tid % kMassRows, len - 1), tile = row >> a.tile_shift, off = row & ((1 << a.tile_shift) - 1), rows_tile = 1 << a.tile_shift;
     const float* x = a.logits + (size_t)(base + tile) * a.heads * rows_tile + off;
     constexpr int kHeads = 16, kAhead = 10;
     float v[kHeads];
@@ -424,7 +425,7 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
         for (int u = 0; u < kHeads; ++u) v[u] = h0 + u < a.Hq ? x[s_off[h0 + u]] : kLow;
     };
-    logits_of(0);
+    logits_of(share * kHeads);
     bool bad = false;
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / 8) {
         const int h = h0 + (tid >> 3), part = tid & 7;
@@ -457,17 +458,22 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         if (h < a.Hq && part == 0) s_lse[h] = L == 0.f ? 0.f : M + log2f(L);       // (every logit -infinity: weights of 0)
     }
-    if (__syncthreads_or(bad) || row0 + tid >= len) return;              // (the outputs' part reports it)
+    if (__syncthreads_or(bad)) return;                 // (the outputs' part reports it)
     float sum = 0.f;
-    for (int h = 0; h < a.Hq; h += kHeads) {           // kHeads loads on their way (a loop of single ones would wait for each)
-        if (h) logits_of(h);
+    for (int h = share * kHeads; h < a.Hq; h += kShares * kHeads) {      // kHeads loads on their way (a loop of single ones would wait for each)
+        if (h != share * kHeads) logits_of(h);
 #pragma unroll
         for (int u = 0; u < kHeads; ++u) sum += h + u < a.Hq ? sm100::fast_exp2(v[u] - s_lse[h + u]) : 0.f;
     }
-    a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
+    if constexpr (kShares > 1) {
+        s_ml[tid].x = sum;
+        __syncthreads();
+        if (share) return;
+        for (int i = 1; i < kShares; ++i) sum += s_ml[tid + i * kMassRows].x;
+    }
+    if (row0 + tid < len) a.mass[(size_t)b * a.d.S_cap() + row] += sum / (float)a.Hq;
 }
 
-constexpr int kLeastMassRows = 128;                    // rows of a CTA of the second kernel
 
 // How the heads of a K/V head are dealt to units, and the line to CTAs.
 struct PagedPlan {
@@ -507,7 +513,7 @@ inline int paged_attention_args(int dtype, const PagedDims& d, const metok_paged
     if (q_seq < 0 || q_head < 0 || out_seq < 0 || out_head < 0 || (q_seq | q_head | out_seq | out_head) % per) return METOK_ERR_INVALID_ARG;
     // outputs of different heads and sequences do not overlap
     if (!rows_apart(d.n_seqs, out_seq, Hq, out_head, d.dh) || !softmax_numbers(softmax_scale, softcap)) return METOK_ERR_INVALID_ARG;
-    const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kLeastMassRows - 1) / kLeastMassRows) : 0);
+    const long long join = (long long)d.n_seqs * Hq + (mass ? (long long)d.n_seqs * ((d.S_cap() + kMassRows - 1) / kMassRows) : 0);
     if (join > 0x7FFFFFFFLL) return METOK_ERR_UNSUPPORTED;
     a->d = d;
     a->Hq = Hq; a->G = p.G; a->NC = p.NC; a->heads = p.heads; a->grid = p.grid; a->tile_shift = p.tile_shift;
@@ -533,7 +539,7 @@ template <typename T, int DH, int NT, bool kUnits>
 int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st, bool spread = false) {
     {
         METOK_TIMED("paged_join", st);
-        const long long blocks = (long long)a.d.n_seqs * (kUnits ? a.d.Hkv * a.NC : a.Hq) + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + NT - 1) / NT) : 0);
+        const long long blocks = (long long)a.d.n_seqs * (kUnits ? a.d.Hkv * a.NC : a.Hq) + (a.mass ? (long long)a.d.n_seqs * ((a.d.S_cap() + kMassRows - 1) / kMassRows) : 0);
         size_t smem = a.mass ? ((size_t)a.d.Hkv * a.NC * 12 + (size_t)a.Hq * 4 + 7) / 8 * 8 + (size_t)a.Hq * 8 : 0;
         if (spread) {
             const long long share = 224 * 1024 / ((blocks + kNumSMs - 1) / kNumSMs) - 8 * 1024;         // (6 KB are static, 1 KB the system's)
