@@ -272,7 +272,7 @@ extern "C" int metok_rotate_heads(int dtype, const metok_rotate_params* p, void*
     if (p->dh != 64 && p->dh != 128) return METOK_ERR_UNSUPPORTED;
     if (p->rotary_dim < 0 || p->rotary_dim > p->dh || p->rotary_dim % 16 || p->n_axes < 1 || p->n_axes > kMaxAxes) return METOK_ERR_INVALID_ARG;
     if (!(p->eps >= 0.f) || p->eps > 3.0e38f) return METOK_ERR_INVALID_ARG;
-    if (p->rotary_dim > 0 && (!p->inv_freq || (!p->positions && p->n_axes > 1))) return METOK_ERR_INVALID_ARG;
+    if (p->rotary_dim > 0 && (!p->inv_freq || (!p->positions && p->n_axes > 1 && p->n > 0))) return METOK_ERR_INVALID_ARG;
     if (!aligned4(p->inv_freq) || !aligned4(p->positions) || !aligned4(p->q_weight) || !aligned4(p->k_weight)) return METOK_ERR_INVALID_ARG;
     const int esize = dtype == METOK_F32 ? 4 : 2, per = 16 / esize;
     RotateArgs a = {};

@@ -130,8 +130,9 @@ def test_zeros_infinities_and_repeats():
     for _ in range(5):
         again = B.metok_rotate_heads(q, k, f, eps=0.0)
         assert torch.equal(again["q"].view(torch.int16), first["q"].view(torch.int16))
-    empty = B.metok_rotate_heads(q[:, :0], k[:, :0], f)
-    assert empty["q"].shape == (4, 0, 128)
+    for pos in (None, torch.zeros((3, 0), dtype=torch.int32, device="cuda")):
+        empty = B.metok_rotate_heads(q[:, :0], k[:, :0], f, pos)
+        assert empty["q"].shape == (4, 0, 128) and empty["k"].shape == (2, 0, 128)
 
 
 def test_captured_and_on_another_stream():
