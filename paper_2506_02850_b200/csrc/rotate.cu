@@ -7,7 +7,7 @@
 //
 // What bounds it is reading and writing Q and K once: the next four turns' elements are on their way to a ring in shared memory, 96 KB for
 // the 24 warps of an SM, that costs no registers (of two turns' in registers, for which there were 16 warps, 76 us).  18 496 rows of 28 + 4 heads of
-// 128: 51.6 us, 5.9 TB/s, as a copy of as many bytes; some 200 operations a turn of a warp, with pointers that are worked out for every turn 56 us.
+// 128: 51.6 us, 5.9 TB/s, as a copy of as many bytes; some 230 operations a turn of a warp, with pointers that are worked out for every turn 56 us.
 #include <math.h>
 
 #include "launchers.h"
