@@ -585,7 +585,7 @@ int launch_paged(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMa
         launch_chained(kern, dim3(a.grid + 1), dim3(kThreads), S::kRing, st, a, tk, tv);
     }
     METOK_LAUNCH_CHECK();
-    return launch_paged_join<T, DH, 128, false>(a, st);
+    return launch_paged_join<T, DH, 128, false, false>(a, st);
 }
 template <int DH>
 int launch_paged_dh(int dtype, const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {

@@ -30,7 +30,6 @@ struct PagedAttnArgs {
     long long* line;                                   // [n_seqs + 1]: tiles of the sequences before each, per unit; then of all
     int32_t* status;
     int withhold;                                      // debug builds: the copies to leave out
-    int marked;                                        // the first kernel marks partials that met a bad page: a sum below 0
 };
 
 // Tiles of sequence b's one unit (0 for a length out of range, which the second kernel reports).
@@ -189,19 +188,26 @@ __device__ __forceinline__ Place find_tile(const PagedAttnArgs& a, int subs, lon
 }
 // The same for a whole CTA: up to 32 sequences every warp looks for itself.
 __device__ __forceinline__ Place find_place(const PagedAttnArgs& a, int subs, long long t_lo, long long t_hi, int* s_b, long long* s_start) {
+    Place p;
     long long start = 0;
-    int b = 0;
-    if (threadIdx.x < 32 || a.d.n_seqs <= 32) b = find_sequence<long long>(a, subs, t_lo, &start);
+    p.b = 0;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);           // the same for all lanes, to the compiler too (0.3 us)
+    if (warp == 0 || a.d.n_seqs <= 32) p.b = find_sequence<long long>(a, subs, t_lo, &start);
     if (a.d.n_seqs > 32 && threadIdx.x == 0) {
-        *s_b = b;
+        *s_b = p.b;
         *s_start = start;
     }
     __syncthreads();
     if (a.d.n_seqs > 32) {
-        b = *s_b;
+        p.b = *s_b;
         start = *s_start;
     }
-    return place_in(a, b, start, t_lo, t_hi);
+    p.nt = unit_tiles(a, p.b);
+    const long long in = t_lo - start;
+    p.sub = (int)(in / p.nt);                          // (64 bits: the caller has just divided so, and the instructions are there)
+    p.t = (int)(in - (long long)p.sub * p.nt);
+    p.left = t_hi - t_lo;
+    return p;
 }
 
 // Logit in log2 units of a raw product: scaled, capped, less the distance's share.
@@ -220,9 +226,10 @@ __device__ __forceinline__ Slots unit_slots(const PagedAttnArgs& a, long long al
 }
 
 // Joins the partials.  The first CTAs: one head's output and lse each, or (kUnits: few partials) those of a unit; the others: the weights of 128
-// rows of a sequence.  NT: threads.
+// rows of a sequence.  NT: threads.  kMarked: the first kernel has marked partials that met a bad page, by a sum below 0; else the pages are looked
+// up here.
 constexpr int kMassRows = 128;                         // rows of a CTA of the second kernel
-template <typename T, int DH, int NT, bool kUnits>
+template <typename T, int DH, int NT, bool kUnits, bool kMarked>
 __global__ void __launch_bounds__(NT)
 paged_join_kernel(const PagedAttnArgs a) {
     constexpr int kJoinThreads = NT, kShares = NT / kMassRows;           // kShares threads have a row's heads
@@ -234,12 +241,12 @@ paged_join_kernel(const PagedAttnArgs a) {
     const int outs = a.d.n_seqs * (kUnits ? a.d.Hkv * a.NC : a.Hq);
     const bool weights = (int)blockIdx.x >= outs;
     const int chunks = (a.d.S_cap() + kMassRows - 1) / kMassRows;
-    const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / (outs / a.d.n_seqs);
+    const int b = weights ? ((int)blockIdx.x - outs) / chunks : (int)blockIdx.x / (kUnits ? a.d.Hkv * a.NC : a.Hq);
     const int len = a.kv_len[b], subs = a.d.Hkv * a.NC;
     const int row0 = weights ? (((int)blockIdx.x - outs) - b * chunks) * kMassRows : 0;
     // the sequence is sound: only then anything is written for it
     bool ok = len >= 0 && len <= a.d.S_cap();
-    if (ok && !a.marked) {
+    if (ok && !kMarked) {
         const int used = (len + (1 << a.d.page_shift) - 1) >> a.d.page_shift;
         bool there = true;
         for (int p = tid; p < used; p += kJoinThreads) {
@@ -250,8 +257,8 @@ paged_join_kernel(const PagedAttnArgs a) {
     }
     const int nt = unit_tiles(a, b);
     long long all = 0, base = 0;                       // tiles of the line, and of the sequences before b
-    const bool few = a.d.n_seqs <= 256;                // a look at all lengths; else the line that the first kernel wrote
-    if (few) {
+    const bool few = a.d.n_seqs <= (kMarked ? kHeldSeqs : 32);           // a look at all lengths; else the line that the first kernel wrote
+    if (few && kMarked) {
         uint32_t sum = 0, before = 0;
         for (int i = lane; i < a.d.n_seqs; i += 32) {
             const uint32_t mine = unit_tiles(a, i);
@@ -260,6 +267,10 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         all = (long long)__reduce_add_sync(0xFFFFFFFFu, sum) * subs;
         base = (long long)__reduce_add_sync(0xFFFFFFFFu, before) * subs;
+    } else if (few) {
+        const int mine = lane < a.d.n_seqs ? unit_tiles(a, lane) : 0;
+        all = (long long)__reduce_add_sync(0xFFFFFFFFu, mine) * subs;
+        base = (long long)__reduce_add_sync(0xFFFFFFFFu, lane < b ? mine : 0) * subs;
     } else {
         grid_dep_wait();
         all = a.line[a.d.n_seqs] * subs;
@@ -299,7 +310,7 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u) {
                         top = fmaxf(top, ml[u].x);
-                        bad |= ml[u].y < 0.f;
+                        bad |= kMarked && ml[u].y < 0.f;
                     }
                     const float less = sm100::fast_exp2(M - top);
                     M = top;
@@ -358,7 +369,7 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 top = fmaxf(top, ml[u].x);
-                bad |= ml[u].y < 0.f;
+                bad |= kMarked && ml[u].y < 0.f;
             }
             const float less = sm100::fast_exp2(M - top);
             M = top;
@@ -373,9 +384,13 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         *reinterpret_cast<float4*>(s_acc[tid]) = acc;
         s_ml[tid] = make_float2(M, L);
-        if (__syncthreads_or(bad)) {
-            if (tid == 0) *a.status = METOK_ERR_INVALID_ARG;
-            return;
+        if constexpr (kMarked) {
+            if (__syncthreads_or(bad)) {
+                if (tid == 0) *a.status = METOK_ERR_INVALID_ARG;
+                return;
+            }
+        } else {
+            __syncthreads();
         }
         if (run == 0) {
 #pragma unroll
@@ -442,7 +457,7 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
                     top = fmaxf(top, p[u].x);
-                    bad |= p[u].y < 0.f;
+                    bad |= kMarked && p[u].y < 0.f;
                 }
                 L *= sm100::fast_exp2(M - top);
 #pragma unroll
@@ -458,7 +473,12 @@ paged_join_kernel(const PagedAttnArgs a) {
         }
         if (h < a.Hq && part == 0) s_lse[h] = L == 0.f ? 0.f : M + log2f(L);       // (every logit -infinity: weights of 0)
     }
-    if (__syncthreads_or(bad)) return;                 // (the outputs' part reports it)
+    if constexpr (kMarked) {
+        if (__syncthreads_or(bad)) return;             // (the outputs' part reports it)
+    } else {
+        __syncthreads();
+    }
+    if (kShares == 1 && row0 + tid >= len) return;
     float sum = 0.f;
     for (int h = share * kHeads; h < a.Hq; h += kShares * kHeads) {      // kHeads loads on their way (a loop of single ones would wait for each)
         if (h != share * kHeads) logits_of(h);
@@ -524,7 +544,6 @@ inline int paged_attention_args(int dtype, const PagedDims& d, const metok_paged
     a->cap_log2 = softcap * kLog2e;
     a->mass = mass; a->lse = lse; a->status = status;
     a->withhold = debug_withheld();
-    a->marked = 0;
     return METOK_OK;
 }
 // What has to hold before a plan can be made.
@@ -535,7 +554,7 @@ inline int paged_attention_heads(const PagedDims& d, const metok_paged_cache* c,
 }
 // spread: the first kernel has whole SMs to its CTAs.  The SMs that it leaves first would take all of the second kernel's CTAs, eight or more of them,
 // so these ask for as much shared memory as lets them share the SMs evenly (120 + 120 CTAs on 30 SMs: 10.5 us instead of 6).
-template <typename T, int DH, int NT, bool kUnits>
+template <typename T, int DH, int NT, bool kUnits, bool kMarked>
 int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st, bool spread = false) {
     {
         METOK_TIMED("paged_join", st);
@@ -545,8 +564,8 @@ int launch_paged_join(const PagedAttnArgs& a, cudaStream_t st, bool spread = fal
             const long long share = 224 * 1024 / ((blocks + kNumSMs - 1) / kNumSMs) - 8 * 1024;         // (6 KB are static, 1 KB the system's)
             smem = std::max(smem, (size_t)std::max(share, 0LL));
         }
-        METOK_ALLOW_SMEM((paged_join_kernel<T, DH, NT, kUnits>), smem);
-        launch_chained(paged_join_kernel<T, DH, NT, kUnits>, dim3((unsigned)blocks), dim3(NT), smem, st, a);
+        METOK_ALLOW_SMEM((paged_join_kernel<T, DH, NT, kUnits, kMarked>), smem);
+        launch_chained(paged_join_kernel<T, DH, NT, kUnits, kMarked>, dim3((unsigned)blocks), dim3(NT), smem, st, a);
     }
     METOK_LAUNCH_CHECK();
     return METOK_OK;

@@ -614,9 +614,9 @@ int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cu
     }
     METOK_LAUNCH_CHECK();
     // a unit's partials are few where the units are many: a CTA joins all of its heads
-    if (a.grid < kNumSMs) return launch_paged_join<T, DH, 128, false>(a, st);
+    if (a.grid < kNumSMs) return launch_paged_join<T, DH, 128, false, true>(a, st);
     const bool few = (long long)a.d.n_seqs * a.d.Hkv * a.NC * 8 >= a.grid;
-    return few ? launch_paged_join<T, DH, 256, true>(a, st, true) : launch_paged_join<T, DH, 256, false>(a, st, true);
+    return few ? launch_paged_join<T, DH, 256, true, true>(a, st, true) : launch_paged_join<T, DH, 256, false, true>(a, st, true);
 }
 template <typename T, int DH>
 int launch_q4_dh(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {
@@ -658,7 +658,6 @@ extern "C" int metok_paged_attention_q4(int dtype, const metok_paged_cache* c, c
     rc = paged_attention_args(dtype, d, c, p, q, q_seq, q_head, Hq, softmax_scale, softcap, slopes, positions, mass, out, out_seq, out_head, lse,
                               status, &a);
     if (rc != METOK_OK) return rc;
-    a.marked = 1;
     if (!ws || !aligned16(ws) || ws_bytes < metok_paged_attention_q4_workspace_bytes(dtype, c, Hq, mass != nullptr)) return METOK_ERR_WORKSPACE;
     Carver cv(ws);
     paged_carve(cv, p, d, mass != nullptr, &a);
