@@ -667,7 +667,7 @@ METOK_API int metok_rotate_heads(int dtype, const metok_rotate_params* p, void* 
  *
  *   metok_paged_attention_q4: (7) over such a cache, q and out of type `dtype` (METOK_F32 or METOK_BF16).
  *   q takes part as one (bf16) or two (fp32) 11-bit numbers per element, relative to the head's
- *   largest; weights in the product with V as one or two 11-bit numbers; logits, sums and accumulated weights are fp32.
+ *   largest; weights in the product with V as two 11-bit numbers; logits, sums and accumulated weights are fp32.
  * ------------------------------------------------------------------------- */
 METOK_API int metok_paged_append_q4(int new_dtype, const metok_paged_cache* c, const void* k_new, const void* v_new,
                         int64_t k_head, int64_t k_row, int64_t v_head, int64_t v_row, int n_new,

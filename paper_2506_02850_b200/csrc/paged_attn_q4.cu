@@ -16,11 +16,12 @@
 // The tensor memory path would take one side of 128 for eight heads, and 4-bit operands of another format whose scales go along the sum, which V's
 // rows do not.
 // Q takes part as fp16 numbers relative to the head's largest element: bf16's eight bits are in one; fp32's are in two to 2^-22.  The weights
-// are 2^12 to 2^15.5 times those relative to the largest and take part as one fp16 number for bf16 outputs (off by 2^-12 of a weight, beside
-// 2^-9 of the output's own rounding), as two for fp32.  Logits, their sums, and outputs up to their end are fp32.
+// are 2^12 to 2^15.5 times those relative to the largest and take part as two fp16 numbers, to 2^-22: as one (off by 2^-11) they moved one bf16
+// output in twelve to forty to another step, and small sums of large terms by several, for 2 to 5 % of the time.  Logits, their sums, and outputs up to
+// their end are fp32.
 //
-// 48 sequences of up to 9001 rows, 28 / 4 heads of 128, capped: 44.5 us with the join, of which reading 157 MB would be 24; some 330 operations a
-// piece (370 capped) at 2.7 a clock.  Three sequences of up to 6313 rows, 40 heads of their own, biased, with weights: 32 us (reading: 13).
+// 48 sequences of up to 9001 rows, 28 / 4 heads of 128, capped: 47.4 us with the join, of which reading 157 MB would be 24.  Three sequences of up to
+// 6313 rows, 40 heads of their own, biased, with weights: 34 us (reading: 13).
 #include "paged_attn.cuh"
 #include "q4.cuh"
 
@@ -91,7 +92,7 @@ struct Q4Block {
     }
 };
 
-// A unit's running softmax.  NG groups of eight heads, QP fp16 numbers per element of Q (and per weight).  Lane l holds the logits of rows
+// A unit's running softmax.  NG groups of eight heads, QP fp16 numbers per element of Q.  Lane l holds the logits of rows
 // pi(l / 4) and pi(l / 4) + 8 of the warp's 16 and of heads 2 (l % 4), + 1; of o the DH / 8 elements from DH / 8 * (l / 4) on.
 template <int DH, int NG, int QP>
 struct Q4Unit {
@@ -320,7 +321,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
             low[n] = pair(-u.m[n][0], -u.m[n][1]);
         }
     }
-    uint32_t p16[RP][QP][NG][2];
+    uint32_t p16[RP][2][NG][2];                        // weights: a number and what it leaves
 #pragma unroll
     for (int r = 0; r < RP; ++r)
 #pragma unroll
@@ -338,7 +339,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
             for (int e = 0; e < 2; ++e) {
                 const __half2 hi = __floats2half2_rn(p[2 * e], p[2 * e + 1]);
                 p16[r][0][n][e] = transpose8x8(as_u32(hi));
-                if constexpr (QP == 2) p16[r][1][n][e] = transpose8x8(pack_f16(p[2 * e] - __low2float(hi), p[2 * e + 1] - __high2float(hi)));
+                p16[r][1][n][e] = transpose8x8(pack_f16(p[2 * e] - __low2float(hi), p[2 * e + 1] - __high2float(hi)));
             }
         }
 #pragma unroll
@@ -381,7 +382,7 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
                 for (int n = 0; n < NG; ++n)
 #pragma unroll
-                    for (int z = 0; z < QP; ++z) {
+                    for (int z = 0; z < 2; ++z) {
                         mma_f16(u.o[n][k], f0[0], f0[1], f1[0], f1[1], p16[r][z][n][0], p16[r][z][n][1]);
                         mma_f16(u.o[n][k + 1], f0[2], f0[3], f1[2], f1[3], p16[r][z][n][0], p16[r][z][n][1]);
                     }
