@@ -94,7 +94,9 @@ rotate_kernel(const RotateArgs a) {
     // the lane's two chunks of eight elements
     const int slots = a.rotary / 16;                   // lanes of a head whose elements turn
     const int c0 = a.interleaved || s >= slots ? 16 * s : 8 * s, c1 = a.interleaved || s >= slots ? 16 * s + 8 : a.rotary / 2 + 8 * s;
-    const int p0 = (int)((uint32_t)passes * part / (uint32_t)a.split), p1 = (int)((uint32_t)passes * (part + 1) / (uint32_t)a.split);
+    // the row's turns: as many for every warp, one more for the first ones (products of turns and warps would pass 32 bits)
+    const int each = (int)((uint32_t)passes / (uint32_t)a.split), over = passes - each * a.split;
+    const int p0 = part * each + min(part, over), p1 = p0 + each + (part < over);
     grid_dep_wait();
     if (row >= a.n) return;                            // uniform in the warp
     // The warp's way over the heads, to be fetched and to be turned: a lane's head, in a turn, and its first element there.
