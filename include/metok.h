@@ -604,7 +604,7 @@ METOK_API int metok_paged_evict(int dtype, const metok_paged_cache* c, void* con
  *     t_i = positions[pair_axis[i]][r] * inv_freq[i],   i = 0 .. rotary_dim/2 - 1,
  *     (y_a, y_b) = (y_a cos t_i - y_b sin t_i,  y_b cos t_i + y_a sin t_i)
  *   where pair i is (a, b) = (i, i + rotary_dim/2), or (2 i, 2 i + 1) if `interleaved`.  Elements
- *   from rotary_dim on do not turn.  fp32 (the sum of squares, too: |x| below 2^60) and rounded
+ *   from rotary_dim on do not turn.  fp32 (the sum of squares, too: |x| below 2^60, however small) and rounded
  *   once; the angles are reduced in 64 bits, so positions may be as large as an int32.
  *
  *   q, q_out [Hq][n][dh], k, k_out [Hkv][n][dh] of `dtype` with the given strides in ELEMENTS

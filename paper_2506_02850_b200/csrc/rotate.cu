@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kWarps = 8, kMaxAxes = 4, kMaxPairs = 64;
 constexpr int kDepth = 4;                              // turns whose elements are on their way
+constexpr float kSmall = 1.2621774483536189e-29f;      // 2^-96: mean squares above it lose next to nothing below fp32's smallest numbers
 
 struct RotateRows {
     const void* x;
@@ -195,15 +196,24 @@ rotate_kernel(const RotateArgs a) {
         fetch();
         if (a.norm) {
             if (out.p == p0 || out.p == a.q.passes) weights(is_k ? a.k.weight : a.q.weight);
-            uint64_t sum = mul_pair(x[0], x[0]);
+            const auto squares = [&](uint32_t lanes) {
+                uint64_t sum = mul_pair(x[0], x[0]);
 #pragma unroll
-            for (int i = 1; i < 8; ++i) sum = fma_pair(x[i], x[i], sum);
-            float ss, odd;
-            unpair(sum, ss, odd);
-            ss += odd;
+                for (int i = 1; i < 8; ++i) sum = fma_pair(x[i], x[i], sum);
+                float ss, odd;
+                unpair(sum, ss, odd);
+                ss += odd;
 #pragma unroll
-            for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-            const float f = rsqrtf(fmaf(ss, 1.f / DH, a.eps));
+                for (int m = 1; m < L; m <<= 1) ss += __shfl_xor_sync(lanes, ss, m);
+                return ss;
+            };
+            float mean = fmaf(squares(0xFFFFFFFFu), 1.f / DH, a.eps);
+            if (mean < kSmall) {                       // few heads: squares that fp32 does not hold.  The same for all lanes of a head
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = mul_pair(x[i], pair(1.f / kSmall, 1.f / kSmall));
+                mean = fmaf(squares(((1u << L) - 1u) << (lane & -L)), 1.f / DH, a.eps * (1.f / kSmall) * (1.f / kSmall));
+            }
+            const float f = rsqrtf(mean);
             const uint64_t f2 = pair(f, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = mul_pair(x[i], mul_pair(f2, w[i]));
