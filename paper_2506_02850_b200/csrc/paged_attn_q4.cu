@@ -132,7 +132,9 @@ struct Q4Unit {
                     const float x0 = x[8 * i + e] * down, x1 = x[8 * i + e + 4] * down;
                     const __half2 hi = __floats2half2_rn(x0, x1);
                     q[0][n][2 * i + (e >> 1)][e & 1] = as_u32(hi);
-                    if constexpr (QP == 2) q[1][n][2 * i + (e >> 1)][e & 1] = pack_f16(x0 - __low2float(hi), x1 - __high2float(hi));
+                    // what is left of an infinite element is nothing (inf - inf would make a NaN of its logits)
+                    const auto rest = [](float x, float h) { return isinf(h) ? 0.f : x - h; };
+                    if constexpr (QP == 2) q[1][n][2 * i + (e >> 1)][e & 1] = pack_f16(rest(x0, __low2float(hi)), rest(x1, __high2float(hi)));
                 }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
