@@ -599,9 +599,10 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
 }
 
 constexpr int kRP = 2;
+// A unit has as many heads as are dealt to it, and so has its room in the workspace; the kernel works on eight or sixteen of them.
 PagedPlan q4_plan(const PagedDims& d, int Hq) {
-    const int G = Hq / d.Hkv, per = ceil_div(G, ceil_div(G, 16)), heads = per <= 8 ? 8 : 16;
-    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads == 8 ? Q4Shape<64, 1, kRP>::kGroups : Q4Shape<64, 2, kRP>::kGroups) * kNumSMs);
+    const int G = Hq / d.Hkv, heads = ceil_div(G, ceil_div(G, 16));
+    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads <= 8 ? Q4Shape<64, 1, kRP>::kGroups : Q4Shape<64, 2, kRP>::kGroups) * kNumSMs);
 }
 
 template <typename T, int DH, int NG, bool kBent, bool kMass>
