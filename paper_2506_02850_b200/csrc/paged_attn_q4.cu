@@ -245,6 +245,8 @@ __device__ __forceinline__ void q4_tile(Q4Unit<DH, NG, QP>& u, const PagedAttnAr
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {   // in units of the cap
                         unpair(mul_pair(two(&x[r][n][i]), pair(a.cap_scale, a.cap_scale)), x[r][n][i], x[r][n][i + 1]);
+                        // rows that are not there have no say in how the others are capped
+                        if (kPart && r0 + 16 * r + 4 * i >= rows) x[r][n][i] = x[r][n][i + 1] = 0.f;
                         most = fmaxf(most, fmaxf(fabsf(x[r][n][i]), fabsf(x[r][n][i + 1])));
                     }
             if (__any_sync(0xFFFFFFFFu, !(most <= 1.f))) {
