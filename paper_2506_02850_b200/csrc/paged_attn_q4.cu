@@ -155,7 +155,8 @@ struct Q4Unit {
 
 __device__ __forceinline__ int row_at(int r) { return r ^ (r >> 2 & 1); }          // pi: the row at place r of eight
 
-// tanh(y) of logits in units of the cap, |y| <= 1: y P(y^2), P the polynomial of degree 6 of least largest relative error (5e-8; 1.6e-7 in fp32).
+// tanh(y) of logits in units of the cap, |y| <= 1: y P(y^2), P the polynomial of degree 6 of least largest relative error (7e-8 with coefficients in
+// fp32; 1.6e-7 worked out in fp32).
 __device__ __forceinline__ uint64_t tanh_near(uint64_t y) {
     using namespace sm100;
     const auto both = [](float c) { return pair(c, c); };
@@ -600,11 +601,12 @@ paged_attn_q4_kernel(const PagedAttnArgs a, const uint8_t* __restrict__ k_pool, 
     if (threadIdx.x == 0 && s_abort) *a.status = METOK_ERR_TIMEOUT;
 }
 
-constexpr int kRP = 2;
+constexpr int kRP = 2, kTileShift = 7;                 // (one piece a warp at a time: a sixth slower)
+static_assert(Q4Shape<64, 1, kRP>::kTile == 1 << kTileShift, "rows of a tile");
 // A unit has as many heads as are dealt to it, and so has its room in the workspace; the kernel works on eight or sixteen of them.
 PagedPlan q4_plan(const PagedDims& d, int Hq) {
     const int G = Hq / d.Hkv, heads = ceil_div(G, ceil_div(G, 16));
-    return paged_plan_of(d, Hq, heads, kRP == 2 ? 7 : 6, (heads <= 8 ? Q4Shape<64, 1, kRP>::kGroups : Q4Shape<64, 2, kRP>::kGroups) * kNumSMs);
+    return paged_plan_of(d, Hq, heads, kTileShift, (heads <= 8 ? Q4Shape<64, 1, kRP>::kGroups : Q4Shape<64, 2, kRP>::kGroups) * kNumSMs);
 }
 
 template <typename T, int DH, int NG, bool kBent, bool kMass>
@@ -619,7 +621,10 @@ int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cu
         launch_chained(kern, dim3(std::min(a.grid, kNumSMs)), dim3(S::kThreads), smem, st, a, (const uint8_t*)k_pool, (const uint8_t*)v_pool);
     }
     METOK_LAUNCH_CHECK();
-    // a unit's partials are few where the units are many: a CTA joins all of its heads
+    // A unit's partials are few where the units are many: a CTA joins all of its heads (192 units 42.8 us the call, a head at a time 48.6; 80 18.2 and 19.4; 56
+    // 15.3 and 15.0; 28 15.3 and 13.4; with weights units lose 1 to 26 us from 80 units on, but
+    // outputs are to be the same as without).
+    // Where the line is short, small CTAs (30 short sequences 8.3 us, of 256 threads 10.6; one of 300 rows 6.0 and 6.3).
     if (a.grid < kNumSMs) return launch_paged_join<T, DH, 128, false, true>(a, st);
     const bool few = (long long)a.d.n_seqs * a.d.Hkv * a.NC * 8 >= a.grid;
     return few ? launch_paged_join<T, DH, 256, true, true>(a, st, true) : launch_paged_join<T, DH, 256, false, true>(a, st, true);
@@ -627,6 +632,7 @@ int launch_q4(const PagedAttnArgs& a, const void* k_pool, const void* v_pool, cu
 template <typename T, int DH>
 int launch_q4_dh(const PagedAttnArgs& a, const void* k, const void* v, cudaStream_t st) {
     const bool bent = a.cap_log2 > 0.f || a.slopes, mass = a.mass != nullptr;
+    // (sixteen heads have no kernels of their own for calls without cap and bias: 66 us instead of 68 for 48 sequences of 36 / 4 heads, fp32 87 instead of 91)
     if (a.heads > 8) return mass ? launch_q4<T, DH, 2, true, true>(a, k, v, st) : launch_q4<T, DH, 2, true, false>(a, k, v, st);
     if (bent) return mass ? launch_q4<T, DH, 1, true, true>(a, k, v, st) : launch_q4<T, DH, 1, true, false>(a, k, v, st);
     return mass ? launch_q4<T, DH, 1, false, true>(a, k, v, st) : launch_q4<T, DH, 1, false, false>(a, k, v, st);

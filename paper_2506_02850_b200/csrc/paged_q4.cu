@@ -3,7 +3,7 @@
 // A CTA takes up to 32 new (packed) rows: its first warp finds where each of them lies in the cache, a lane each, then a thread takes a block of
 // 16 elements (words of eight) of its row in head after head, so that what it works out about the row serves all of them.
 // 53 653 rows of 4 heads of 128: in 35 us, 141 MB (20.7 M instructions at 2.5 a clock and SM; a copy of as many bytes takes 26), out 32 us.
-// 18 496 rows out: 11.4 us cold.  With places worked out for every item 24 M instructions either way and 40 us in; of 64 or more rows a CTA
+// 18 496 rows out: 13 us, 9.9 where outputs stay in L2, 14 from cold caches.  With places worked out for every item 24 M instructions either way and 40 us in; of 64 or more rows a CTA
 // takes longer to begin and they go out in 40 to 57 us.
 #include "launchers.h"
 #include "paged.cuh"

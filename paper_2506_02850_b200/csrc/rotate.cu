@@ -5,9 +5,9 @@
 // out one or two of the pairs' angles and the groups exchange them: t = position * inv_freq / 2 pi in 64 bits, of which the distance to
 // the nearest integer is exact enough for any int32 position, and sincospi of that in 32.  Elements are worked on two at a time.
 //
-// What bounds it is reading and writing Q and K once: the next four turns' elements are on their way to a ring in shared memory, 96 KB for
-// the 24 warps of an SM, that costs no registers (of two turns' in registers, for which there were 16 warps, 76 us).  18 496 rows of 28 + 4 heads of
-// 128: 51.6 us, 5.9 TB/s, as a copy of as many bytes; some 230 operations a turn of a warp, with pointers that are worked out for every turn 56 us.
+// What bounds it is reading and writing Q and K once: the next four turns' elements are on their way to a ring in shared memory, 96 KB (fp32:
+// 192) for the 24 warps of an SM, that costs no registers (of two turns' in registers, for which there were 16 warps, 76 us).  18 496 rows of 28 + 4 heads of
+// 128: 52 us, 5.8 TB/s, as a copy of as many bytes (56 in passes that go on for long); some 230 operations a turn of a warp, with pointers that are worked out for every turn 56 us.
 #include <math.h>
 
 #include "launchers.h"
@@ -320,7 +320,8 @@ extern "C" int metok_rotate_heads(int dtype, const metok_rotate_params* p, void*
     if (sides == 2 && !apart(out[0], out[1])) return METOK_ERR_INVALID_ARG;
     a.n = p->n; a.rotary = p->rotary_dim; a.interleaved = p->interleaved != 0; a.norm = p->norm != 0;
     a.eps = p->eps; a.inv_freq = p->inv_freq; a.positions = p->positions;
-    // few rows: a row's heads are dealt to as many warps as keep 32 of them on every SM
+    // few rows: a row's heads are dealt to 32 warps for every SM, which holds 24 (with 24: 600 rows of 28 + 4 heads 5.5 us instead of 5.3, 2000 of 14 + 2
+    // 5.5 instead of 5.1, 1000 of 28 + 4 6.3 instead of 6.5; others alike)
     const int passes = a.q.passes + a.k.passes;
     a.split = std::max(1, std::min(passes, (int)std::min<long long>(passes, (32LL * kNumSMs + p->n - 1) / p->n)));
     const long long blocks = ((long long)p->n * a.split + kWarps - 1) / kWarps;

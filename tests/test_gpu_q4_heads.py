@@ -35,3 +35,16 @@ def test_bias_by_indices_and_positions_without_a_bias(dtype, Hq, Hkv):
         (out, lse, _), (out_err, lse_err, _), absv, most = reference(c, q, 0.125, 0.0, slopes, index, b)
         tol = out_err + HALF[dtype] * out.abs() + 2.0 ** -22 * absv + 2.0 ** -37 * n * most
         assert bool(((got["out"][b].double() - out).abs() <= tol).all()) and bool(((got["lse"][b].double() - lse).abs() <= lse_err + STEP * lse.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq,Hkv,dh,n_seqs", [(28, 4, 128, 3), (28, 4, 128, 20), (12, 1, 64, 70), (5, 5, 64, 2)])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
+def test_outputs_do_not_depend_on_weights_or_lse(dtype, Hq, Hkv, dh, n_seqs, cap):
+    c = Codes([3000 // n_seqs + 37 * b for b in range(n_seqs)], Hkv, dh, 16, seed=4, growth=1)
+    q = torch.randn((n_seqs, Hq, dh), generator=c.g, device="cuda").to(dtype)
+    call = lambda mass, lse: B.metok_paged_attention_q4(q, c.k, c.v, c.block_table, c.kv_len, 0.1, softcap=cap, mass=mass, with_lse=lse)
+    want, weighed, bare = call(None, True), call(c.mass.clone(), True), call(c.mass.clone(), False)
+    torch.cuda.synchronize()
+    assert torch.equal(weighed["out"], want["out"]) and torch.equal(weighed["lse"], want["lse"])
+    assert torch.equal(bare["out"], want["out"]) and "lse" not in bare
